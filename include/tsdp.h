@@ -409,6 +409,75 @@ int tsdp_verify_commit_static(int device, int T, float beta0, float beta1, float
                               const tsdp_accept_t* accept, uint64_t seed, float draft_nfe, float* d_actions,
                               int* h_t_new, int* h_jstar, float* d_logalpha, void* cuda_stream);
 
+/* ---- Operators of a training step ---------------------------------------------------------------------------------
+ *
+ * What a caller needs beside tsdp_gemm to tune the networks that this library runs (a UNet or transformer drafter, Sec. 3.2
+ * "Draft Model Training"): GroupNorm with its activation and FiLM vectors, forward and backward; saved activations in eight
+ * bits; the weight gradients of projections and convolutions, which read them.
+ *
+ * They need no context.  Every buffer is the caller's, device memory of GPU `device` (which need not be the current one and
+ * does not become it).  A call only enqueues kernels on `cuda_stream`: it neither waits nor allocates, and may be captured into a graph.
+ * Two calls in flight at once need workspaces of their own.  The same inputs give the same bits on every run.
+ * Tensors are [N, L, C] (sequences, positions, channels), channels innermost without a gap, strides x_n of a sequence and x_l of a
+ * position in ELEMENTS (so the zero-padded layout and channel slices of wider rows can be given as they are); what lies between
+ * rows is neither read nor written.  Rows in 16-byte pieces (strides, C and address) take the fast kernels, all others
+ * are served too.  N = 0 is a call with nothing to do (gradients of parameters become zero).
+ * Errors: ARG (null pointers, sizes, strides under which written rows overlap, workspace too small), CUDA (text on stderr). */
+enum { TSDP_TYPE_FP32 = 0, TSDP_TYPE_BF16 = 1 };
+enum { TSDP_ACT_NONE = 0, TSDP_ACT_MISH = 1, TSDP_ACT_SILU = 2, TSDP_ACT_GELU = 3 /* tanh form */ };
+enum { TSDP_MAX_TAPS = 15 };
+
+/* A tensor kept in eight bits: dense rows r = n L + l, q [N L, C] and scale [N L, ceil(C / 32)].  Channels 32 j .. 32 j + 31 of a row
+ * stand for q 2^(scale - 127), |q| <= 127; scale is the smallest of 1 .. 248 for which no rounded value exceeds 127, so that a value
+ * is off by half a step at most (2^(scale-128), 2^-7 of the block's largest magnitude); rounding to nearest, halves to even.  A
+ * block with an infinity or a NaN has scale 255 and stands for NaN. */
+typedef struct {
+  int8_t* q;
+  uint8_t* scale;
+} tsdp_saved_t;
+
+int tsdp_checkpoint_pack(int device, int dtype, const void* d_x, int64_t x_n, int64_t x_l, int N, int L, int C,
+                         const tsdp_saved_t* out, void* cuda_stream);
+/* The values that a copy stands for; exact in either type. */
+int tsdp_checkpoint_unpack(int device, int dtype, const tsdp_saved_t* in, void* d_x, int64_t x_n, int64_t x_l, int N, int L,
+                           int C, void* cuda_stream);
+
+/* C a multiple of groups, C / groups <= 2048, eps > 0. */
+typedef struct {
+  int dtype;
+  int N, L, C, groups;
+  int act;
+  float eps;
+} tsdp_norm_t;
+
+/* y = scale act(gamma (x - mean) rstd + beta) + bias, mean and rstd = 1 / sqrt(variance + eps) over the L positions and C / groups channels
+ * of each group.  gamma, beta [C] fp32; d_film [N, 2C] fp32 (scale, then bias) or null; x, y of the type in `shape`; d_mean, d_rstd
+ * [N, groups] fp32 or null; saved_x, saved_y (null: none) receive the 8-bit copies of x and of y as it was rounded.
+ * d_y may be d_x with the same strides. */
+int tsdp_group_norm(int device, const tsdp_norm_t* shape, const void* d_x, int64_t x_n, int64_t x_l, const float* d_gamma,
+                    const float* d_beta, const float* d_film, void* d_y, int64_t y_n, int64_t y_l, float* d_mean, float* d_rstd,
+                    const tsdp_saved_t* saved_x, const tsdp_saved_t* saved_y, void* cuda_stream);
+
+/* Gradients of the same: from dy to dx, dgamma, dbeta [C] fp32 and dfilm [N, 2C] fp32 (null to skip).  The forward pass's input comes as
+ * d_x or, where saved_x is given, as its 8-bit copy; d_mean and d_rstd are the forward pass's (act, gamma, beta, film too).  d_dx may
+ * be d_dy with the same strides.  shape->eps is not used.  Workspace: tsdp_group_norm_grad_workspace bytes (0 on a bad argument). */
+size_t tsdp_group_norm_grad_workspace(int device, const tsdp_norm_t* shape);
+int tsdp_group_norm_grad(int device, const tsdp_norm_t* shape, const void* d_dy, int64_t dy_n, int64_t dy_l, const void* d_x,
+                         int64_t x_n, int64_t x_l, const tsdp_saved_t* saved_x, const float* d_gamma, const float* d_beta,
+                         const float* d_film, const float* d_mean, const float* d_rstd, void* d_dx, int64_t dx_n, int64_t dx_l,
+                         float* d_dgamma, float* d_dbeta, float* d_dfilm, void* d_workspace, size_t workspace_bytes,
+                         void* cuda_stream);
+
+/* Weight gradient of a projection (taps = 1) or of a convolution with `taps` (odd) taps and zero padding taps / 2, its input given as its
+ * 8-bit copy [N L, K]:
+ *     dW[tap][i][o] = sum_{n, l} x[n, l + tap - taps / 2, i] dy[n, l, o],     db[o] = sum_{n, l} dy[n, l, o]
+ * dW [taps, K, O] and db [O] (null to skip) fp32, the order of tsdp_load_weights' matrices ([in, out], convolutions [tap, in, out]).
+ * d_dy [N L, O] of type dtype, rows dy_l elements apart.  Products are exact (an fp32 dy is taken in three bf16 parts), sums fp32.  A wait inside the
+ * kernel that expires (each is bounded) leaves NaN in dW.  Workspace: tsdp_weight_grad_workspace bytes, on a 16-byte boundary. */
+size_t tsdp_weight_grad_workspace(int device, int dtype, int N, int L, int K, int O, int taps);
+int tsdp_weight_grad(int device, int dtype, const tsdp_saved_t* saved_x, const void* d_dy, int64_t dy_l, int N, int L, int K,
+                     int O, int taps, float* d_dW, float* d_db, void* d_workspace, size_t workspace_bytes, void* cuda_stream);
+
 #ifdef __cplusplus
 }
 #endif

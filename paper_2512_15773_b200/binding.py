@@ -16,7 +16,10 @@ EXPORTS = ["tsdp_init", "tsdp_destroy", "tsdp_strerror", "tsdp_last_error", "tsd
            "tsdp_load_weights", "tsdp_set_schedule", "tsdp_sample_chunk", "tsdp_sample_chunk_host",
            "tsdp_round", "tsdp_denoise", "tsdp_gemm", "tsdp_gemm_timed", "tsdp_stats", "tsdp_reset_stats",
            "tsdp_kernel_launches", "tsdp_profile", "tsdp_profile_read", "tsdp_verify_commit_static", "tsdp_set_scheduler", "tsdp_set_progress",
-           "tsdp_sched_eval", "tsdp_serve", "tsdp_request_counts", "tsdp_process_reward", "tsdp_distill_loss", "tsdp_distill_step", "tsdp_debug_arm_gemm_timeout", "tsdp_debug_arm_round_failure", "tsdp_debug_check_guards"]
+           "tsdp_sched_eval", "tsdp_serve", "tsdp_request_counts", "tsdp_process_reward", "tsdp_distill_loss", "tsdp_distill_step", "tsdp_debug_arm_gemm_timeout", "tsdp_debug_arm_round_failure", "tsdp_debug_check_guards",
+           "tsdp_checkpoint_pack", "tsdp_checkpoint_unpack", "tsdp_group_norm", "tsdp_group_norm_grad_workspace", "tsdp_group_norm_grad",
+           "tsdp_weight_grad_workspace", "tsdp_weight_grad"]
+ACT = {"none": 0, "mish": 1, "silu": 2, "gelu": 3}
 PROF_FAMILIES = ["gemm", "layernorm", "attention", "embed_head", "round", "small_net", "gemm_draft", "drafter_cluster", "accept", "verifier_cluster",
                  "layernorm_draft", "attention_draft", "embed_head_draft"]
 
@@ -44,6 +47,15 @@ class StatsT(C.Structure):
                 ("hist_drafted", C.c_uint64 * TSDP_MAX_T), ("hist_tested", C.c_uint64 * TSDP_MAX_T),
                 ("hist_accepted", C.c_uint64 * TSDP_MAX_T), ("call_ms_p50", C.c_double), ("call_ms_p99", C.c_double),
                 ("call_ms_samples", C.c_uint64), ("cand_dense", C.c_uint64), ("cand_computed", C.c_uint64)]
+
+
+class SavedT(C.Structure):
+    _fields_ = [("q", C.c_void_p), ("scale", C.c_void_p)]
+
+
+class NormT(C.Structure):
+    _fields_ = [("dtype", C.c_int), ("N", C.c_int), ("L", C.c_int), ("C", C.c_int), ("groups", C.c_int), ("act", C.c_int),
+                ("eps", C.c_float)]
 
 
 class TsdpError(RuntimeError):
@@ -96,6 +108,16 @@ def load_library():
     lib.tsdp_kernel_launches.argtypes = [vp]; lib.tsdp_kernel_launches.restype = u64
     lib.tsdp_profile.argtypes = [vp, i]
     lib.tsdp_profile_read.argtypes = [vp, fp, fp, fp]
+    i64, saved = C.c_int64, C.POINTER(SavedT)
+    lib.tsdp_checkpoint_pack.argtypes = [i, i, vp, i64, i64, i, i, i, saved, vp]
+    lib.tsdp_checkpoint_unpack.argtypes = [i, i, saved, vp, i64, i64, i, i, i, vp]
+    lib.tsdp_group_norm.argtypes = [i, C.POINTER(NormT), vp, i64, i64, vp, vp, vp, vp, i64, i64, vp, vp, saved, saved, vp]
+    lib.tsdp_group_norm_grad_workspace.argtypes = [i, C.POINTER(NormT)]
+    lib.tsdp_group_norm_grad_workspace.restype = C.c_size_t
+    lib.tsdp_group_norm_grad.argtypes = [i, C.POINTER(NormT), vp, i64, i64, vp, i64, i64, saved, vp, vp, vp, vp, vp, vp, i64, i64,
+                                         vp, vp, vp, vp, C.c_size_t, vp]
+    lib.tsdp_weight_grad_workspace.argtypes = [i, i, i, i, i, i, i]; lib.tsdp_weight_grad_workspace.restype = C.c_size_t
+    lib.tsdp_weight_grad.argtypes = [i, i, saved, vp, i64, i, i, i, i, i, vp, vp, vp, C.c_size_t, vp]
     _lib = lib
     return lib
 
@@ -164,6 +186,165 @@ def verify_commit_static(d_xt, d_muhat, d_eps, h_t, B, K, D, accept, seed, d_act
                                        _ptr(h_t_new), _ptr(h_jstar), _ptr(d_logalpha), stream)
     if st != 0:
         raise TsdpError(st, "tsdp_verify_commit_static", lib.tsdp_strerror(st).decode())
+
+
+# ---------------------------------------------------------------------------------------------- operators of a training step
+# Module-level functions on torch tensors (see tsdp.h): they check types, shapes and devices, which the C side cannot see, and
+# only enqueue work on `stream` (a cudaStream_t; 0 is the default stream).  The tensors have to live until that work is done.
+
+def _dtype_code(t, name):
+    s = str(t.dtype)
+    if s == "torch.bfloat16":
+        return 1
+    if s == "torch.float32":
+        return 0
+    raise ValueError(f"{name}: bfloat16 or float32 expected, got {s}")
+
+
+def _rows(t, name, like=None):
+    """(address, stride of a sequence, stride of a position, N, L, C) of a tensor [N, L, C] or [rows, C]."""
+    if t.device.type != "cuda":
+        raise ValueError(f"{name}: a CUDA tensor expected")
+    shape, stride = t.shape, t.stride()
+    if len(shape) == 2:
+        shape, stride = (1, *shape), (0, *stride)
+    if len(shape) != 3:
+        raise ValueError(f"{name}: [N, L, C] or [rows, C] expected, got {tuple(t.shape)}")
+    if stride[2] != 1 and shape[2] != 1:
+        raise ValueError(f"{name}: channels have to be innermost, without a gap")
+    if like is not None and (t.shape != like.shape or t.dtype != like.dtype or t.device != like.device):
+        raise ValueError(f"{name}: {tuple(like.shape)} of {like.dtype} on {like.device} expected, got {tuple(t.shape)} of {t.dtype} on {t.device}")
+    return t.data_ptr(), stride[0], stride[1], *shape
+
+
+def _dense(t, name, shape, dtype, device):
+    """Address of a dense tensor of this shape and type on this device; None stays None."""
+    if t is None:
+        return None
+    if t.shape != shape or str(t.dtype) != dtype or t.device != device or not t.is_contiguous():
+        raise ValueError(f"{name}: contiguous {tuple(shape)} of {dtype} on {device} expected, got {tuple(t.shape)} of {t.dtype} on {t.device}")
+    return t.data_ptr()
+
+
+def _saved(pair, name, rows, channels, device):
+    """The 8-bit copy (q, scale) as the C side takes it; None stays None."""
+    if pair is None:
+        return None
+    q, scale = pair
+    if q.numel() != rows * channels or q.shape[-1] != channels:
+        raise ValueError(f"{name}: q of {rows} rows of {channels} channels expected, got {tuple(q.shape)}")
+    if scale.numel() != rows * (-(-channels // 32)):
+        raise ValueError(f"{name}: {-(-channels // 32)} scales for each of {rows} rows expected, got {tuple(scale.shape)}")
+    return SavedT(_dense(q, name + " q", q.shape, "torch.int8", device), _dense(scale, name + " scale", scale.shape, "torch.uint8", device))
+
+
+def _act(act):
+    if act not in ACT:
+        raise ValueError(f"act: one of {sorted(ACT)} expected, got {act!r}")
+    return ACT[act]
+
+
+def _status(st, what):
+    if st != 0:
+        raise TsdpError(st, what, load_library().tsdp_strerror(st).decode())
+
+
+def saved_like(x):
+    """An empty 8-bit copy (q, scale) for a tensor [N, L, C] or [rows, C]."""
+    import torch
+    return (torch.empty(x.shape, dtype=torch.int8, device=x.device),
+            torch.empty((*x.shape[:-1], -(-x.shape[-1] // 32)), dtype=torch.uint8, device=x.device))
+
+
+def checkpoint_pack(x, saved, stream=0):
+    """Write the 8-bit copy of x into saved = (q, scale)."""
+    p, sn, sl, N, L, ch = _rows(x, "x")
+    _status(load_library().tsdp_checkpoint_pack(x.device.index, _dtype_code(x, "x"), p, sn, sl, N, L, ch,
+                                                _saved(saved, "saved", N * L, ch, x.device), stream), "tsdp_checkpoint_pack")
+
+
+def checkpoint_unpack(saved, x, stream=0):
+    """Write the values that saved = (q, scale) stands for into x."""
+    p, sn, sl, N, L, ch = _rows(x, "x")
+    _status(load_library().tsdp_checkpoint_unpack(x.device.index, _dtype_code(x, "x"), _saved(saved, "saved", N * L, ch, x.device), p, sn,
+                                                  sl, N, L, ch, stream), "tsdp_checkpoint_unpack")
+
+
+def group_norm(x, gamma, beta, groups, y, act="mish", film=None, eps=1e-5, mean=None, rstd=None, saved_x=None, saved_y=None, stream=0):
+    """y = film scale * act(GroupNorm(x)) + film bias; mean, rstd [N, groups] and the 8-bit copies of x and y where given."""
+    p, sn, sl, N, L, ch = _rows(x, "x")
+    yp, yn, yl, *_ = _rows(y, "y", x)
+    dev, f32 = x.device, "torch.float32"
+    shape = NormT(_dtype_code(x, "x"), N, L, ch, groups, _act(act), eps)
+    _status(load_library().tsdp_group_norm(
+        dev.index, shape, p, sn, sl, _dense(gamma, "gamma", (ch,), f32, dev), _dense(beta, "beta", (ch,), f32, dev),
+        _dense(film, "film", (N, 2 * ch), f32, dev), yp, yn, yl, _dense(mean, "mean", (N, groups), f32, dev),
+        _dense(rstd, "rstd", (N, groups), f32, dev), _saved(saved_x, "saved_x", N * L, ch, dev), _saved(saved_y, "saved_y", N * L, ch, dev),
+        stream), "tsdp_group_norm")
+
+
+def group_norm_grad_workspace(dy, groups):
+    """Bytes of workspace that group_norm_grad takes for gradients like dy."""
+    _, _, _, N, L, ch = _rows(dy, "dy")
+    n = load_library().tsdp_group_norm_grad_workspace(dy.device.index, NormT(_dtype_code(dy, "dy"), N, L, ch, groups, 0, 1e-5))
+    if n == 0:
+        raise TsdpError(1, "tsdp_group_norm_grad_workspace", "sizes")
+    return n
+
+
+def group_norm_grad(dy, x, gamma, beta, groups, mean, rstd, dx, dgamma, dbeta, workspace, act="mish", film=None, dfilm=None,
+                    saved_x=None, stream=0):
+    """Gradients of group_norm: dx, dgamma, dbeta and, where given, dfilm; the input as x or (x None) as its 8-bit copy saved_x."""
+    p, sn, sl, N, L, ch = _rows(dy, "dy")
+    if (x is None) == (saved_x is None):
+        raise ValueError("x, saved_x: one of the two expected")
+    xp, xn, xl = (None, 0, 0) if x is None else _rows(x, "x", dy)[:3]
+    dp, dn, dl, *_ = _rows(dx, "dx", dy)
+    dev, f32 = dy.device, "torch.float32"
+    shape = NormT(_dtype_code(dy, "dy"), N, L, ch, groups, _act(act), 1.0)
+    _status(load_library().tsdp_group_norm_grad(
+        dev.index, shape, p, sn, sl, xp, xn, xl, _saved(saved_x, "saved_x", N * L, ch, dev), _dense(gamma, "gamma", (ch,), f32, dev),
+        _dense(beta, "beta", (ch,), f32, dev), _dense(film, "film", (N, 2 * ch), f32, dev), _dense(mean, "mean", (N, groups), f32, dev),
+        _dense(rstd, "rstd", (N, groups), f32, dev), dp, dn, dl, _dense(dgamma, "dgamma", (ch,), f32, dev),
+        _dense(dbeta, "dbeta", (ch,), f32, dev), _dense(dfilm, "dfilm", (N, 2 * ch), f32, dev), *_workspace(workspace, dev), stream),
+        "tsdp_group_norm_grad")
+
+
+def _workspace(t, device):
+    if t.device != device or not t.is_contiguous():
+        raise ValueError(f"workspace: a contiguous tensor on {device} expected")
+    return t.data_ptr(), t.numel() * t.element_size()
+
+
+def _weight_sizes(dy, taps, length):
+    p, _, sl, _, rows, out = _rows(dy, "dy")
+    if dy.dim() != 2:
+        raise ValueError(f"dy: [rows, out] expected, got {tuple(dy.shape)}")
+    L = max(rows, 1) if length is None else length
+    if L < 1 or rows % L:
+        raise ValueError(f"length: a divisor of the {rows} rows expected, got {L}")
+    return p, sl, rows // L, L, out
+
+
+def weight_grad_workspace(dy, channels, taps=1, length=None):
+    """Bytes of workspace that weight_grad takes for gradients like dy and `channels` input channels."""
+    _, _, N, L, out = _weight_sizes(dy, taps, length)
+    n = load_library().tsdp_weight_grad_workspace(dy.device.index, _dtype_code(dy, "dy"), N, L, channels, out, taps)
+    if n == 0:
+        raise TsdpError(1, "tsdp_weight_grad_workspace", "sizes")
+    return n
+
+
+def weight_grad(saved_x, dy, dW, workspace, db=None, length=None, stream=0):
+    """dW [taps, in, out] (or [in, out]) and db [out] from dy [rows, out] and the 8-bit copy of the layer's input [rows, in];
+    length: rows of a sequence, beyond whose ends a convolution sees zeros (default: all rows are one sequence)."""
+    taps, channels = (1, dW.shape[0]) if dW.dim() == 2 else dW.shape[:2]
+    p, sl, N, L, out = _weight_sizes(dy, taps, length)
+    dev, f32 = dy.device, "torch.float32"
+    shape = (channels, out) if dW.dim() == 2 else (taps, channels, out)
+    _status(load_library().tsdp_weight_grad(
+        dev.index, _dtype_code(dy, "dy"), _saved(saved_x, "saved_x", N * L, channels, dev), p, sl, N, L, channels, out, taps,
+        _dense(dW, "dW", shape, f32, dev), _dense(db, "db", (out,), f32, dev), *_workspace(workspace, dev), stream), "tsdp_weight_grad")
 
 
 class Sampler:

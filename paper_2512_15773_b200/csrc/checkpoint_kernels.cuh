@@ -1,0 +1,159 @@
+// Activations kept in eight bits between the forward and the backward pass of a training step.
+//
+// A row of C channels is cut into blocks of 32.  A block is 32 whole numbers q, |q| <= 127, and one byte b, and stands for
+// q * 2^(b - 127); b is the smallest in 1 .. 248 with max |rint(x 2^(127 - b))| <= 127, and 255 for a block that holds an infinity
+// or a NaN (read back as NaN).  The scale is a power of two, so that scaling is exact in every type, a copy depends on nothing but
+// the values, and what it stands for is exact in bf16 (7 bits and a sign): the backward products take it without a rounding.
+// The one rounding is that to q, half a step at most: |x - q 2^(b-127)| <= 2^(b-128), 2^-7 of the block's largest value.
+// (b = 249 would stand for values past the largest fp32: there q stays at 127 instead.)
+#pragma once
+#include "common.cuh"
+
+namespace tsdp {
+
+struct Rows { void* p; long long sn, sl; };          // element (n, l, c) at p + n sn + l sl + c
+struct Copy8 { signed char* q; unsigned char* b; };  // dense rows r = n L + l: q [rows, C], b [rows, (C + 31) / 32]
+
+__host__ __device__ inline int copy_blocks(int C) { return (C + 31) >> 5; }
+
+// b from the bits of the block's largest magnitude (bits of non-negative floats order like the values, NaN above infinity).
+// 127.5 = 1.9921875 * 2^6 is the first value that rounds to 128: from a mantissa of 0x7f0000 on the exponent goes up by one.
+__device__ __forceinline__ uint32_t copy_byte(uint32_t top) {
+  if (top >= 0x7f800000u) return 255u;
+  return (uint32_t)min(max((int)((top + 0x10000u) >> 23) - 6, 1), 248);
+}
+__device__ __forceinline__ float copy_inv_step(uint32_t b) { return __uint_as_float(b == 255u ? 0u : (254u - b) << 23); }     // 2^(127-b)
+__device__ __forceinline__ float copy_step(uint32_t b) { return __uint_as_float(b == 255u ? 0x7fc00000u : b << 23); }        // 2^(b-127)
+// q of one value, in the low byte: x 2^(127-b) is exact, the sum with 1.5 * 2^23 rounds it to a whole number, halves to even.
+__device__ __forceinline__ uint32_t copy_q(float x, float inv, uint32_t b) {
+  float s = x * inv;
+  if (b == 248u) s = fminf(fmaxf(s, -127.f), 127.f);
+  return b == 255u ? 0u : __float_as_uint(s + 12582912.f) & 0xffu;
+}
+// Four of them in a word.
+__device__ __forceinline__ uint32_t copy_q4(const float* x, float inv, uint32_t b) {
+  uint32_t w[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    float s = x[i] * inv;
+    if (b == 248u) s = fminf(fmaxf(s, -127.f), 127.f);
+    w[i] = __float_as_uint(s + 12582912.f);
+  }
+  const uint32_t r = __byte_perm(__byte_perm(w[0], w[1], 0x0040), __byte_perm(w[2], w[3], 0x0040), 0x5410);
+  return b == 255u ? 0u : r;
+}
+__device__ __forceinline__ float copy_value(uint32_t word, int i, float step) {
+  return (float)(signed char)(word >> (8 * i)) * step;
+}
+
+// V consecutive values as fp32; V * sizeof(T) = 16 bytes, or one value.
+template <typename T, int V> __device__ __forceinline__ void load_values(const T* p, float* v) {
+  if constexpr (V == 1) {
+    v[0] = to_f(*p);
+  } else if constexpr (sizeof(T) == 2) {
+    const uint4 u = *reinterpret_cast<const uint4*>(p);
+    const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) { v[2 * i] = __uint_as_float(w[i] << 16); v[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u); }
+  } else {
+    const float4 u = *reinterpret_cast<const float4*>(p);
+    v[0] = u.x; v[1] = u.y; v[2] = u.z; v[3] = u.w;
+  }
+}
+template <typename T, int V> __device__ __forceinline__ void store_values(T* p, const float* v) {
+  if constexpr (V == 1) {
+    *p = from_f<T>(v[0]);
+  } else if constexpr (sizeof(T) == 2) {
+    *reinterpret_cast<uint4*>(p) = make_uint4(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7]));
+  } else {
+    *reinterpret_cast<float4*>(p) = make_float4(v[0], v[1], v[2], v[3]);
+  }
+}
+
+// Eight channels a thread, four neighbouring lanes a block of 32; a row's threads are counted in whole blocks, so that the four lanes of
+// a block sit side by side whatever C is.  A thread keeps its channels and walks the rows.  C % 8 = 0, 16-byte aligned rows.
+constexpr int COPY_THREADS = 256;
+template <typename T>
+__global__ void __launch_bounds__(COPY_THREADS)
+checkpoint_pack_kernel(Rows x, Copy8 out, int N, int L, int C) {
+  const int units = 4 * copy_blocks(C), per = min(units, COPY_THREADS);      // threads on a row
+  const int lanes = COPY_THREADS / per, lane = threadIdx.x / per;
+  const long long rows = (long long)N * L;
+  for (long long r0 = (long long)blockIdx.x * lanes; r0 < rows; r0 += (long long)gridDim.x * lanes) {
+    const long long r = r0 + lane;
+    const bool row_in = lane < lanes && r < rows;
+    const long long n = L == 1 ? r : r / L;
+    const T* row = reinterpret_cast<const T*>(x.p) + n * x.sn + (r - n * L) * x.sl;
+    for (int u0 = 0; u0 < units; u0 += per) {
+      const int u = u0 + threadIdx.x - lane * per, c = 8 * u;
+      const bool in = row_in && c < C;
+      float v[8] = {};
+      if (in) {
+        load_values<T, 16 / sizeof(T)>(row + c, v);
+        if constexpr (sizeof(T) == 4) load_values<T, 4>(row + c + 4, v + 4);
+      }
+      uint32_t top = 0;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) top = max(top, __float_as_uint(v[i]) & 0x7fffffffu);
+      top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
+      top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
+      const uint32_t b = copy_byte(top);
+      const float inv = copy_inv_step(b);
+      if (in) *reinterpret_cast<uint2*>(out.q + r * C + c) = make_uint2(copy_q4(v, inv, b), copy_q4(v + 4, inv, b));
+      if (in && (u & 3) == 0) out.b[r * copy_blocks(C) + (u >> 2)] = (unsigned char)b;
+    }
+  }
+}
+
+// Any width, any alignment: a warp per block, a lane per channel.
+template <typename T>
+__global__ void __launch_bounds__(COPY_THREADS)
+checkpoint_pack_any_kernel(Rows x, Copy8 out, int N, int L, int C) {
+  const int nb = copy_blocks(C), lane = threadIdx.x & 31;
+  const long long blocks = (long long)N * L * nb;
+  for (long long i = (long long)blockIdx.x * (COPY_THREADS / 32) + (threadIdx.x >> 5); i < blocks; i += (long long)gridDim.x * (COPY_THREADS / 32)) {
+    const long long r = i / nb, n = r / L;
+    const int c = (int)(i - r * nb) * 32 + lane;
+    float v = 0.f;
+    if (c < C) v = to_f(reinterpret_cast<const T*>(x.p)[n * x.sn + (r - n * L) * x.sl + c]);
+    const uint32_t b = copy_byte(__reduce_max_sync(0xffffffffu, __float_as_uint(v) & 0x7fffffffu));
+    if (c < C) out.q[r * C + c] = (signed char)copy_q(v, copy_inv_step(b), b);
+    if (lane == 0) out.b[i] = (unsigned char)b;
+  }
+}
+
+template <typename T>
+__global__ void __launch_bounds__(COPY_THREADS)
+checkpoint_unpack_kernel(Copy8 in, Rows x, int N, int L, int C) {
+  const int units = C >> 3, per = min(units, COPY_THREADS);
+  const int lanes = COPY_THREADS / per, lane = threadIdx.x / per;
+  const long long rows = (long long)N * L;
+  if (lane >= lanes) return;
+  for (long long r = (long long)blockIdx.x * lanes + lane; r < rows; r += (long long)gridDim.x * lanes) {
+    const long long n = L == 1 ? r : r / L;
+    T* row = reinterpret_cast<T*>(x.p) + n * x.sn + (r - n * L) * x.sl;
+    for (int u = threadIdx.x - lane * per; u < units; u += per) {
+      const uint2 w = *reinterpret_cast<const uint2*>(in.q + r * C + 8 * u);
+      const float step = copy_step(in.b[r * copy_blocks(C) + (u >> 2)]);
+      float v[8];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) { v[i] = copy_value(w.x, i, step); v[4 + i] = copy_value(w.y, i, step); }
+      store_values<T, 16 / sizeof(T)>(row + 8 * u, v);
+      if constexpr (sizeof(T) == 4) store_values<T, 4>(row + 8 * u + 4, v + 4);
+    }
+  }
+}
+
+template <typename T>
+__global__ void __launch_bounds__(COPY_THREADS)
+checkpoint_unpack_any_kernel(Copy8 in, Rows x, int N, int L, int C) {
+  const int nb = copy_blocks(C), lane = threadIdx.x & 31;
+  const long long blocks = (long long)N * L * nb;
+  for (long long i = (long long)blockIdx.x * (COPY_THREADS / 32) + (threadIdx.x >> 5); i < blocks; i += (long long)gridDim.x * (COPY_THREADS / 32)) {
+    const long long r = i / nb, n = r / L;
+    const int c = (int)(i - r * nb) * 32 + lane;
+    if (c < C) reinterpret_cast<T*>(x.p)[n * x.sn + (r - n * L) * x.sl + c] = from_f<T>((float)in.q[r * C + c] * copy_step(in.b[i]));
+  }
+}
+
+}  // namespace tsdp

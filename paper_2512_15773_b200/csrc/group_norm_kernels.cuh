@@ -1,0 +1,420 @@
+// GroupNorm with an activation and FiLM vectors over channels-last activations, and its gradients, for training.
+//
+//   h = (x - mean_g) rstd_g       mean, 1 / sqrt(variance + eps) over the L positions and C / groups channels of a group
+//   z = gamma h + beta,  a = act(z),  y = scale a + bias          scale, bias [N, C]: the FiLM vectors, 1 and 0 without them
+//
+//   dz = dy scale act'(z);   dbeta = sum dz;   dgamma = sum dz h;   dscale = sum_l dy a;   dbias = sum_l dy
+//   dx = rstd (gamma dz - m1 - h m2),   m1, m2: means over the group of gamma dz and gamma dz h
+//
+// The group sums of the last line follow from the sums over l of dz and dz h that a channel needs anyway:
+// sum_group gamma dz = sum_c gamma_c sum_l dz.
+//
+// What bounds them: bytes. Forward x and y once each, backward dy, x (or its 8-bit copy) and dx.
+// A cluster of CTAs owns some groups of one sequence, each CTA a share of the positions: statistics need all of a group before its
+// first output.  A thread owns V neighbouring channels (16 bytes) and walks positions, so that the affine and FiLM
+// vectors stay in registers and sums over positions need no exchange until the end.  The second walk reads x (and dy) again: what the cluster has just read is in the L2.
+#pragma once
+#include "checkpoint_kernels.cuh"
+#include "gemm_tcgen05.cuh"
+
+namespace tsdp {
+
+enum { ACT_NONE = 0, ACT_MISH = 1, ACT_SILU = 2, ACT_GELU = 3 };
+
+// a = act(z) and its derivative.  One exponential and one division each, on the fast instructions: e^v by ex2.approx is off by 2 units
+// of 2^-24 and by the rounding of v log2(e), 2e-6 of e^v at the ends of the range where it matters (|z| <= 20).
+// Mish: with u = e^z, d = (u + 1)^2 + 1:  tanh(log(1 + u)) = u (u + 2) / d,  derivative t + 4 z u (u + 1) / d^2.  Past z = 20 both are
+// those of the identity to 2^-24, and u is held there so that it stays finite.
+// GELU (tanh form): 1/2 (1 + tanh w) = 1 / (1 + e^-2w).
+struct ActValue { float a, d; };
+__device__ __forceinline__ float act_recip(float v) { return __fdividef(1.f, v); }
+template <bool GRAD> __device__ __forceinline__ ActValue act_mish(float z) {
+  const float zc = z > 20.f ? 20.f : z;                    // (a NaN stays one)
+  const float u = __expf(zc), w = u + 1.f, r = act_recip(fmaf(w, w, 1.f));
+  const float t = u * (u + 2.f) * r;
+  return {z * t, GRAD ? fmaf(4.f * zc * r, r * u * w, t) : 0.f};
+}
+template <bool GRAD> __device__ __forceinline__ ActValue act_silu(float z) {
+  const float s = act_recip(1.f + __expf(-z)), a = z * s;
+  return {a, GRAD ? fmaf(a, 1.f - s, s) : 0.f};
+}
+template <bool GRAD> __device__ __forceinline__ ActValue act_gelu(float z) {
+  const float k = 0.7978845608028654f, q = fminf(z * z, 1e4f);      // (past |z| = 100 the logistic function is 0 or 1)
+  const float s = act_recip(1.f + __expf(-2.f * k * z * fmaf(0.044715f, q, 1.f))), a = z * s;
+  return {a, GRAD ? fmaf(a * (1.f - s), 2.f * k * fmaf(0.134145f, q, 1.f), s) : 0.f};
+}
+template <bool GRAD, int V> __device__ __forceinline__ void act_values(int act, const float* z, float* a, float* d) {
+#define TSDP_ACT_LOOP(EXPR)                                  \
+  _Pragma("unroll") for (int i = 0; i < V; ++i) {            \
+    const ActValue r = EXPR;                                 \
+    a[i] = r.a;                                              \
+    if (GRAD) d[i] = r.d;                                    \
+  }
+  if (act == ACT_MISH) { TSDP_ACT_LOOP(act_mish<GRAD>(z[i])) }
+  else if (act == ACT_SILU) { TSDP_ACT_LOOP(act_silu<GRAD>(z[i])) }
+  else if (act == ACT_GELU) { TSDP_ACT_LOOP(act_gelu<GRAD>(z[i])) }
+  else { TSDP_ACT_LOOP((ActValue{z[i], 1.f})) }
+#undef TSDP_ACT_LOOP
+}
+
+struct NormArgs {
+  int N, L, C, groups, act;
+  float eps;
+  Rows x, y, dy, dx;
+  const float *gamma, *beta, *film;            // film [N, 2C]: scale, bias; null
+  float *mean, *rstd;                          // [N, groups]
+  Copy8 cx, cy;                                // forward: 8-bit copies to write (q null: none); backward: cx is x
+  float *dfilm, *part;                         // [N, 2C] or null; [splits, 2, C]
+  // the plan: a set is `per_set` groups, `width` channels; cols threads on a position; `ranks` CTAs of a cluster share the positions
+  int per_set, sets, width, cols, lanes, ranks, splits;
+};
+
+constexpr int GN_THREADS = 256;
+constexpr int GN_MAX_WIDTH = 2048;             // channels of a set: their sums stay in shared memory
+
+__device__ __forceinline__ float ld_rank_f32(const float* p, uint32_t rank) {       // the same shared-memory word of another CTA of the cluster
+  float v;
+  asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(ptx::mapa_rank(ptx::smem_u32(p), rank)) : "memory");
+  return v;
+}
+
+// Positions of lane r of a share [lo, hi) walked in steps of `lanes`.
+__device__ __forceinline__ int lane_rows(int lo, int hi, int r, int lanes) { return max(0, (hi - lo - r + lanes - 1) / lanes); }
+
+// ------------------------------------------------------------------------------------------------------------------ forward
+// First walk: each thread keeps, per channel, the sums about its own first value (so that a large mean costs no digits); mean and centred
+// sum of squares of its share are then merged, thread by thread and CTA by CTA, with their counts: M2 = sum M2_i + n_i (mean_i - mean)^2.
+template <typename T, int V>
+__global__ void __launch_bounds__(GN_THREADS)
+group_norm_kernel(NormArgs g) {
+  extern __shared__ __align__(16) float gn_smem[];
+  const int cg = g.C / g.groups;
+  float* s_mean = gn_smem;                                  // [lanes][tile channels]
+  float* s_m2 = s_mean + GN_THREADS * V;                    // the same
+  float* s_grp = s_m2 + GN_THREADS * V;                     // [2][per_set]: this CTA's mean and M2
+  float* s_stat = s_grp + 2 * g.per_set;                    // [2][per_set]: mean and rstd
+  const uint32_t rank = g.ranks > 1 ? ptx::cluster_rank() : 0u;
+  const int set = (blockIdx.x / g.ranks) % g.sets, split = blockIdx.x / g.ranks / g.sets;
+  const int c_set = set * g.width, width = min(g.width, g.C - c_set), n_grp = width / cg;
+  const int share = (g.L + g.ranks - 1) / g.ranks, lo = min(g.L, (int)rank * share), hi = min(g.L, lo + share);
+  const int lane = threadIdx.x / g.cols, col = threadIdx.x - lane * g.cols, tile = g.cols * V;
+  const int warp = threadIdx.x >> 5, wl = threadIdx.x & 31;
+  for (int n = split; n < g.N; n += g.splits) {
+    const T* x = reinterpret_cast<const T*>(g.x.p) + n * g.x.sn + c_set;
+    // a group may be wider than a tile of columns: its parts are merged in turn
+    for (int t0 = 0; t0 < width; t0 += tile) {
+      const int c = t0 + col * V;
+      const bool in = lane < g.lanes && c < width;
+      if (in) {
+        float k[V], s[V], q[V];
+#pragma unroll
+        for (int i = 0; i < V; ++i) k[i] = s[i] = q[i] = 0.f;
+        int l = lo + lane;
+        if (l < hi) load_values<T, V>(x + l * g.x.sl + c, k);
+        constexpr int U = 4;
+        for (; l < hi; l += U * g.lanes) {
+          float v[U][V];
+#pragma unroll
+          for (int j = 0; j < U; ++j) {
+#pragma unroll
+            for (int i = 0; i < V; ++i) v[j][i] = k[i];
+            if (l + j * g.lanes < hi) load_values<T, V>(x + (l + j * g.lanes) * g.x.sl + c, v[j]);
+          }
+#pragma unroll
+          for (int j = 0; j < U; ++j)
+#pragma unroll
+            for (int i = 0; i < V; ++i) { const float d = v[j][i] - k[i]; s[i] += d; q[i] = fmaf(d, d, q[i]); }
+        }
+        const int cnt = lane_rows(lo, hi, lane, g.lanes);
+        const float inv = cnt ? 1.f / cnt : 0.f;
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+          s_mean[lane * tile + col * V + i] = fmaf(s[i], inv, k[i]);
+          s_m2[lane * tile + col * V + i] = fmaf(-s[i] * inv, s[i], q[i]);
+        }
+      }
+      __syncthreads();
+      // groups that this tile holds (a part of): a warp each
+      const int t1 = min(width, t0 + tile);
+      for (int gr = t0 / cg + warp; gr * cg < t1; gr += GN_THREADS / 32) {
+        const int a = max(gr * cg, t0) - t0, b = min(gr * cg + cg, t1) - t0, w = b - a, items = w * g.lanes;
+        float sum = 0.f;
+        for (int i = wl; i < items; i += 32) {
+          const int r = i / w;
+          sum += lane_rows(lo, hi, r, g.lanes) * s_mean[r * tile + a + i - r * w];
+        }
+        const float cnt = (float)(hi - lo) * w;
+        const float m = cnt > 0.f ? warp_sum(sum) / cnt : 0.f;
+        float m2 = 0.f;
+        for (int i = wl; i < items; i += 32) {
+          const int r = i / w, rows = lane_rows(lo, hi, r, g.lanes);
+          const float d = s_mean[r * tile + a + i - r * w] - m;
+          if (rows) m2 += s_m2[r * tile + a + i - r * w] + rows * d * d;
+        }
+        m2 = warp_sum(m2);
+        if (wl == 0) {
+          if (gr * cg >= t0) { s_grp[gr] = m; s_grp[g.per_set + gr] = m2; }
+          else {                                            // the group began in an earlier tile, with `before` channels of it
+            const float nb = (float)(hi - lo) * (t0 - gr * cg), d = m - s_grp[gr], f = nb + cnt > 0.f ? cnt / (nb + cnt) : 0.f;
+            s_grp[gr] += d * f;
+            s_grp[g.per_set + gr] += m2 + d * d * nb * f;
+          }
+        }
+      }
+      __syncthreads();
+    }
+    if (g.ranks > 1) ptx::cluster_sync_all();
+    for (int gr = threadIdx.x; gr < n_grp; gr += GN_THREADS) {
+      float m = s_grp[gr], m2 = s_grp[g.per_set + gr];
+      if (g.ranks > 1) {
+        m = 0.f; m2 = 0.f;
+        for (int r = 0; r < g.ranks; ++r) m += ld_rank_f32(s_grp + gr, r) * (float)max(0, min(g.L, (r + 1) * share) - min(g.L, r * share));
+        m /= (float)g.L;
+        for (int r = 0; r < g.ranks; ++r) {
+          const float rows = (float)max(0, min(g.L, (r + 1) * share) - min(g.L, r * share)), d = ld_rank_f32(s_grp + gr, r) - m;
+          if (rows > 0.f) m2 += ld_rank_f32(s_grp + g.per_set + gr, r) + d * d * rows * cg;
+        }
+      }
+      const float rs = rsqrtf(m2 / ((float)g.L * cg) + g.eps);
+      s_stat[gr] = m; s_stat[g.per_set + gr] = rs;
+      if (rank == 0) {
+        const long long at = (long long)n * g.groups + c_set / cg + gr;
+        if (g.mean) g.mean[at] = m;
+        if (g.rstd) g.rstd[at] = rs;
+      }
+    }
+    __syncthreads();
+    // second walk
+    T* y = reinterpret_cast<T*>(g.y.p) + n * g.y.sn + c_set;
+    for (int t0 = 0; t0 < width; t0 += tile) {
+      const int c = t0 + col * V;
+      const bool in = lane < g.lanes && c < width;
+      float ga[V], be[V], mu[V], rs[V], fs[V], fb[V];
+#pragma unroll
+      for (int i = 0; i < V; ++i) { ga[i] = be[i] = mu[i] = rs[i] = fb[i] = 0.f; fs[i] = 1.f; }
+      if (in) {
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+          const int gr = (c + i) / cg;
+          ga[i] = g.gamma[c_set + c + i]; be[i] = g.beta[c_set + c + i];
+          mu[i] = s_stat[gr]; rs[i] = s_stat[g.per_set + gr];
+          if (g.film) { fs[i] = g.film[(long long)n * 2 * g.C + c_set + c + i]; fb[i] = g.film[((long long)n * 2 + 1) * g.C + c_set + c + i]; }
+        }
+      }
+      for (int l0 = lo; l0 < hi; l0 += g.lanes) {             // (a whole CTA's trip: the copies' blocks span lanes)
+        const int l = l0 + lane;
+        const bool row = in && l < hi;
+        float v[V], z[V], a[V], d[V];
+#pragma unroll
+        for (int i = 0; i < V; ++i) v[i] = 0.f;
+        if (row) load_values<T, V>(x + l * g.x.sl + c, v);
+#pragma unroll
+        for (int i = 0; i < V; ++i) z[i] = fmaf((v[i] - mu[i]) * rs[i], ga[i], be[i]);
+        act_values<false, V>(g.act, z, a, d);
+#pragma unroll
+        for (int i = 0; i < V; ++i) a[i] = to_f(from_f<T>(fmaf(a[i], fs[i], fb[i])));
+        if (row) store_values<T, V>(y + l * g.y.sl + c, a);
+        if constexpr (V > 1) {
+          const long long r = (long long)n * g.L + l;
+#pragma unroll
+          for (int which = 0; which < 2; ++which) {
+            const Copy8& o = which ? g.cy : g.cx;
+            if (o.q == nullptr) continue;
+            const float* w = which ? a : v;
+            uint32_t top = 0;
+#pragma unroll
+            for (int i = 0; i < V; ++i) top = max(top, row ? __float_as_uint(w[i]) & 0x7fffffffu : 0u);
+#pragma unroll
+            for (int o2 = 1; o2 < 32 / V; o2 *= 2) top = max(top, __shfl_xor_sync(0xffffffffu, top, o2));
+            const uint32_t b = copy_byte(top);
+            const float inv = copy_inv_step(b);
+            if (row) {
+              if constexpr (V == 8) *reinterpret_cast<uint2*>(o.q + r * g.C + c_set + c) = make_uint2(copy_q4(w, inv, b), copy_q4(w + 4, inv, b));
+              else *reinterpret_cast<uint32_t*>(o.q + r * g.C + c_set + c) = copy_q4(w, inv, b);
+              if ((c & 31) == 0) o.b[r * copy_blocks(g.C) + ((c_set + c) >> 5)] = (unsigned char)b;
+            }
+          }
+        }
+      }
+    }
+    if (g.ranks > 1) ptx::cluster_sync_all();               // s_grp may be written again once every CTA has read it
+    else __syncthreads();
+  }
+  if (g.ranks > 1) ptx::cluster_sync_all();                 // no CTA leaves while another may read its shared memory
+}
+
+// ------------------------------------------------------------------------------------------------------------------ backward
+// V values of x as the forward pass saw it (COPY: as its 8-bit copy has it).
+template <typename T, int V, bool COPY>
+__device__ __forceinline__ void load_x(const NormArgs& g, int n, int l, int c, float* v) {
+  if constexpr (!COPY) {
+    load_values<T, V>(reinterpret_cast<const T*>(g.x.p) + n * g.x.sn + l * g.x.sl + c, v);
+  } else {
+    const long long r = (long long)n * g.L + l;
+    const float step = copy_step(g.cx.b[r * copy_blocks(g.C) + (c >> 5)]);
+    const signed char* q = g.cx.q + r * g.C + c;
+    if constexpr (V == 1) v[0] = (float)*q * step;
+    else {
+      uint32_t w[2];
+      if constexpr (V == 8) { const uint2 u = *reinterpret_cast<const uint2*>(q); w[0] = u.x; w[1] = u.y; }
+      else w[0] = *reinterpret_cast<const uint32_t*>(q);
+#pragma unroll
+      for (int i = 0; i < V; ++i) v[i] = copy_value(w[i >> 2], i & 3, step);
+    }
+  }
+}
+
+template <int V> struct NormVectors { float ga[V], be[V], mu[V], rs[V], fs[V]; };
+template <int V>
+__device__ __forceinline__ void norm_vectors(const NormArgs& g, int n, int c, bool in, NormVectors<V>& p) {
+  const int cg = g.C / g.groups;
+#pragma unroll
+  for (int i = 0; i < V; ++i) {
+    p.ga[i] = p.be[i] = p.mu[i] = p.rs[i] = 0.f; p.fs[i] = 1.f;
+    if (in) {
+      const int gr = (c + i) / cg;
+      p.ga[i] = g.gamma[c + i]; p.be[i] = g.beta[c + i];
+      p.mu[i] = g.mean[(long long)n * g.groups + gr]; p.rs[i] = g.rstd[(long long)n * g.groups + gr];
+      if (g.film) p.fs[i] = g.film[(long long)n * 2 * g.C + c + i];
+    }
+  }
+}
+
+// dz, h and dy a of V values
+template <typename T, int V, bool COPY>
+__device__ __forceinline__ void norm_dz(const NormArgs& g, int n, int l, int c, const NormVectors<V>& p, float* dz, float* h, float* dy, float* dya) {
+  float x[V], z[V], a[V], d[V];
+  load_x<T, V, COPY>(g, n, l, c, x);
+  load_values<T, V>(reinterpret_cast<const T*>(g.dy.p) + n * g.dy.sn + l * g.dy.sl + c, dy);
+#pragma unroll
+  for (int i = 0; i < V; ++i) { h[i] = (x[i] - p.mu[i]) * p.rs[i]; z[i] = fmaf(h[i], p.ga[i], p.be[i]); }
+  act_values<true, V>(g.act, z, a, d);
+#pragma unroll
+  for (int i = 0; i < V; ++i) { dz[i] = dy[i] * p.fs[i] * d[i]; dya[i] = dy[i] * a[i]; }
+}
+
+// A cluster walks the sequences split, split + splits, ... and keeps its channels' share of dgamma and dbeta in shared memory.
+template <typename T, int V, bool COPY>
+__global__ void __launch_bounds__(GN_THREADS)
+group_norm_grad_kernel(NormArgs g) {
+  extern __shared__ __align__(16) float gn_smem[];
+  const int cg = g.C / g.groups;
+  float* s_lane = gn_smem;                                  // [4][lanes][tile channels]: sums of a lane
+  float* s_sum = s_lane + 4 * GN_THREADS * V;               // [4][width]: of the CTA
+  float* s_tot = s_sum + 4 * g.width;                       // [2][width]: of the cluster (dz, dz h)
+  float* s_acc = s_tot + 2 * g.width;                       // [2][width]: over the sequences so far
+  float* s_grp = s_acc + 2 * g.width;                       // [2][per_set]: m1, m2
+  const uint32_t rank = g.ranks > 1 ? ptx::cluster_rank() : 0u;
+  const int set = (blockIdx.x / g.ranks) % g.sets, split = blockIdx.x / g.ranks / g.sets;
+  const int c_set = set * g.width, width = min(g.width, g.C - c_set), n_grp = width / cg;
+  const int share = (g.L + g.ranks - 1) / g.ranks, lo = min(g.L, (int)rank * share), hi = min(g.L, lo + share);
+  const int lane = threadIdx.x / g.cols, col = threadIdx.x - lane * g.cols, tile = g.cols * V;
+  const int warp = threadIdx.x >> 5, wl = threadIdx.x & 31;
+  const bool film = g.film != nullptr && g.dfilm != nullptr;
+  const int sums = film ? 4 : 2;
+  for (int i = threadIdx.x; i < 2 * g.width; i += GN_THREADS) s_acc[i] = 0.f;
+  for (int n = split; n < g.N; n += g.splits) {
+    for (int t0 = 0; t0 < width; t0 += tile) {
+      const int c = t0 + col * V;
+      const bool in = lane < g.lanes && c < width;
+      if (in) {
+        NormVectors<V> p;
+        norm_vectors<V>(g, n, c_set + c, true, p);
+        float s0[V], s1[V], s2[V], s3[V];
+#pragma unroll
+        for (int i = 0; i < V; ++i) s0[i] = s1[i] = s2[i] = s3[i] = 0.f;
+#pragma unroll 2
+        for (int l = lo + lane; l < hi; l += g.lanes) {
+          float dz[V], h[V], dy[V], dya[V];
+          norm_dz<T, V, COPY>(g, n, l, c_set + c, p, dz, h, dy, dya);
+#pragma unroll
+          for (int i = 0; i < V; ++i) { s0[i] += dz[i]; s1[i] = fmaf(dz[i], h[i], s1[i]); s2[i] += dya[i]; s3[i] += dy[i]; }
+        }
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+          float* o = s_lane + lane * tile + col * V + i;
+          o[0] = s0[i]; o[GN_THREADS * V] = s1[i];
+          if (film) { o[2 * GN_THREADS * V] = s2[i]; o[3 * GN_THREADS * V] = s3[i]; }
+        }
+      }
+      __syncthreads();
+      const int w = min(width - t0, tile);
+      for (int i = threadIdx.x; i < sums * w; i += GN_THREADS) {
+        const int k = i / w, cc = i - k * w;
+        float s = 0.f;
+        for (int r = 0; r < g.lanes; ++r) s += s_lane[k * GN_THREADS * V + r * tile + cc];
+        s_sum[k * g.width + t0 + cc] = s;
+      }
+      __syncthreads();
+    }
+    if (g.ranks > 1) ptx::cluster_sync_all();
+    for (int i = threadIdx.x; i < sums * width; i += GN_THREADS) {
+      const int k = i / width, c = i - k * width;
+      float s = s_sum[k * g.width + c];
+      if (g.ranks > 1) {
+        s = 0.f;
+        for (int r = 0; r < g.ranks; ++r) s += ld_rank_f32(s_sum + k * g.width + c, r);
+      }
+      if (k < 2) { s_tot[k * g.width + c] = s; s_acc[k * g.width + c] += s; }
+      else if (rank == 0) g.dfilm[((long long)n * 2 + k - 2) * g.C + c_set + c] = s;
+    }
+    __syncthreads();
+    const float inv = 1.f / ((float)g.L * cg);
+    for (int gr = warp; gr < n_grp; gr += GN_THREADS / 32) {
+      float a = 0.f, b = 0.f;
+      for (int i = wl; i < cg; i += 32) {
+        const float ga = g.gamma[c_set + gr * cg + i];
+        a = __fadd_rn(a, __fmul_rn(ga, s_tot[gr * cg + i])); b = __fadd_rn(b, __fmul_rn(ga, s_tot[g.width + gr * cg + i]));
+      }
+      a = warp_sum(a); b = warp_sum(b);
+      if (wl == 0) { s_grp[gr] = a * inv; s_grp[g.per_set + gr] = b * inv; }
+    }
+    __syncthreads();
+    T* dx = reinterpret_cast<T*>(g.dx.p) + n * g.dx.sn + c_set;
+    for (int t0 = 0; t0 < width; t0 += tile) {
+      const int c = t0 + col * V;
+      if (!(lane < g.lanes && c < width)) continue;
+      NormVectors<V> p;
+      norm_vectors<V>(g, n, c_set + c, true, p);
+      float m1[V], m2[V];
+#pragma unroll
+      for (int i = 0; i < V; ++i) { m1[i] = s_grp[(c + i) / cg]; m2[i] = s_grp[g.per_set + (c + i) / cg]; }
+#pragma unroll 2
+      for (int l = lo + lane; l < hi; l += g.lanes) {
+        float dz[V], h[V], dy[V], dya[V];
+        norm_dz<T, V, COPY>(g, n, l, c_set + c, p, dz, h, dy, dya);
+#pragma unroll
+        for (int i = 0; i < V; ++i) dz[i] = p.rs[i] * fmaf(-h[i], m2[i], __fadd_rn(__fmul_rn(dz[i], p.ga[i]), -m1[i]));
+        store_values<T, V>(dx + l * g.dx.sl + c, dz);
+      }
+    }
+    if (g.ranks > 1) ptx::cluster_sync_all();
+    else __syncthreads();
+  }
+  __syncthreads();
+  if (rank == 0)
+    for (int i = threadIdx.x; i < 2 * width; i += GN_THREADS) {
+      const int k = i / width, c = i - k * width;
+      g.part[((long long)split * 2 + k) * g.C + c_set + c] = s_acc[k * g.width + c];
+    }
+  if (g.ranks > 1) ptx::cluster_sync_all();
+}
+
+// dbeta, dgamma: the shares of the splits, in their order.
+constexpr int GN_JOIN_CH = 32, GN_JOIN_LANES = 8;
+__global__ void __launch_bounds__(GN_JOIN_CH * GN_JOIN_LANES)
+group_norm_join_kernel(const float* part, int splits, int C, float* dgamma, float* dbeta) {
+  __shared__ float s[GN_JOIN_LANES][GN_JOIN_CH];
+  const int c = blockIdx.x * GN_JOIN_CH + (threadIdx.x % GN_JOIN_CH), k = blockIdx.y, lane = threadIdx.x / GN_JOIN_CH;
+  float v = 0.f;
+  if (c < C)
+    for (int i = lane; i < splits; i += GN_JOIN_LANES) v += part[((long long)i * 2 + k) * C + c];
+  s[lane][threadIdx.x % GN_JOIN_CH] = v;
+  __syncthreads();
+  if (lane == 0 && c < C) {
+    for (int i = 1; i < GN_JOIN_LANES; ++i) v += s[i][threadIdx.x];
+    (k ? dgamma : dbeta)[c] = v;
+  }
+}
+
+}  // namespace tsdp

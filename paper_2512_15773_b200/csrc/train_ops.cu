@@ -1,0 +1,404 @@
+// Host side of the operators of a training step (include/tsdp.h): checks of arguments, the plan of a launch, the launches.
+// They need no context: every buffer is the caller's, every call only enqueues work on the caller's stream.
+#include <cuda.h>
+#include <cuda_runtime.h>
+
+#include <atomic>
+#include <cstdio>
+
+#include "../../include/tsdp.h"
+#include "checkpoint_kernels.cuh"
+#include "group_norm_kernels.cuh"
+#include "weight_grad_tcgen05.cuh"
+
+using namespace tsdp;
+
+namespace {
+
+constexpr int MAX_DEVICES = 64;
+
+// The caller's device for the time of a call, the one that was current afterwards.
+struct DeviceScope {
+  int before = -1;
+  cudaError_t err;
+  explicit DeviceScope(int device) {
+    err = cudaGetDevice(&before);
+    if (err == cudaSuccess && before != device) err = cudaSetDevice(device);
+    else if (err == cudaSuccess) before = -1;
+  }
+  ~DeviceScope() { if (before >= 0) cudaSetDevice(before); }
+};
+
+int fail_cuda(const char* what, cudaError_t e) {
+  fprintf(stderr, "%s: %s\n", what, cudaGetErrorString(e));
+  return TSDP_ERR_CUDA;
+}
+
+int device_sms(int device) {
+  static std::atomic<int> known[MAX_DEVICES];
+  int n = known[device].load(std::memory_order_relaxed);
+  if (n == 0) {
+    if (cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, device) != cudaSuccess || n < 1) n = 148;
+    known[device].store(n, std::memory_order_relaxed);
+  }
+  return n;
+}
+
+// Dynamic shared memory beyond 48 KB is asked for once per kernel and device.
+template <typename F> cudaError_t allow_smem(F kern, int bytes, int device, std::atomic<unsigned long long>& done) {
+  const unsigned long long bit = 1ull << device;
+  if (done.load(std::memory_order_relaxed) & bit) return cudaSuccess;
+  const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+  if (e == cudaSuccess) done.fetch_or(bit, std::memory_order_relaxed);
+  return e;
+}
+
+bool aligned16(const void* p) { return ((uintptr_t)p & 15) == 0; }
+size_t esize(int dtype) { return dtype == TSDP_TYPE_BF16 ? 2 : 4; }
+bool dtype_ok(int dtype) { return dtype == TSDP_TYPE_FP32 || dtype == TSDP_TYPE_BF16; }
+
+// 16 bytes at a time: every row starts on a 16-byte boundary and holds whole 16-byte pieces.
+bool rows_wide(const Rows& r, int dtype, int C) {
+  const int v = 16 / (int)esize(dtype);
+  return aligned16(r.p) && r.sn % v == 0 && r.sl % v == 0 && C % v == 0;
+}
+// A dimension of one element has no stride of its own.
+Rows rows_of(const void* p, long long sn, long long sl, int N, int L, int C) {
+  return Rows{const_cast<void*>(p), N > 1 ? sn : 0, L > 1 ? sl : (C + 7) / 8 * 8};
+}
+bool strides_ok(long long sn, long long sl) { return sn >= 0 && sl >= 0; }
+// Rows that are written must not overlap.
+bool rows_apart(long long N, long long L, int C, long long sn, long long sl) {
+  if (L > 1 && sl < C) return false;
+  if (N > 1 && sn < C) return false;
+  if (N > 1 && L > 1) return sn >= (L - 1) * sl + C || sl >= (N - 1) * sn + C;
+  return true;
+}
+bool copy_ok(const tsdp_saved_t* s) { return s != nullptr && s->q != nullptr && s->scale != nullptr; }
+Copy8 copy_of(const tsdp_saved_t* s) { return s ? Copy8{reinterpret_cast<signed char*>(s->q), s->scale} : Copy8{nullptr, nullptr}; }
+
+template <typename T>
+cudaError_t pack(const Rows& x, Copy8 out, int N, int L, int C, int sms, cudaStream_t s) {
+  const long long rows = (long long)N * L;
+  const bool wide = rows_wide(x, sizeof(T) == 2 ? TSDP_TYPE_BF16 : TSDP_TYPE_FP32, C) && C % 8 == 0 && ((uintptr_t)out.q & 7) == 0;
+  if (wide) {
+    const int lanes = COPY_THREADS / min(4 * copy_blocks(C), COPY_THREADS);
+    const long long blocks = min((rows + lanes - 1) / lanes, (long long)sms * 32);
+    checkpoint_pack_kernel<T><<<(unsigned)blocks, COPY_THREADS, 0, s>>>(x, out, N, L, C);
+  } else {
+    const long long blocks = min((rows * copy_blocks(C) + 7) / 8, (long long)sms * 64);
+    checkpoint_pack_any_kernel<T><<<(unsigned)blocks, COPY_THREADS, 0, s>>>(x, out, N, L, C);
+  }
+  return cudaGetLastError();
+}
+
+template <typename T>
+cudaError_t unpack(Copy8 in, const Rows& x, int N, int L, int C, int sms, cudaStream_t s) {
+  const long long rows = (long long)N * L;
+  const bool wide = rows_wide(x, sizeof(T) == 2 ? TSDP_TYPE_BF16 : TSDP_TYPE_FP32, C) && C % 8 == 0 && ((uintptr_t)in.q & 7) == 0;
+  if (wide) {
+    const int lanes = COPY_THREADS / min(C / 8, COPY_THREADS);
+    const long long blocks = min((rows + lanes - 1) / lanes, (long long)sms * 32);
+    checkpoint_unpack_kernel<T><<<(unsigned)blocks, COPY_THREADS, 0, s>>>(in, x, N, L, C);
+  } else {
+    const long long blocks = min((rows * copy_blocks(C) + 7) / 8, (long long)sms * 64);
+    checkpoint_unpack_any_kernel<T><<<(unsigned)blocks, COPY_THREADS, 0, s>>>(in, x, N, L, C);
+  }
+  return cudaGetLastError();
+}
+
+// ---------------------------------------------------------------------------------------------------------- GroupNorm
+bool norm_ok(const tsdp_norm_t* n) {
+  return n && dtype_ok(n->dtype) && n->N >= 0 && n->L >= 1 && n->C >= 1 && n->groups >= 1 && n->C % n->groups == 0 &&
+         n->C / n->groups <= GN_MAX_WIDTH && n->act >= TSDP_ACT_NONE && n->act <= TSDP_ACT_GELU && n->eps > 0.f && n->eps < 1e30f;
+}
+
+int gcd(int a, int b) { while (b) { const int t = a % b; a = b; b = t; } return a; }
+
+// The smallest set whose channels are a multiple of `unit` fits a CTA.
+bool set_fits(int C, int groups, int unit) { const int cg = C / groups; return (long long)min(unit / gcd(cg, unit), groups) * cg <= GN_MAX_WIDTH; }
+
+// Which groups a CTA takes, how its threads lie over them, how many CTAs share the positions.
+// unit: channels that a set has to be a multiple of (16-byte pieces, 32 for 8-bit copies).
+void norm_plan(NormArgs& g, int V, int unit, int elem, int sms, bool grad) {
+  const int cg = g.C / g.groups;
+  g.per_set = unit / gcd(cg, unit);
+  if (g.per_set > g.groups) g.per_set = g.groups;
+  const int step = g.per_set;
+  // rows of 128 bytes at least, where that leaves enough sets for the SMs and a row does not outgrow the threads
+  while (g.per_set + step <= g.groups && (g.per_set + step) * cg <= GN_THREADS * V && g.per_set * cg * elem < 128) g.per_set += step;
+  g.width = g.per_set * cg;
+  g.sets = (g.groups + g.per_set - 1) / g.per_set;
+  g.cols = min((g.width + V - 1) / V, GN_THREADS);
+  if (unit == 32 && g.cols < GN_THREADS) {                          // whole blocks of 32 channels side by side in a warp
+    const int per = 32 / V;
+    g.cols = (g.cols + per - 1) / per * per;
+  }
+  g.lanes = GN_THREADS / g.cols;
+  g.ranks = 1;
+  while (g.ranks < 8 && (long long)g.N * g.sets * g.ranks < 2 * sms && g.L >= 8ll * g.lanes * g.ranks) g.ranks *= 2;
+  const long long fill = (long long)sms * (grad ? 4 : 8) / ((long long)g.sets * g.ranks);
+  g.splits = (int)min((long long)g.N, max(1ll, grad ? fill : (1ll << 24) / ((long long)g.sets * g.ranks)));
+}
+
+template <typename F>
+cudaError_t launch(F kern, const NormArgs& g, int smem, cudaStream_t s) {
+  cudaLaunchConfig_t cfg{};
+  cudaLaunchAttribute at[1];
+  cfg.gridDim = dim3((unsigned)((long long)g.splits * g.sets * g.ranks));
+  cfg.blockDim = dim3(GN_THREADS);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = s;
+  at[0].id = cudaLaunchAttributeClusterDimension;
+  at[0].val.clusterDim.x = g.ranks; at[0].val.clusterDim.y = 1; at[0].val.clusterDim.z = 1;
+  cfg.attrs = at;
+  cfg.numAttrs = g.ranks > 1 ? 1 : 0;
+  return cudaLaunchKernelEx(&cfg, kern, g);
+}
+
+template <typename T, int V>
+cudaError_t norm_forward(NormArgs& g, int sms, int device, cudaStream_t s) {
+  const int unit = V > 1 && (g.cx.q || g.cy.q) ? 32 : V;
+  norm_plan(g, V, unit, sizeof(T), sms, false);
+  static std::atomic<unsigned long long> done{0};
+  const int smem = (2 * GN_THREADS * V + 4 * g.per_set) * 4;
+  const cudaError_t e = allow_smem(group_norm_kernel<T, V>, (2 * GN_THREADS * V + 4 * GN_MAX_WIDTH) * 4, device, done);
+  return e != cudaSuccess ? e : launch(group_norm_kernel<T, V>, g, smem, s);
+}
+
+template <typename T, int V, bool COPY>
+cudaError_t norm_backward(NormArgs& g, int sms, int device, cudaStream_t s) {
+  static std::atomic<unsigned long long> done{0};
+  const int smem = (4 * GN_THREADS * V + 8 * g.width + 2 * g.per_set) * 4;
+  const cudaError_t e = allow_smem(group_norm_grad_kernel<T, V, COPY>, (4 * GN_THREADS * V + 10 * GN_MAX_WIDTH) * 4, device, done);
+  return e != cudaSuccess ? e : launch(group_norm_grad_kernel<T, V, COPY>, g, smem, s);
+}
+
+size_t norm_grad_bytes(const NormArgs& g) { return (size_t)g.splits * 2 * g.C * 4; }
+
+// ------------------------------------------------------------------------------------------------------ weight gradient
+typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
+                                  const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+EncodeTiledFn encode_fn() {
+  static std::atomic<void*> known{nullptr};
+  void* fn = known.load(std::memory_order_relaxed);
+  if (!fn) {
+    cudaDriverEntryPointQueryResult q;
+    if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &fn, cudaEnableDefault, &q) != cudaSuccess || q != cudaDriverEntryPointSuccess) return nullptr;
+    known.store(fn, std::memory_order_relaxed);
+  }
+  return reinterpret_cast<EncodeTiledFn>(fn);
+}
+
+constexpr int BIAS_SHARES = 64;
+struct WgradPlan { int bn, ctas; size_t share_bytes, bytes; };
+
+WgradPlan wgrad_plan(WgradArgs& g, bool fp32, int sms) {
+  WgradPlan p;
+  p.bn = g.O <= 64 ? 64 : (g.O <= 128 || fp32 ? 128 : 256);
+  g.tiles_k = (g.K + WG_BM - 1) / WG_BM;
+  g.tiles_o = (g.O + p.bn - 1) / p.bn;
+  g.stages = (g.M + WG_BK - 1) / WG_BK;
+  g.line = g.stages * g.taps * g.tiles_k * g.tiles_o;
+  p.ctas = (int)min((long long)sms, max(1ll, g.line / 2));
+  p.share_bytes = (size_t)2 * p.ctas * WG_BM * p.bn * 4;
+  p.bytes = p.share_bytes + (size_t)BIAS_SHARES * g.O * 4;
+  return p;
+}
+
+template <int BN, int DYK>
+cudaError_t wgrad_launch(const CUtensorMap& map, const WgradArgs& g, int ctas, int device, cudaStream_t s) {
+  static std::atomic<unsigned long long> done{0};
+  const cudaError_t e = allow_smem(weight_grad_kernel<BN, DYK>, wg_smem_bytes(BN, DYK), device, done);
+  if (e != cudaSuccess) return e;
+  weight_grad_kernel<BN, DYK><<<ctas, WG_THREADS, wg_smem_bytes(BN, DYK), s>>>(map, g);
+  weight_grad_join_kernel<BN><<<(unsigned)(4ll * g.taps * g.tiles_k * g.tiles_o), 256, 0, s>>>(g, ctas);
+  return cudaGetLastError();
+}
+
+bool wgrad_ok(int dtype, long long N, int L, int K, int O, int taps) {
+  return dtype_ok(dtype) && N >= 0 && L >= 1 && K >= 1 && O >= 1 && K <= (1 << 20) && O <= (1 << 20) && taps >= 1 && taps <= TSDP_MAX_TAPS &&
+         (taps & 1) == 1 && N * L < (1ll << 31) - 64 && (long long)taps * K * O < (1ll << 40);
+}
+
+}  // namespace
+
+extern "C" {
+
+int tsdp_checkpoint_pack(int device, int dtype, const void* d_x, int64_t x_n, int64_t x_l, int N, int L, int C, const tsdp_saved_t* out, void* stream) {
+  if (device < 0 || device >= MAX_DEVICES || !dtype_ok(dtype) || N < 0 || L < 0 || C < 1 || !strides_ok(x_n, x_l)) return TSDP_ERR_ARG;
+  if (N == 0 || L == 0) return TSDP_OK;
+  if (!d_x || !copy_ok(out)) return TSDP_ERR_ARG;
+  DeviceScope scope(device);
+  if (scope.err != cudaSuccess) return fail_cuda("tsdp_checkpoint_pack", scope.err);
+  const Rows x = rows_of(d_x, x_n, x_l, N, L, C);
+  const int sms = device_sms(device);
+  cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
+  const cudaError_t e = dtype == TSDP_TYPE_BF16 ? pack<__nv_bfloat16>(x, copy_of(out), N, L, C, sms, s) : pack<float>(x, copy_of(out), N, L, C, sms, s);
+  return e == cudaSuccess ? TSDP_OK : fail_cuda("tsdp_checkpoint_pack", e);
+}
+
+int tsdp_checkpoint_unpack(int device, int dtype, const tsdp_saved_t* in, void* d_x, int64_t x_n, int64_t x_l, int N, int L, int C, void* stream) {
+  if (device < 0 || device >= MAX_DEVICES || !dtype_ok(dtype) || N < 0 || L < 0 || C < 1 || !strides_ok(x_n, x_l)) return TSDP_ERR_ARG;
+  if (N == 0 || L == 0) return TSDP_OK;
+  if (!d_x || !copy_ok(in) || !rows_apart(N, L, C, x_n, x_l)) return TSDP_ERR_ARG;
+  DeviceScope scope(device);
+  if (scope.err != cudaSuccess) return fail_cuda("tsdp_checkpoint_unpack", scope.err);
+  const Rows x = rows_of(d_x, x_n, x_l, N, L, C);
+  const int sms = device_sms(device);
+  cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
+  const cudaError_t e = dtype == TSDP_TYPE_BF16 ? unpack<__nv_bfloat16>(copy_of(in), x, N, L, C, sms, s) : unpack<float>(copy_of(in), x, N, L, C, sms, s);
+  return e == cudaSuccess ? TSDP_OK : fail_cuda("tsdp_checkpoint_unpack", e);
+}
+
+int tsdp_group_norm(int device, const tsdp_norm_t* shape, const void* d_x, int64_t x_n, int64_t x_l, const float* d_gamma, const float* d_beta,
+                    const float* d_film, void* d_y, int64_t y_n, int64_t y_l, float* d_mean, float* d_rstd, const tsdp_saved_t* saved_x,
+                    const tsdp_saved_t* saved_y, void* stream) {
+  if (device < 0 || device >= MAX_DEVICES || !norm_ok(shape) || !strides_ok(x_n, x_l) || !strides_ok(y_n, y_l)) return TSDP_ERR_ARG;
+  if ((saved_x && !copy_ok(saved_x)) || (saved_y && !copy_ok(saved_y))) return TSDP_ERR_ARG;
+  if (shape->N == 0) return TSDP_OK;
+  if (!d_x || !d_gamma || !d_beta || !d_y || !rows_apart(shape->N, shape->L, shape->C, y_n, y_l)) return TSDP_ERR_ARG;
+  DeviceScope scope(device);
+  if (scope.err != cudaSuccess) return fail_cuda("tsdp_group_norm", scope.err);
+  const int sms = device_sms(device), dtype = shape->dtype, N = shape->N, L = shape->L, C = shape->C;
+  cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
+  NormArgs g{};
+  g.N = N; g.L = L; g.C = C; g.groups = shape->groups; g.act = shape->act; g.eps = shape->eps;
+  g.x = rows_of(d_x, x_n, x_l, N, L, C);
+  g.y = rows_of(d_y, y_n, y_l, N, L, C);
+  g.gamma = d_gamma; g.beta = d_beta; g.film = d_film; g.mean = d_mean; g.rstd = d_rstd;
+  const Copy8 cx = copy_of(saved_x), cy = copy_of(saved_y);
+  const bool wide = rows_wide(g.x, dtype, C) && rows_wide(g.y, dtype, C) && set_fits(C, g.groups, 16 / (int)esize(dtype));
+  // copies are written on the way where rows come in 16-byte pieces, by a pass of their own elsewhere
+  const bool fused = wide && ((uintptr_t)cx.q & 7) == 0 && ((uintptr_t)cy.q & 7) == 0 && set_fits(C, g.groups, 32);
+  cudaError_t e = cudaSuccess;
+  if (fused) { g.cx = cx; g.cy = cy; }
+  else if (cx.q) e = dtype == TSDP_TYPE_BF16 ? pack<__nv_bfloat16>(g.x, cx, N, L, C, sms, s) : pack<float>(g.x, cx, N, L, C, sms, s);
+  if (e == cudaSuccess) {
+    if (dtype == TSDP_TYPE_BF16) e = wide ? norm_forward<__nv_bfloat16, 8>(g, sms, device, s) : norm_forward<__nv_bfloat16, 1>(g, sms, device, s);
+    else e = wide ? norm_forward<float, 4>(g, sms, device, s) : norm_forward<float, 1>(g, sms, device, s);
+  }
+  if (e == cudaSuccess && !fused && cy.q)
+    e = dtype == TSDP_TYPE_BF16 ? pack<__nv_bfloat16>(g.y, cy, N, L, C, sms, s) : pack<float>(g.y, cy, N, L, C, sms, s);
+  return e == cudaSuccess ? TSDP_OK : fail_cuda("tsdp_group_norm", e);
+}
+
+// (the widest plan: 16-byte pieces or not, the number of splits may differ)
+size_t tsdp_group_norm_grad_workspace(int device, const tsdp_norm_t* shape) {
+  if (device < 0 || device >= MAX_DEVICES || !norm_ok(shape)) return 0;
+  size_t most = 16;
+  for (int V : {1, 16 / (int)esize(shape->dtype)}) {
+    if (!set_fits(shape->C, shape->groups, V)) continue;
+    NormArgs g{};
+    g.N = shape->N < 1 ? 1 : shape->N; g.L = shape->L; g.C = shape->C; g.groups = shape->groups;
+    norm_plan(g, V, V, (int)esize(shape->dtype), device_sms(device), true);
+    if (norm_grad_bytes(g) > most) most = norm_grad_bytes(g);
+  }
+  return most;
+}
+
+int tsdp_group_norm_grad(int device, const tsdp_norm_t* shape, const void* d_dy, int64_t dy_n, int64_t dy_l, const void* d_x, int64_t x_n, int64_t x_l,
+                         const tsdp_saved_t* saved_x, const float* d_gamma, const float* d_beta, const float* d_film, const float* d_mean,
+                         const float* d_rstd, void* d_dx, int64_t dx_n, int64_t dx_l, float* d_dgamma, float* d_dbeta, float* d_dfilm,
+                         void* d_workspace, size_t workspace_bytes, void* stream) {
+  if (device < 0 || device >= MAX_DEVICES || !norm_ok(shape) || !strides_ok(dy_n, dy_l) || !strides_ok(x_n, x_l) || !strides_ok(dx_n, dx_l) ||
+      !d_dgamma || !d_dbeta || (d_dfilm && !d_film))
+    return TSDP_ERR_ARG;
+  DeviceScope scope(device);
+  if (scope.err != cudaSuccess) return fail_cuda("tsdp_group_norm_grad", scope.err);
+  const int sms = device_sms(device), dtype = shape->dtype, C = shape->C;
+  cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
+  cudaError_t e;
+  if (shape->N == 0) {
+    e = cudaMemsetAsync(d_dgamma, 0, (size_t)C * 4, s);
+    if (e == cudaSuccess) e = cudaMemsetAsync(d_dbeta, 0, (size_t)C * 4, s);
+    return e == cudaSuccess ? TSDP_OK : fail_cuda("tsdp_group_norm_grad", e);
+  }
+  if (!d_dy || (saved_x ? !copy_ok(saved_x) : !d_x) || !d_gamma || !d_beta || !d_mean || !d_rstd || !d_dx || !d_workspace || ((uintptr_t)d_workspace & 3) ||
+      !rows_apart(shape->N, shape->L, C, dx_n, dx_l))
+    return TSDP_ERR_ARG;
+  NormArgs g{};
+  g.N = shape->N; g.L = shape->L; g.C = C; g.groups = shape->groups; g.act = shape->act; g.eps = shape->eps;
+  g.x = rows_of(d_x, x_n, x_l, g.N, g.L, C);
+  g.dy = rows_of(d_dy, dy_n, dy_l, g.N, g.L, C);
+  g.dx = rows_of(d_dx, dx_n, dx_l, g.N, g.L, C);
+  g.gamma = d_gamma; g.beta = d_beta; g.film = d_film; g.mean = const_cast<float*>(d_mean); g.rstd = const_cast<float*>(d_rstd);
+  g.dfilm = d_dfilm;
+  g.cx = copy_of(saved_x);
+  g.part = reinterpret_cast<float*>(d_workspace);
+  const bool copy = saved_x != nullptr;
+  const bool wide = set_fits(C, g.groups, 16 / (int)esize(dtype)) && rows_wide(g.dy, dtype, C) && rows_wide(g.dx, dtype, C) && (copy ? ((uintptr_t)g.cx.q & 7) == 0 : rows_wide(g.x, dtype, C));
+  const int V = wide ? 16 / (int)esize(dtype) : 1;
+  norm_plan(g, V, V, (int)esize(dtype), sms, true);
+  if (workspace_bytes < norm_grad_bytes(g)) return TSDP_ERR_ARG;
+  if (dtype == TSDP_TYPE_BF16) {
+    if (wide) e = copy ? norm_backward<__nv_bfloat16, 8, true>(g, sms, device, s) : norm_backward<__nv_bfloat16, 8, false>(g, sms, device, s);
+    else e = copy ? norm_backward<__nv_bfloat16, 1, true>(g, sms, device, s) : norm_backward<__nv_bfloat16, 1, false>(g, sms, device, s);
+  } else {
+    if (wide) e = copy ? norm_backward<float, 4, true>(g, sms, device, s) : norm_backward<float, 4, false>(g, sms, device, s);
+    else e = copy ? norm_backward<float, 1, true>(g, sms, device, s) : norm_backward<float, 1, false>(g, sms, device, s);
+  }
+  if (e == cudaSuccess) {
+    group_norm_join_kernel<<<dim3((C + GN_JOIN_CH - 1) / GN_JOIN_CH, 2), GN_JOIN_CH * GN_JOIN_LANES, 0, s>>>(g.part, g.splits, C, d_dgamma, d_dbeta);
+    e = cudaGetLastError();
+  }
+  return e == cudaSuccess ? TSDP_OK : fail_cuda("tsdp_group_norm_grad", e);
+}
+
+size_t tsdp_weight_grad_workspace(int device, int dtype, int N, int L, int K, int O, int taps) {
+  if (device < 0 || device >= MAX_DEVICES || !wgrad_ok(dtype, N, L, K, O, taps)) return 0;
+  WgradArgs g{};
+  g.M = (long long)(N < 1 ? 1 : N) * L; g.K = K; g.O = O; g.taps = taps;
+  return wgrad_plan(g, dtype == TSDP_TYPE_FP32, device_sms(device)).bytes;
+}
+
+int tsdp_weight_grad(int device, int dtype, const tsdp_saved_t* saved_x, const void* d_dy, int64_t dy_l, int N, int L, int K, int O, int taps, float* d_dW,
+                     float* d_db, void* d_workspace, size_t workspace_bytes, void* stream) {
+  if (device < 0 || device >= MAX_DEVICES || !wgrad_ok(dtype, N, L, K, O, taps) || !d_dW || dy_l < 0) return TSDP_ERR_ARG;
+  DeviceScope scope(device);
+  if (scope.err != cudaSuccess) return fail_cuda("tsdp_weight_grad", scope.err);
+  cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
+  cudaError_t e;
+  if (N == 0) {
+    e = cudaMemsetAsync(d_dW, 0, (size_t)taps * K * O * 4, s);
+    if (e == cudaSuccess && d_db) e = cudaMemsetAsync(d_db, 0, (size_t)O * 4, s);
+    return e == cudaSuccess ? TSDP_OK : fail_cuda("tsdp_weight_grad", e);
+  }
+  if (!copy_ok(saved_x) || !d_dy || !d_workspace || !aligned16(d_workspace)) return TSDP_ERR_ARG;
+  WgradArgs g{};
+  g.x = copy_of(saved_x);
+  g.dy = d_dy; g.ldy = dy_l;
+  g.M = (long long)N * L; g.L = L; g.K = K; g.O = O; g.taps = taps;
+  g.dW = d_dW;
+  const bool fp32 = dtype == TSDP_TYPE_FP32;
+  const WgradPlan p = wgrad_plan(g, fp32, device_sms(device));
+  if (workspace_bytes < p.bytes || 4ll * g.taps * g.tiles_k * g.tiles_o >= (1ll << 31)) return TSDP_ERR_ARG;
+  g.share = reinterpret_cast<float*>(d_workspace);
+  CUtensorMap map{};
+  const bool tma = !fp32 && aligned16(d_dy) && dy_l % 8 == 0 && dy_l >= O && dy_l < (1ll << 38);
+  if (tma) {
+    EncodeTiledFn encode = encode_fn();
+    if (!encode) { fprintf(stderr, "tsdp_weight_grad: cuTensorMapEncodeTiled unavailable\n"); return TSDP_ERR_CUDA; }
+    cuuint64_t gdim[2] = {(cuuint64_t)O, (cuuint64_t)g.M};
+    cuuint64_t gstr[1] = {(cuuint64_t)dy_l * 2};
+    cuuint32_t box[2] = {64, WG_BK}, estr[2] = {1, 1};
+    const CUresult r = encode(&map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(d_dy), gdim, gstr, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                              CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    if (r != CUDA_SUCCESS) { fprintf(stderr, "tsdp_weight_grad: cuTensorMapEncodeTiled failed with code %d\n", (int)r); return TSDP_ERR_CUDA; }
+  }
+  if (fp32) e = p.bn == 64 ? wgrad_launch<64, WG_DY_FP32>(map, g, p.ctas, device, s) : wgrad_launch<128, WG_DY_FP32>(map, g, p.ctas, device, s);
+  else if (p.bn == 64) e = tma ? wgrad_launch<64, WG_DY_TMA>(map, g, p.ctas, device, s) : wgrad_launch<64, WG_DY_BF16>(map, g, p.ctas, device, s);
+  else if (p.bn == 128) e = tma ? wgrad_launch<128, WG_DY_TMA>(map, g, p.ctas, device, s) : wgrad_launch<128, WG_DY_BF16>(map, g, p.ctas, device, s);
+  else e = tma ? wgrad_launch<256, WG_DY_TMA>(map, g, p.ctas, device, s) : wgrad_launch<256, WG_DY_BF16>(map, g, p.ctas, device, s);
+  if (e == cudaSuccess && d_db) {
+    float* part = reinterpret_cast<float*>(reinterpret_cast<char*>(d_workspace) + p.share_bytes);
+    const dim3 grid((O + 31) / 32, BIAS_SHARES);
+    if (fp32) bias_grad_kernel<float><<<grid, 256, 0, s>>>(reinterpret_cast<const float*>(d_dy), dy_l, g.M, O, part);
+    else bias_grad_kernel<__nv_bfloat16><<<grid, 256, 0, s>>>(reinterpret_cast<const __nv_bfloat16*>(d_dy), dy_l, g.M, O, part);
+    bias_grad_join_kernel<<<(O + 255) / 256, 256, 0, s>>>(part, BIAS_SHARES, O, d_db);
+    e = cudaGetLastError();
+  }
+  return e == cudaSuccess ? TSDP_OK : fail_cuda("tsdp_weight_grad", e);
+}
+
+}  // extern "C"

@@ -1,0 +1,367 @@
+// Weight gradient of a projection or a "same" convolution whose input was kept in eight bits, on the 5th-generation tensor cores:
+//
+//   dW[tap][i][o] = sum over sequences n and positions l of  x^[n, l + tap - taps/2, i] dy[n, l, o]        (x^ zero outside a sequence)
+//
+// x^ = q 2^(b - 127) is exact in bf16, so that its products with a bf16 dy are those of the values themselves; sums are fp32.  An fp32
+// dy is cut into three bf16 parts that add up to it exactly (8 + 8 + 8 bits of its 24), multiplied one after the other into
+// the same accumulator.
+//
+// A tile of dW is 128 input channels x BN output channels of one tap; the reduction runs over rows (n, l), 64 to a stage.  Both
+// operands come row by row, that is with the reduction index slowest: the tensor core reads them "MN-major" from rows of 128 bytes
+// in the 128-byte swizzle.
+//   warps 2..9   x^: a thread fetches 32 channels of one row (q and one byte b, a stage ahead), turns them into bf16 and stores them into
+//                the swizzled tile; the tap's shift and the zeros outside a sequence are made here.  dy goes the same way where TMA cannot
+//                take it (fp32, unaligned rows).
+//   warp 0       dy by TMA otherwise
+//   warp 1       one thread issues tcgen05.mma into one of two accumulators in tensor memory
+//   warps 10..13 epilogue: the accumulator to dW, or to this CTA's share of it
+// Work is the line of all (tile, stage) pairs, cut into equal pieces, one per CTA, so that no CTA is idle whatever the sizes; a tile that
+// more than one CTA worked on is added up from their shares in the order of the line: the same bits on every run.
+// Every wait is bounded; a CTA whose wait runs out leaves NaN in what it had to write.
+#pragma once
+#include "checkpoint_kernels.cuh"
+#include "gemm_tcgen05.cuh"
+
+namespace tsdp {
+
+constexpr int WG_BM = 128, WG_BK = 64, WG_THREADS = 448, WG_LOADERS = 256, WG_STAGE_A = WG_BK * WG_BM * 2;
+enum { WG_DY_TMA = 0, WG_DY_BF16 = 1, WG_DY_FP32 = 2 };
+__host__ __device__ constexpr int wg_parts(int dyk) { return dyk == WG_DY_FP32 ? 3 : 1; }
+__host__ __device__ constexpr int wg_stage_bytes(int BN, int dyk) { return WG_STAGE_A + wg_parts(dyk) * WG_BK * BN * 2; }
+__host__ __device__ constexpr int wg_stages(int BN, int dyk) {
+  return 200 * 1024 / wg_stage_bytes(BN, dyk) < 6 ? 200 * 1024 / wg_stage_bytes(BN, dyk) : 6;
+}
+__host__ __device__ constexpr int wg_smem_bytes(int BN, int dyk) { return wg_stages(BN, dyk) * wg_stage_bytes(BN, dyk) + 256 + 1024; }
+
+struct WgradArgs {
+  Copy8 x;                                  // [M, K]
+  const void* dy; long long ldy;            // [M, O]
+  long long M;                              // rows = sequences x L
+  int L, K, O, taps;
+  int tiles_k, tiles_o;                     // tile = (tap, kt, ot), ot fastest
+  long long stages, line;                   // of a tile; of all tiles
+  float* dW;                                // [taps, K, O]
+  float* share;                             // [2 grid][128][BN]: what a CTA has of its first / of its last tile
+};
+// The line's piece of CTA i of n.
+__host__ __device__ inline long long wg_begin(long long line, int i, int n) { return line / n * i + min((long long)i, line % n); }
+
+// Descriptor of an operand tile whose reduction index is the slow one: rows (one reduction index) of 64 elements, 128 bytes apart, groups of
+// eight rows 1024 bytes apart (stride byte offset); further columns of 64 elements start `lead` bytes on (leading byte offset).
+__device__ __forceinline__ uint64_t umma_desc_mn_sw128(uint32_t smem_addr, uint32_t lead) {
+  uint64_t d = 0;
+  d |= (uint64_t)((smem_addr >> 4) & 0x3FFF);
+  d |= (uint64_t)(lead >> 4) << 16;
+  d |= (uint64_t)(1024 >> 4) << 32;
+  d |= (uint64_t)1 << 46;                 // version
+  d |= (uint64_t)2 << 61;                 // SWIZZLE_128B
+  return d;
+}
+
+// Two bf16 values of a word pair's bytes j, j + 1: the magnitude's seven bits on 128 (bf16 counts by ones there), 128 or 256 taken off by
+// the sign bit; both exact, and so is the product with a power of two.
+__device__ __forceinline__ uint32_t wg_pair(uint32_t word, uint32_t sel, __nv_bfloat162 step) {
+  const uint32_t p = __byte_perm(word, 0u, sel);
+  const uint32_t hi = (p & 0x007f007fu) | 0x43004300u, lo = (p & 0x00800080u) | 0xc300c300u;
+  const __nv_bfloat162 v = __hmul2(__hadd2(*reinterpret_cast<const __nv_bfloat162*>(&hi), *reinterpret_cast<const __nv_bfloat162*>(&lo)), step);
+  return *reinterpret_cast<const uint32_t*>(&v);
+}
+__device__ __forceinline__ void st_shared16(uint32_t addr, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+  asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
+}
+
+template <int BN, int DYK>
+__global__ void __launch_bounds__(WG_THREADS, 1)
+weight_grad_kernel(const __grid_constant__ CUtensorMap tmDy, WgradArgs g) {
+  constexpr int STAGES = wg_stages(BN, DYK), STAGE_BYTES = wg_stage_bytes(BN, DYK), PARTS = wg_parts(DYK);
+  constexpr uint32_t TMEM_COLS = 2 * BN < 32 ? 32 : 2 * BN;
+  constexpr uint32_t IDESC = umma_idesc_bf16(BN, WG_BM) | (1u << 15) | (1u << 16);      // both operands MN-major
+  extern __shared__ uint8_t wg_raw[];
+  const uint32_t base = (ptx::smem_u32(wg_raw) + 1023u) & ~1023u;
+  const uint32_t bar0 = base + STAGES * STAGE_BYTES;
+  auto full = [&](int s) { return bar0 + 8u * s; };
+  auto empty = [&](int s) { return bar0 + 8u * (STAGES + s); };
+  auto tfull = [&](int b) { return bar0 + 8u * (2 * STAGES + b); };
+  auto tempty = [&](int b) { return bar0 + 8u * (2 * STAGES + 2 + b); };
+  const uint32_t slot = bar0 + 8u * (2 * STAGES + 4);
+  const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < STAGES; ++s) { ptx::mbar_init(full(s), WG_LOADERS / 32 + (DYK == WG_DY_TMA ? 1 : 0)); ptx::mbar_init(empty(s), 1); }
+    for (int b = 0; b < 2; ++b) { ptx::mbar_init(tfull(b), 1); ptx::mbar_init(tempty(b), 4); }
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+  }
+  if (warp == 1) { ptx::tmem_alloc(slot, TMEM_COLS); ptx::tmem_relinquish(); }
+  ptx::tc_fence_before();
+  __syncthreads();
+  ptx::tc_fence_after();
+  const uint32_t tmem = *reinterpret_cast<volatile uint32_t*>(wg_raw + (slot - ptx::smem_u32(wg_raw)));
+
+  const long long begin = wg_begin(g.line, blockIdx.x, gridDim.x), end = wg_begin(g.line, blockIdx.x + 1, gridDim.x);
+  const long long t_first = begin / g.stages;
+  bool ok = true;
+
+  if (warp == 0) {
+    if (DYK == WG_DY_TMA && ptx::elect_one()) {
+      long long t = t_first;
+      int st = (int)(begin - t * g.stages), s = 0;
+      uint32_t ph = 1;
+      for (long long i = begin; i < end; ++i) {
+        if (!ptx::mbar_wait_thread(empty(s), ph)) { ok = false; break; }
+        const uint32_t b0 = base + s * STAGE_BYTES + WG_STAGE_A;
+        const int o0 = (int)(t % g.tiles_o) * BN;
+        ptx::mbar_expect_tx(full(s), BN * WG_BK * 2);
+#pragma unroll
+        for (int j = 0; j < BN / 64; ++j) ptx::tma_load_2d(b0 + j * WG_BK * 128, &tmDy, o0 + 64 * j, st * WG_BK, full(s));
+        if (++s == STAGES) { s = 0; ph ^= 1; }
+        if (++st == g.stages) { st = 0; ++t; }
+      }
+    }
+  } else if (warp == 1) {
+    if (ptx::elect_one()) {
+      long long t = t_first;
+      int st = (int)(begin - t * g.stages), s = 0, buf = 0;
+      uint32_t ph = 0, tph = 1;
+      bool fresh = true;
+      for (long long i = begin; i < end; ++i) {
+        if (fresh && !ptx::mbar_wait_thread(tempty(buf), tph)) { ok = false; break; }
+        if (!ptx::mbar_wait_thread(full(s), ph)) { ok = false; break; }
+        ptx::tc_fence_after();
+        const uint32_t a0 = base + s * STAGE_BYTES, d = tmem + buf * BN;
+#pragma unroll
+        for (int p = 0; p < PARTS; ++p)
+#pragma unroll
+          for (int k = 0; k < WG_BK / 16; ++k)      // 16 rows = 2048 bytes of every column of 64 channels
+            ptx::tc_mma_bf16(d, umma_desc_mn_sw128(a0 + k * 2048, WG_BK * 128),
+                             umma_desc_mn_sw128(a0 + WG_STAGE_A + p * (WG_BK * BN * 2) + k * 2048, WG_BK * 128), IDESC,
+                             fresh && p == 0 && k == 0 ? 0u : 1u);
+        fresh = false;
+        ptx::tc_commit(empty(s));
+        if (++s == STAGES) { s = 0; ph ^= 1; }
+        if (++st == g.stages || i + 1 == end) {
+          ptx::tc_commit(tfull(buf));
+          st = 0; ++t; fresh = true;
+          if (++buf == 2) { buf = 0; tph ^= 1; }
+        }
+      }
+    }
+  } else if (warp < 10) {
+    // x^ (and dy where it does not come by TMA): row of the stage, block of 32 channels
+    const int tid = threadIdx.x - 64, r = tid >> 2, bq = tid & 3, nb = copy_blocks(g.K);
+    const bool wide = (g.K & 15) == 0 && ((uintptr_t)g.x.q & 15) == 0;
+    struct Fetch { uint32_t w[8]; uint32_t b; } f;
+    long long t = t_first;
+    int st = (int)(begin - t * g.stages);
+    int l = (int)(((long long)st * WG_BK + r) % g.L);                    // position of the row in its sequence
+    const int l_step = WG_BK % g.L;
+    auto fetch = [&](Fetch& o) {
+      const int kt = (int)((t / g.tiles_o) % g.tiles_k), tap = (int)(t / g.tiles_o / g.tiles_k);
+      const int shift = tap - g.taps / 2, ls = l + shift;
+      const long long m = (long long)st * WG_BK + r, ms = m + shift;
+      const int c = kt * WG_BM + bq * 32;
+      const bool in = m < g.M && ls >= 0 && ls < g.L && c < g.K;
+      o.b = in ? (uint32_t)g.x.b[ms * nb + (c >> 5)] : 0u;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) o.w[j] = 0u;
+      if (in) {
+        const signed char* q = g.x.q + ms * g.K + c;
+        if (wide) {
+          const uint4 u = *reinterpret_cast<const uint4*>(q);
+          o.w[0] = u.x; o.w[1] = u.y; o.w[2] = u.z; o.w[3] = u.w;
+          if (c + 16 < g.K) {
+            const uint4 v = *reinterpret_cast<const uint4*>(q + 16);
+            o.w[4] = v.x; o.w[5] = v.y; o.w[6] = v.z; o.w[7] = v.w;
+          }
+        } else {
+#pragma unroll
+          for (int j = 0; j < 32; ++j)
+            if (c + j < g.K) o.w[j >> 2] |= (uint32_t)(unsigned char)q[j] << (8 * (j & 3));
+        }
+      }
+    };
+    auto step = [&] {
+      l += l_step;
+      if (l >= g.L) l -= g.L;
+      if (++st == g.stages) { st = 0; ++t; l = r % g.L; }
+    };
+    // rows of 128 bytes per 64 channels; the two halves of a row take their 16-byte pieces in another order, so that the eight threads of
+    // a store phase (two rows, four blocks) touch eight different pieces
+    const uint32_t half = (uint32_t)(bq >> 1), row_off = half * (WG_BK * 128) + (uint32_t)r * 128;
+    const uint32_t ch0 = (uint32_t)(bq & 1) * 4, rx = (uint32_t)(r & 7);
+    int s = 0;
+    uint32_t ph = 1;
+    if (begin < end) fetch(f);
+    for (long long i = begin; i < end && ok; ++i) {
+      Fetch cur = f;
+      const long long m_cur = (long long)st * WG_BK + r;
+      const int o0 = (int)(t % g.tiles_o) * BN;
+      step();
+      if (i + 1 < end) fetch(f);
+      ok = ptx::mbar_wait_warp(empty(s), ph);
+      if (!ok) break;
+      const uint32_t a0 = base + s * STAGE_BYTES;
+      const uint32_t sb = cur.b == 255u ? 0x7fc0u : cur.b << 7, sb2 = sb | sb << 16;
+      const __nv_bfloat162 stp = *reinterpret_cast<const __nv_bfloat162*>(&sb2);
+#pragma unroll
+      for (int jj = 0; jj < 4; ++jj) {
+        const uint32_t j = (uint32_t)jj ^ (2 * half);
+        // (a select between two words: an index known at run time would move the array to local memory)
+        const uint32_t w0 = half ? cur.w[2 * (jj ^ 2)] : cur.w[2 * jj], w1 = half ? cur.w[2 * (jj ^ 2) + 1] : cur.w[2 * jj + 1];
+        st_shared16(a0 + row_off + (((ch0 + j) ^ rx) << 4), wg_pair(w0, 0x4140, stp), wg_pair(w0, 0x4342, stp), wg_pair(w1, 0x4140, stp),
+                    wg_pair(w1, 0x4342, stp));
+      }
+      if constexpr (DYK != WG_DY_TMA) {
+        // eight output channels at a time
+        const bool row_in = m_cur < g.M;
+        const uint32_t b0 = a0 + WG_STAGE_A;
+        for (int u = bq; u < BN / 8; u += 4) {
+          const int o = o0 + 8 * u;
+          uint32_t part[3][4];
+          if constexpr (DYK == WG_DY_BF16) {
+            const unsigned short* p = reinterpret_cast<const unsigned short*>(g.dy) + m_cur * g.ldy + o;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              const uint32_t x0 = row_in && o + 2 * j < g.O ? p[2 * j] : 0u, x1 = row_in && o + 2 * j + 1 < g.O ? p[2 * j + 1] : 0u;
+              part[0][j] = x0 | x1 << 16;
+            }
+          } else {
+            const float* p = reinterpret_cast<const float*>(g.dy) + m_cur * g.ldy + o;
+            uint32_t e[3][8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+              const float v = row_in && o + j < g.O ? p[j] : 0.f;
+              const uint32_t bits = __float_as_uint(v), h0 = bits & 0xffff0000u;
+              const float r1 = v - __uint_as_float(h0);
+              const uint32_t h1 = __float_as_uint(r1) & 0xffff0000u;
+              const float r2 = r1 - __uint_as_float(h1);
+              const bool odd = (bits & 0x7f800000u) == 0x7f800000u;      // an infinity or a NaN is its own first part
+              e[0][j] = odd ? ((bits & 0x7fffffu) ? 0x7fc00000u : h0) : h0;
+              e[1][j] = odd ? 0u : h1;
+              e[2][j] = odd ? 0u : __float_as_uint(r2);
+            }
+#pragma unroll
+            for (int k = 0; k < 3; ++k)
+#pragma unroll
+              for (int j = 0; j < 4; ++j) part[k][j] = __byte_perm(e[k][2 * j], e[k][2 * j + 1], 0x7632);
+          }
+#pragma unroll
+          for (int k = 0; k < PARTS; ++k)
+            st_shared16(b0 + k * (WG_BK * BN * 2) + (u >> 3) * (WG_BK * 128) + r * 128 + ((((uint32_t)u & 7) ^ rx) << 4), part[k][0], part[k][1],
+                        part[k][2], part[k][3]);
+        }
+      }
+      ptx::fence_async_smem();
+      __syncwarp();
+      if (lane == 0) ptx::mbar_arrive(full(s));
+      if (++s == STAGES) { s = 0; ph ^= 1; }
+    }
+  } else {
+    const int quad = warp & 3, row = quad * 32 + lane;                   // tensor-memory lane quadrant of this warp; input channel of the tile
+    long long i = begin, t = t_first;
+    int buf = 0;
+    uint32_t ph = 0;
+    while (i < end) {
+      const long long t_end = min((t + 1) * g.stages, end);
+      const bool whole = i == t * g.stages && t_end == (t + 1) * g.stages;
+      const bool good = ok && ptx::mbar_wait_warp(tfull(buf), ph);
+      ptx::tc_fence_after();
+      const int o0 = (int)(t % g.tiles_o) * BN, kt = (int)((t / g.tiles_o) % g.tiles_k), tap = (int)(t / g.tiles_o / g.tiles_k);
+      const int k = kt * WG_BM + row;
+      float* out = whole ? g.dW + ((long long)tap * g.K + k) * g.O + o0 : g.share + ((2ll * blockIdx.x + (t == t_first ? 0 : 1)) * WG_BM + row) * BN;
+      const int cols = whole ? min(BN, g.O - o0) : BN;
+      const bool vec = !whole || ((g.O & 3) == 0 && ((uintptr_t)g.dW & 15) == 0);
+      for (int c0 = 0; c0 < BN; c0 += 32) {
+        uint32_t v[32];
+        if (good) {
+          ptx::tmem_ld32(tmem + buf * BN + ((uint32_t)(quad * 32) << 16) + c0, v);
+          ptx::tmem_ld_wait();
+        } else {
+#pragma unroll
+          for (int j = 0; j < 32; ++j) v[j] = 0x7fc00000u;
+        }
+        if (whole && k >= g.K) continue;
+        if (vec) {
+#pragma unroll
+          for (int j = 0; j < 8; ++j)
+            if (c0 + 4 * j < cols) *reinterpret_cast<uint4*>(out + c0 + 4 * j) = make_uint4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
+        } else {
+#pragma unroll
+          for (int j = 0; j < 32; ++j)
+            if (c0 + j < cols) out[c0 + j] = __uint_as_float(v[j]);
+        }
+      }
+      if (!good) ok = false;
+      ptx::tc_fence_before();
+      __syncwarp();
+      if (lane == 0) ptx::mbar_arrive(tempty(buf));
+      if (++buf == 2) { buf = 0; ph ^= 1; }
+      i = t_end; ++t;
+    }
+  }
+  if (!ok) {
+    const long long t0 = clock64();
+    while (clock64() - t0 < 400000ll) { }      // copies that are still in flight land before the memory is given back
+  }
+  ptx::tc_fence_before();
+  __syncthreads();
+  ptx::tc_fence_after();
+  if (warp == 1) ptx::tmem_dealloc(tmem, TMEM_COLS);
+}
+
+// Tiles that several CTAs worked on: their shares, in the order of the line.  One block per tile and 32 of its rows.
+template <int BN>
+__global__ void __launch_bounds__(256)
+weight_grad_join_kernel(WgradArgs g, int ctas) {
+  const long long t = blockIdx.x >> 2;
+  const long long a = t * g.stages, b = a + g.stages;
+  // the CTA that holds stage a: pieces differ by one in length, so the quotient is off by one at most
+  int i = (int)min((long long)ctas - 1, a / (g.line / ctas + 1));
+  while (i + 1 < ctas && wg_begin(g.line, i + 1, ctas) <= a) ++i;
+  if (wg_begin(g.line, i + 1, ctas) >= b) return;                        // one CTA had all of it
+  const int o0 = (int)(t % g.tiles_o) * BN, kt = (int)((t / g.tiles_o) % g.tiles_k), tap = (int)(t / g.tiles_o / g.tiles_k);
+  const int row0 = (blockIdx.x & 3) * 32;
+  for (int e = threadIdx.x * 4; e < 32 * BN; e += 256 * 4) {
+    const int row = row0 + e / BN, c = e % BN, k = kt * WG_BM + row;
+    if (k >= g.K || o0 + c >= g.O) continue;
+    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int j = i; j < ctas && wg_begin(g.line, j, ctas) < b; ++j) {
+      const int which = wg_begin(g.line, j, ctas) / g.stages == t ? 0 : 1;
+      const float4 u = *reinterpret_cast<const float4*>(g.share + ((2ll * j + which) * WG_BM + row) * BN + c);
+      v.x += u.x; v.y += u.y; v.z += u.z; v.w += u.w;
+    }
+    float* out = g.dW + ((long long)tap * g.K + k) * g.O + o0 + c;
+    if ((g.O & 3) == 0 && ((uintptr_t)g.dW & 15) == 0) *reinterpret_cast<float4*>(out) = v;
+    else {
+      const float w[4] = {v.x, v.y, v.z, v.w};
+      for (int j = 0; j < 4; ++j) if (o0 + c + j < g.O) out[j] = w[j];
+    }
+  }
+}
+
+// db[o] = sum of dy over the rows: a block takes 32 columns and a share of the rows, the shares are joined by group_norm_join's scheme.
+template <typename T>
+__global__ void __launch_bounds__(256)
+bias_grad_kernel(const T* dy, long long ldy, long long M, int O, float* part) {
+  __shared__ float s[8][32];
+  const int o = blockIdx.x * 32 + (threadIdx.x & 31), lane = threadIdx.x >> 5;
+  const long long share = (M + gridDim.y - 1) / gridDim.y, lo = blockIdx.y * share, hi = min(M, lo + share);
+  float v = 0.f;
+  if (o < O)
+    for (long long m = lo + lane; m < hi; m += 8) v += to_f(dy[m * ldy + o]);
+  s[lane][threadIdx.x & 31] = v;
+  __syncthreads();
+  if (lane == 0 && o < O) {
+    for (int i = 1; i < 8; ++i) v += s[i][threadIdx.x];
+    part[(long long)blockIdx.y * O + o] = v;
+  }
+}
+__global__ void __launch_bounds__(256)
+bias_grad_join_kernel(const float* part, int shares, int O, float* db) {
+  const int o = blockIdx.x * 256 + threadIdx.x;
+  if (o >= O) return;
+  float v = 0.f;
+  for (int i = 0; i < shares; ++i) v += part[(long long)i * O + o];
+  db[o] = v;
+}
+
+}  // namespace tsdp

@@ -21,40 +21,57 @@ namespace tsdp {
 
 enum { ACT_NONE = 0, ACT_MISH = 1, ACT_SILU = 2, ACT_GELU = 3 };
 
-// a = act(z) and its derivative.  One exponential and one division each, on the fast instructions: e^v by ex2.approx is off by 2 units
-// of 2^-24 and by the rounding of v log2(e), 2e-6 of e^v at the ends of the range where it matters (|z| <= 20).
-// Mish: with u = e^z, d = (u + 1)^2 + 1:  tanh(log(1 + u)) = u (u + 2) / d,  derivative t + 4 z u (u + 1) / d^2.  Past z = 20 both are
-// those of the identity to 2^-24, and u is held there so that it stays finite.
-// GELU (tanh form): 1/2 (1 + tanh w) = 1 / (1 + e^-2w).
-struct ActValue { float a, d; };
-__device__ __forceinline__ float act_recip(float v) { return __fdividef(1.f, v); }
-template <bool GRAD> __device__ __forceinline__ ActValue act_mish(float z) {
-  const float zc = z > 20.f ? 20.f : z;                    // (a NaN stays one)
-  const float u = __expf(zc), w = u + 1.f, r = act_recip(fmaf(w, w, 1.f));
-  const float t = u * (u + 2.f) * r;
-  return {z * t, GRAD ? fmaf(4.f * zc * r, r * u * w, t) : 0.f};
-}
-template <bool GRAD> __device__ __forceinline__ ActValue act_silu(float z) {
-  const float s = act_recip(1.f + __expf(-z)), a = z * s;
-  return {a, GRAD ? fmaf(a, 1.f - s, s) : 0.f};
-}
-template <bool GRAD> __device__ __forceinline__ ActValue act_gelu(float z) {
-  const float k = 0.7978845608028654f, q = fminf(z * z, 1e4f);      // (past |z| = 100 the logistic function is 0 or 1)
-  const float s = act_recip(1.f + __expf(-2.f * k * z * fmaf(0.044715f, q, 1.f))), a = z * s;
-  return {a, GRAD ? fmaf(a * (1.f - s), 2.f * k * fmaf(0.134145f, q, 1.f), s) : 0.f};
+// a = act(z) and its derivative, two values at a time on the packed fp32 pipe.  One exponential and one reciprocal each, by the hardware
+// instructions: e^v is off by 2 units of 2^-24 and by the rounding of v log2(e), 2e-6 of e^v at the ends of the range where it matters
+// (|z| <= 20).
+// Mish: with u = e^z, r = 1 / ((u + 1)^2 + 1):  tanh(log(1 + u)) = t = u (u + 2) r,  derivative t + 4 z r (u (u + 1) r).  Past z = 20 both are
+// those of the identity to 2^-24, and u is held there so that it stays finite (min.NaN: a NaN stays one).
+// GELU (tanh form): 1/2 (1 + tanh w) = 1 / (1 + e^-2w); past |z| = 100 that is 0 or 1 and the polynomial is held.
+__device__ __forceinline__ float act_ex2(float v) { float r; asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v)); return r; }
+__device__ __forceinline__ float act_rcp(float v) { float r; asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v)); return r; }
+__device__ __forceinline__ float act_min(float a, float b) { float r; asm("min.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b)); return r; }
+__device__ __forceinline__ float2 two(float v) { return make_float2(v, v); }
+__device__ __forceinline__ float2 exp2_of(float2 v, float k) { v = __fmul2_rn(v, two(k)); return make_float2(act_ex2(v.x), act_ex2(v.y)); }
+__device__ __forceinline__ float2 rcp_of(float2 v) { return make_float2(act_rcp(v.x), act_rcp(v.y)); }
+constexpr float ACT_LOG2E = 1.4426950408889634f;
+template <bool GRAD> __device__ __forceinline__ void act_pair(int act, float2 z, float2& a, float2& d) {
+  if (act == ACT_MISH) {
+    const float2 zc = make_float2(act_min(z.x, 20.f), act_min(z.y, 20.f)), u = exp2_of(zc, ACT_LOG2E), w = __fadd2_rn(u, two(1.f));
+    const float2 r = rcp_of(__ffma2_rn(w, w, two(1.f)));
+    const float2 t = __fmul2_rn(__ffma2_rn(u, u, __fadd2_rn(u, u)), r);
+    a = __fmul2_rn(z, t);
+    if (GRAD) d = __ffma2_rn(__fmul2_rn(__fmul2_rn(zc, two(4.f)), r), __fmul2_rn(__fmul2_rn(u, w), r), t);
+  } else if (act == ACT_SILU) {
+    const float2 s = rcp_of(__fadd2_rn(exp2_of(z, -ACT_LOG2E), two(1.f)));
+    a = __fmul2_rn(z, s);
+    if (GRAD) d = __ffma2_rn(a, __ffma2_rn(s, two(-1.f), two(1.f)), s);
+  } else if (act == ACT_GELU) {
+    float2 q = __fmul2_rn(z, z);
+    q = make_float2(act_min(q.x, 1e4f), act_min(q.y, 1e4f));
+    const float k = 0.7978845608028654f;
+    const float2 s = rcp_of(__fadd2_rn(exp2_of(__fmul2_rn(z, __ffma2_rn(q, two(0.044715f), two(1.f))), -2.f * k * ACT_LOG2E), two(1.f)));
+    a = __fmul2_rn(z, s);
+    if (GRAD) d = __ffma2_rn(__fmul2_rn(a, __ffma2_rn(s, two(-1.f), two(1.f))), __ffma2_rn(q, two(2.f * k * 0.134145f), two(2.f * k)), s);
+  } else {
+    a = z;
+    if (GRAD) d = two(1.f);
+  }
 }
 template <bool GRAD, int V> __device__ __forceinline__ void act_values(int act, const float* z, float* a, float* d) {
-#define TSDP_ACT_LOOP(EXPR)                                  \
-  _Pragma("unroll") for (int i = 0; i < V; ++i) {            \
-    const ActValue r = EXPR;                                 \
-    a[i] = r.a;                                              \
-    if (GRAD) d[i] = r.d;                                    \
+  if constexpr (V == 1) {
+    float2 av, dv;
+    act_pair<GRAD>(act, two(z[0]), av, dv);
+    a[0] = av.x;
+    if (GRAD) d[0] = dv.x;
+  } else {
+#pragma unroll
+    for (int i = 0; i < V; i += 2) {
+      float2 av, dv;
+      act_pair<GRAD>(act, make_float2(z[i], z[i + 1]), av, dv);
+      a[i] = av.x; a[i + 1] = av.y;
+      if (GRAD) { d[i] = dv.x; d[i + 1] = dv.y; }
+    }
   }
-  if (act == ACT_MISH) { TSDP_ACT_LOOP(act_mish<GRAD>(z[i])) }
-  else if (act == ACT_SILU) { TSDP_ACT_LOOP(act_silu<GRAD>(z[i])) }
-  else if (act == ACT_GELU) { TSDP_ACT_LOOP(act_gelu<GRAD>(z[i])) }
-  else { TSDP_ACT_LOOP((ActValue{z[i], 1.f})) }
-#undef TSDP_ACT_LOOP
 }
 
 struct NormArgs {
@@ -67,6 +84,8 @@ struct NormArgs {
   float *dfilm, *part;                         // [N, 2C] or null; [splits, 2, C]
   // the plan: a set is `per_set` groups, `width` channels; cols threads on a position; `ranks` CTAs of a cluster share the positions
   int per_set, sets, width, cols, lanes, ranks, splits;
+  // slab kernels: threads of a group that a shuffle adds up; rows of partial sums left (of warps or lanes); bytes of a stage
+  int fold, red_rows, stage_bytes;
 };
 
 constexpr int GN_THREADS = 256;

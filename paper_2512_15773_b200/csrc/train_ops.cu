@@ -9,6 +9,7 @@
 #include "../../include/tsdp.h"
 #include "checkpoint_kernels.cuh"
 #include "group_norm_kernels.cuh"
+#include "group_norm_slab.cuh"
 #include "weight_grad_tcgen05.cuh"
 
 using namespace tsdp;
@@ -141,6 +142,46 @@ void norm_plan(NormArgs& g, int V, int unit, int elem, int sms, bool grad) {
   g.splits = (int)min((long long)g.N, max(1ll, grad ? fill : (1ll << 24) / ((long long)g.sets * g.ranks)));
 }
 
+// The slab kernels' plan: false where a group of one sequence is more than the threads of a CTA hold in registers (SLAB_ITEMS pieces each).
+// A set grows while it fits two pieces a thread and leaves four CTAs' worth of work for each place on the chip.
+constexpr int SLAB_ITEMS = 4, SLAB_SMEM = 112 * 1024;
+int slab_items(const NormArgs& g, int V, int unit, int per_set, int& cols) {
+  cols = (per_set * (g.C / g.groups) + V - 1) / V;
+  if (unit == 32) cols = (cols + 32 / V - 1) / (32 / V) * (32 / V);
+  return cols > GN_THREADS ? GN_THREADS : (g.L + GN_THREADS / cols - 1) / (GN_THREADS / cols);
+}
+bool slab_plan(NormArgs& g, int V, int unit, int elem, int sms, bool grad, bool copy, int& items, int& smem) {
+  const int cg = g.C / g.groups, places = sms * GN_SLAB_CTAS;
+  if (cg % V != 0 || (copy && g.C % 16 != 0)) return false;
+  if (copy && unit < 16) unit = 16;
+  int per_set = min(unit / gcd(cg, unit), g.groups), cols, c2;
+  items = slab_items(g, V, unit, per_set, cols);
+  if (items > SLAB_ITEMS) return false;
+  while (per_set * 2 <= g.groups && (long long)g.N * ((g.groups + 2 * per_set - 1) / (2 * per_set)) >= 4ll * places) {
+    const int more = slab_items(g, V, unit, 2 * per_set, c2);
+    if (more > max(2, items)) break;
+    per_set *= 2; items = more; cols = c2;
+  }
+  g.per_set = per_set;
+  g.width = per_set * cg;
+  g.sets = (g.groups + per_set - 1) / per_set;
+  g.cols = cols;
+  g.lanes = GN_THREADS / cols;
+  g.ranks = 1;
+  const int gcols = cg / V;
+  g.fold = 1;
+  while (g.fold < 32 && gcols % (2 * g.fold) == 0 && cols % (2 * g.fold) == 0) g.fold *= 2;
+  g.red_rows = cols < 32 && (cols & (cols - 1)) == 0 ? GN_THREADS / 32 : g.lanes;
+  const int slab = g.L * g.width;
+  g.stage_bytes = grad ? slab * (elem + (copy ? 1 : elem)) + 4 * g.width : slab * elem + 8 * g.width;
+  smem = GN_RING * g.stage_bytes;
+  if (grad) smem = max(smem + (g.dfilm ? 4 * g.lanes * g.width * 4 : 0), 2 * g.lanes * g.width * 4);
+  if (smem > SLAB_SMEM) return false;
+  const long long at_once = max(1, places / g.sets), turns = (g.N + at_once - 1) / at_once;
+  g.splits = (int)((g.N + turns - 1) / turns);
+  return true;
+}
+
 template <typename F>
 cudaError_t launch(F kern, const NormArgs& g, int smem, cudaStream_t s) {
   cudaLaunchConfig_t cfg{};
@@ -156,9 +197,30 @@ cudaError_t launch(F kern, const NormArgs& g, int smem, cudaStream_t s) {
   return cudaLaunchKernelEx(&cfg, kern, g);
 }
 
+template <typename T, int ITEMS>
+cudaError_t norm_slab(const NormArgs& g, int smem, int device, cudaStream_t s) {
+  static std::atomic<unsigned long long> done{0};
+  const cudaError_t e = allow_smem(group_norm_slab_kernel<T, ITEMS>, SLAB_SMEM, device, done);
+  return e != cudaSuccess ? e : launch(group_norm_slab_kernel<T, ITEMS>, g, smem, s);
+}
+template <typename T, int ITEMS, bool COPY>
+cudaError_t norm_slab_grad(const NormArgs& g, int smem, int device, cudaStream_t s) {
+  static std::atomic<unsigned long long> done{0};
+  const cudaError_t e = allow_smem(group_norm_slab_grad_kernel<T, ITEMS, COPY>, SLAB_SMEM, device, done);
+  return e != cudaSuccess ? e : launch(group_norm_slab_grad_kernel<T, ITEMS, COPY>, g, smem, s);
+}
+
+// The vectors that slab kernels read in pairs or by bulk copies.
+bool vectors_wide(const NormArgs& g) { return ((uintptr_t)g.gamma & 7) == 0 && ((uintptr_t)g.beta & 7) == 0 && (!g.film || aligned16(g.film)); }
+
 template <typename T, int V>
 cudaError_t norm_forward(NormArgs& g, int sms, int device, cudaStream_t s) {
-  const int unit = V > 1 && (g.cx.q || g.cy.q) ? 32 : V;
+  const int unit = V > 1 && set_fits(g.C, g.groups, 32) ? 32 : V;      // (with or without copies: the same plan, the same bits)
+  int items, bytes;
+  if constexpr (V > 1) {
+    if (vectors_wide(g) && slab_plan(g, V, unit, sizeof(T), sms, false, false, items, bytes))
+      return items <= 1 ? norm_slab<T, 1>(g, bytes, device, s) : (items <= 2 ? norm_slab<T, 2>(g, bytes, device, s) : norm_slab<T, 4>(g, bytes, device, s));
+  }
   norm_plan(g, V, unit, sizeof(T), sms, false);
   static std::atomic<unsigned long long> done{0};
   const int smem = (2 * GN_THREADS * V + 4 * g.per_set) * 4;
@@ -167,7 +229,12 @@ cudaError_t norm_forward(NormArgs& g, int sms, int device, cudaStream_t s) {
 }
 
 template <typename T, int V, bool COPY>
-cudaError_t norm_backward(NormArgs& g, int sms, int device, cudaStream_t s) {
+cudaError_t norm_backward(NormArgs& g, bool slab, int items, int bytes, int device, cudaStream_t s) {
+  if constexpr (V > 1) {
+    if (slab)
+      return items <= 1 ? norm_slab_grad<T, 1, COPY>(g, bytes, device, s)
+                        : (items <= 2 ? norm_slab_grad<T, 2, COPY>(g, bytes, device, s) : norm_slab_grad<T, 4, COPY>(g, bytes, device, s));
+  }
   static std::atomic<unsigned long long> done{0};
   const int smem = (4 * GN_THREADS * V + 8 * g.width + 2 * g.per_set) * 4;
   const cudaError_t e = allow_smem(group_norm_grad_kernel<T, V, COPY>, (4 * GN_THREADS * V + 10 * GN_MAX_WIDTH) * 4, device, done);
@@ -283,15 +350,21 @@ int tsdp_group_norm(int device, const tsdp_norm_t* shape, const void* d_x, int64
   return e == cudaSuccess ? TSDP_OK : fail_cuda("tsdp_group_norm", e);
 }
 
-// (the widest plan: 16-byte pieces or not, the number of splits may differ)
+// (the plan depends on the alignment of what a call is given: the largest of all)
 size_t tsdp_group_norm_grad_workspace(int device, const tsdp_norm_t* shape) {
   if (device < 0 || device >= MAX_DEVICES || !norm_ok(shape)) return 0;
   size_t most = 16;
-  for (int V : {1, 16 / (int)esize(shape->dtype)}) {
+  const int elem = (int)esize(shape->dtype), sms = device_sms(device);
+  for (int form = 0; form < 6; ++form) {                 // one value at a time, 16 bytes, four forms of slabs
+    const int V = form == 0 ? 1 : 16 / elem;
     if (!set_fits(shape->C, shape->groups, V)) continue;
     NormArgs g{};
+    float some;
+    int items, bytes;
     g.N = shape->N < 1 ? 1 : shape->N; g.L = shape->L; g.C = shape->C; g.groups = shape->groups;
-    norm_plan(g, V, V, (int)esize(shape->dtype), device_sms(device), true);
+    g.dfilm = form & 1 ? &some : nullptr;
+    if (form < 2) norm_plan(g, V, V, elem, sms, true);
+    else if (!slab_plan(g, GN_GRAD_V, V, elem, sms, true, form >= 4, items, bytes)) continue;
     if (norm_grad_bytes(g) > most) most = norm_grad_bytes(g);
   }
   return most;
@@ -329,14 +402,16 @@ int tsdp_group_norm_grad(int device, const tsdp_norm_t* shape, const void* d_dy,
   const bool copy = saved_x != nullptr;
   const bool wide = set_fits(C, g.groups, 16 / (int)esize(dtype)) && rows_wide(g.dy, dtype, C) && rows_wide(g.dx, dtype, C) && (copy ? ((uintptr_t)g.cx.q & 7) == 0 : rows_wide(g.x, dtype, C));
   const int V = wide ? 16 / (int)esize(dtype) : 1;
-  norm_plan(g, V, V, (int)esize(dtype), sms, true);
+  int items = 0, bytes = 0;
+  const bool slab = wide && vectors_wide(g) && (!copy || aligned16(g.cx.q)) && slab_plan(g, GN_GRAD_V, V, (int)esize(dtype), sms, true, copy, items, bytes);
+  if (!slab) norm_plan(g, V, V, (int)esize(dtype), sms, true);
   if (workspace_bytes < norm_grad_bytes(g)) return TSDP_ERR_ARG;
   if (dtype == TSDP_TYPE_BF16) {
-    if (wide) e = copy ? norm_backward<__nv_bfloat16, 8, true>(g, sms, device, s) : norm_backward<__nv_bfloat16, 8, false>(g, sms, device, s);
-    else e = copy ? norm_backward<__nv_bfloat16, 1, true>(g, sms, device, s) : norm_backward<__nv_bfloat16, 1, false>(g, sms, device, s);
+    if (wide) e = copy ? norm_backward<__nv_bfloat16, 8, true>(g, slab, items, bytes, device, s) : norm_backward<__nv_bfloat16, 8, false>(g, slab, items, bytes, device, s);
+    else e = copy ? norm_backward<__nv_bfloat16, 1, true>(g, slab, items, bytes, device, s) : norm_backward<__nv_bfloat16, 1, false>(g, slab, items, bytes, device, s);
   } else {
-    if (wide) e = copy ? norm_backward<float, 4, true>(g, sms, device, s) : norm_backward<float, 4, false>(g, sms, device, s);
-    else e = copy ? norm_backward<float, 1, true>(g, sms, device, s) : norm_backward<float, 1, false>(g, sms, device, s);
+    if (wide) e = copy ? norm_backward<float, 4, true>(g, slab, items, bytes, device, s) : norm_backward<float, 4, false>(g, slab, items, bytes, device, s);
+    else e = copy ? norm_backward<float, 1, true>(g, slab, items, bytes, device, s) : norm_backward<float, 1, false>(g, slab, items, bytes, device, s);
   }
   if (e == cudaSuccess) {
     group_norm_join_kernel<<<dim3((C + GN_JOIN_CH - 1) / GN_JOIN_CH, 2), GN_JOIN_CH * GN_JOIN_LANES, 0, s>>>(g.part, g.splits, C, d_dgamma, d_dbeta);

@@ -30,17 +30,28 @@ __device__ __forceinline__ uint32_t copy_q(float x, float inv, uint32_t b) {
   if (b == 248u) s = fminf(fmaxf(s, -127.f), 127.f);
   return b == 255u ? 0u : __float_as_uint(s + 12582912.f) & 0xffu;
 }
-// Four of them in a word.
-__device__ __forceinline__ uint32_t copy_q4(const float* x, float inv, uint32_t b) {
-  uint32_t w[4];
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    float s = x[i] * inv;
-    if (b == 248u) s = fminf(fmaxf(s, -127.f), 127.f);
-    w[i] = __float_as_uint(s + 12582912.f);
+// Four of them in a word, two products and two sums at a time.
+__device__ __forceinline__ uint32_t copy_q4(float2 x0, float2 x1, float inv, uint32_t b) {
+  const float2 k = make_float2(inv, inv), magic = make_float2(12582912.f, 12582912.f);
+  x0 = __fmul2_rn(x0, k); x1 = __fmul2_rn(x1, k);
+  if (b >= 248u) {                             // (rare: the largest magnitudes of fp32, and what is not finite)
+    if (b == 255u) return 0u;
+    x0.x = fminf(fmaxf(x0.x, -127.f), 127.f); x0.y = fminf(fmaxf(x0.y, -127.f), 127.f);
+    x1.x = fminf(fmaxf(x1.x, -127.f), 127.f); x1.y = fminf(fmaxf(x1.y, -127.f), 127.f);
   }
-  const uint32_t r = __byte_perm(__byte_perm(w[0], w[1], 0x0040), __byte_perm(w[2], w[3], 0x0040), 0x5410);
-  return b == 255u ? 0u : r;
+  x0 = __fadd2_rn(x0, magic); x1 = __fadd2_rn(x1, magic);
+  return __byte_perm(__byte_perm(__float_as_uint(x0.x), __float_as_uint(x0.y), 0x0040), __byte_perm(__float_as_uint(x1.x), __float_as_uint(x1.y), 0x0040), 0x5410);
+}
+__device__ __forceinline__ uint32_t copy_q4(const float* x, float inv, uint32_t b) {
+  return copy_q4(make_float2(x[0], x[1]), make_float2(x[2], x[3]), inv, b);
+}
+// Largest magnitude (as bits) of eight bf16 values, of four fp32 ones.
+__device__ __forceinline__ uint32_t copy_top_bf16(uint4 u) {
+  const uint32_t m = __vmaxu2(__vmaxu2(u.x & 0x7fff7fffu, u.y & 0x7fff7fffu), __vmaxu2(u.z & 0x7fff7fffu, u.w & 0x7fff7fffu));
+  return max(m << 16, m & 0xffff0000u);
+}
+__device__ __forceinline__ uint32_t copy_top_fp32(uint4 u) {
+  return max(max(u.x & 0x7fffffffu, u.y & 0x7fffffffu), max(u.z & 0x7fffffffu, u.w & 0x7fffffffu));
 }
 __device__ __forceinline__ float copy_value(uint32_t word, int i, float step) {
   return (float)(signed char)(word >> (8 * i)) * step;

@@ -55,6 +55,36 @@ template <typename T, int V> __device__ __forceinline__ void piece_values(const 
     }
   }
 }
+// The 8-bit copy of 16 bytes of a row; the lanes of a block of 32 sit side by side in a warp.  top = 0 where there is no row.
+template <typename T> __device__ __forceinline__ void write_copy(const Copy8& o, uint4 u, bool row, long long r, int C, int c) {
+  constexpr int V = 16 / sizeof(T);
+  uint32_t top = sizeof(T) == 2 ? copy_top_bf16(u) : copy_top_fp32(u);
+  if (!row) top = 0;
+#pragma unroll
+  for (int i = 1; i < 32 / V; i *= 2) top = max(top, __shfl_xor_sync(0xffffffffu, top, i));
+  const uint32_t b = copy_byte(top);
+  const float is = copy_inv_step(b);
+  float2 w[V / 2];
+  unpack16<T, V>(u, w);
+  if (row) {
+    signed char* q = o.q + r * C + c;
+    if constexpr (V == 8) *reinterpret_cast<uint2*>(q) = make_uint2(copy_q4(w[0], w[1], is, b), copy_q4(w[2], w[3], is, b));
+    else *reinterpret_cast<uint32_t*>(q) = copy_q4(w[0], w[1], is, b);
+    if ((c & 31) == 0) o.b[r * copy_blocks(C) + (c >> 5)] = (unsigned char)b;
+  }
+}
+// f(the activation as a constant): the choice is made once, not for every value.
+template <int A> struct ActIs { static constexpr int value = A; };
+template <typename F> __device__ __forceinline__ void with_act(int act, F&& f) {
+  if (act == ACT_MISH) f(ActIs<ACT_MISH>{});
+  else if (act == ACT_SILU) f(ActIs<ACT_SILU>{});
+  else if (act == ACT_GELU) f(ActIs<ACT_GELU>{});
+  else f(ActIs<ACT_NONE>{});
+}
+template <typename T, int V> __device__ __forceinline__ uint4 pack16(const float2* y) {
+  if constexpr (sizeof(T) == 2) return make_uint4(pack_bf16(y[0].x, y[0].y), pack_bf16(y[1].x, y[1].y), pack_bf16(y[2].x, y[2].y), pack_bf16(y[3].x, y[3].y));
+  else return make_uint4(__float_as_uint(y[0].x), __float_as_uint(y[0].y), __float_as_uint(y[1].x), __float_as_uint(y[1].y));
+}
 // Sum over the threads of a group: within a warp by shuffles, the rest through s_red.  One barrier.
 template <int K>
 __device__ __forceinline__ void group_sum(const NormArgs& g, int gcols, int col, int row, float* s_red, float (&v)[K]) {
@@ -174,45 +204,27 @@ group_norm_slab_kernel(NormArgs g) {
       if (g.mean) g.mean[at] = mean;
       if (g.rstd) g.rstd[at] = rstd;
     }
+    with_act(g.act, [&](auto act) {
 #pragma unroll
-    for (int j = 0; j < ITEMS; ++j) {
-      const int l = lane + j * g.lanes;
-      const bool row = in && l < g.L;
-      float2 v[P], y[P];
-      unpack16<T, V>(raw[j], v);
+      for (int j = 0; j < ITEMS; ++j) {
+        const int l = lane + j * g.lanes;
+        const bool row = in && l < g.L;
+        float2 v[P], y[P];
+        unpack16<T, V>(raw[j], v);
 #pragma unroll
-      for (int i = 0; i < P; ++i) {
-        const float2 z = __ffma2_rn(__fmul2_rn(__fadd2_rn(v[i], two(-mean)), two(rstd)), ga[i], be[i]);
-        float2 a, d;
-        act_pair<false>(g.act, z, a, d);
-        y[i] = __ffma2_rn(a, fs[i], fb[i]);
-      }
-      uint4 out;
-      if constexpr (sizeof(T) == 2) out = make_uint4(pack_bf16(y[0].x, y[0].y), pack_bf16(y[1].x, y[1].y), pack_bf16(y[2].x, y[2].y), pack_bf16(y[3].x, y[3].y));
-      else out = make_uint4(__float_as_uint(y[0].x), __float_as_uint(y[0].y), __float_as_uint(y[1].x), __float_as_uint(y[1].y));
-      if (row) *reinterpret_cast<uint4*>(reinterpret_cast<T*>(g.y.p) + n * g.y.sn + l * g.y.sl + c) = out;
-      const long long r = (long long)n * g.L + l;
-#pragma unroll
-      for (int which = 0; which < 2; ++which) {
-        const Copy8& o = which ? g.cy : g.cx;
-        if (o.q == nullptr) continue;
-        float w[V];
-        unpack16<T, V>(which ? out : raw[j], reinterpret_cast<float2*>(w));
-        uint32_t top = 0;
-#pragma unroll
-        for (int i = 0; i < V; ++i) top = max(top, __float_as_uint(w[i]) & 0x7fffffffu);
-        if (!row) top = 0;
-#pragma unroll
-        for (int o2 = 1; o2 < 32 / V; o2 *= 2) top = max(top, __shfl_xor_sync(0xffffffffu, top, o2));
-        const uint32_t b = copy_byte(top);
-        const float is = copy_inv_step(b);
-        if (row) {
-          if constexpr (V == 8) *reinterpret_cast<uint2*>(o.q + r * g.C + c) = make_uint2(copy_q4(w, is, b), copy_q4(w + 4, is, b));
-          else *reinterpret_cast<uint32_t*>(o.q + r * g.C + c) = copy_q4(w, is, b);
-          if ((c & 31) == 0) o.b[r * copy_blocks(g.C) + (c >> 5)] = (unsigned char)b;
+        for (int i = 0; i < P; ++i) {
+          const float2 z = __ffma2_rn(__fmul2_rn(__fadd2_rn(v[i], two(-mean)), two(rstd)), ga[i], be[i]);
+          float2 a, d;
+          act_pair<false>(decltype(act)::value, z, a, d);
+          y[i] = __ffma2_rn(a, fs[i], fb[i]);
         }
+        const uint4 out = pack16<T, V>(y);
+        if (row) *reinterpret_cast<uint4*>(reinterpret_cast<T*>(g.y.p) + n * g.y.sn + l * g.y.sl + c) = out;
+        const long long r = (long long)n * g.L + l;
+        if (g.cx.q) write_copy<T>(g.cx, raw[j], row, r, g.C, c);
+        if (g.cy.q) write_copy<T>(g.cy, out, row, r, g.C, c);
       }
-    }
+    });
   }
 }
 
@@ -307,6 +319,7 @@ group_norm_slab_grad_kernel(NormArgs g) {
 #pragma unroll
       for (int i = 0; i < P; ++i) h[i] = __fmul2_rn(__fadd2_rn(h[i], two(-mean)), two(rstd));
     };
+    with_act(g.act, [&](auto act) {
 #pragma unroll
     for (int j = 0; j < ITEMS; ++j) {
       const int l = lane + j * g.lanes;
@@ -325,7 +338,7 @@ group_norm_slab_grad_kernel(NormArgs g) {
 #pragma unroll
         for (int i = 0; i < P; ++i) {
           float2 a, d;
-          act_pair<true>(g.act, __ffma2_rn(h[i], ga[i], be[i]), a, d);
+          act_pair<true>(decltype(act)::value, __ffma2_rn(h[i], ga[i], be[i]), a, d);
           if (dfilm) { s_a[i] = __ffma2_rn(dy[i], a, s_a[i]); s_y[i] = __fadd2_rn(s_y[i], dy[i]); }
           dz[j][i] = __fmul2_rn(__fmul2_rn(dy[i], fs[i]), d);
           s_z[i] = __fadd2_rn(s_z[i], dz[j][i]);
@@ -333,6 +346,7 @@ group_norm_slab_grad_kernel(NormArgs g) {
         }
       }
     }
+    });
     float m[2] = {0.f, 0.f};
 #pragma unroll
     for (int i = 0; i < P; ++i) {

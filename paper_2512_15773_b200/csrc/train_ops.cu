@@ -10,6 +10,7 @@
 #include "checkpoint_kernels.cuh"
 #include "group_norm_kernels.cuh"
 #include "group_norm_slab.cuh"
+#include "group_norm_warp.cuh"
 #include "weight_grad_tcgen05.cuh"
 
 using namespace tsdp;
@@ -182,6 +183,19 @@ bool slab_plan(NormArgs& g, int V, int unit, int elem, int sms, bool grad, bool 
   return true;
 }
 
+// One warp per group: false where a group's channels are not 32, 64, 128 or 256 or a lane would hold more than `most` pieces of V channels.
+bool warp_plan(NormArgs& g, int V, int most, int ctas, int sms, int& items) {
+  const int cg = g.C / g.groups;
+  if (cg < 32 || cg > 256 || (cg & (cg - 1)) || cg / V > 32) return false;
+  const int R = 32 / (cg / V);
+  if (g.L > most * R) return false;
+  items = (g.L + R - 1) / R;
+  const long long places = max(1ll, (long long)sms * ctas * (GN_WARP_THREADS / 32) / g.groups), turns = (g.N + places - 1) / places;
+  g.splits = (int)((g.N + turns - 1) / turns);
+  g.sets = g.ranks = 1;
+  return true;
+}
+
 template <typename F>
 cudaError_t launch(F kern, const NormArgs& g, int smem, cudaStream_t s) {
   cudaLaunchConfig_t cfg{};
@@ -210,6 +224,36 @@ cudaError_t norm_slab_grad(const NormArgs& g, int smem, int device, cudaStream_t
   return e != cudaSuccess ? e : launch(group_norm_slab_grad_kernel<T, ITEMS, COPY>, g, smem, s);
 }
 
+template <typename F>
+cudaError_t launch_warps(F kern, const NormArgs& g, int smem, cudaStream_t s) {
+  const long long warps = (long long)g.splits * g.groups;
+  kern<<<(unsigned)((warps + GN_WARP_THREADS / 32 - 1) / (GN_WARP_THREADS / 32)), GN_WARP_THREADS, smem, s>>>(g);
+  return cudaGetLastError();
+}
+template <typename T>
+cudaError_t norm_warp(const NormArgs& g, int items, cudaStream_t s) {
+  if (items <= 1) return launch_warps(group_norm_warp_kernel<T, 1>, g, 0, s);
+  if (items <= 2) return launch_warps(group_norm_warp_kernel<T, 2>, g, 0, s);
+  if constexpr (sizeof(T) == 4)
+    if (items > 4) return launch_warps(group_norm_warp_kernel<T, 8>, g, 0, s);
+  return launch_warps(group_norm_warp_kernel<T, 4>, g, 0, s);
+}
+template <typename T, int ITEMS, bool COPY>
+cudaError_t norm_warp_grad_items(const NormArgs& g, int device, cudaStream_t s) {
+  static std::atomic<unsigned long long> done{0};
+  constexpr int smem = gn_warp_grad_smem<T, COPY>(ITEMS);
+  const cudaError_t e = allow_smem(group_norm_warp_grad_kernel<T, ITEMS, COPY>, smem, device, done);
+  return e != cudaSuccess ? e : launch_warps(group_norm_warp_grad_kernel<T, ITEMS, COPY>, g, smem, s);
+}
+template <typename T, bool COPY>
+cudaError_t norm_warp_grad(const NormArgs& g, int items, int device, cudaStream_t s) {
+  if (items <= 1) return norm_warp_grad_items<T, 1, COPY>(g, device, s);
+  if (items <= 2) return norm_warp_grad_items<T, 2, COPY>(g, device, s);
+  if constexpr (sizeof(T) == 2)
+    if (items > 4) return norm_warp_grad_items<T, 8, COPY>(g, device, s);
+  return norm_warp_grad_items<T, 4, COPY>(g, device, s);
+}
+
 // The vectors that slab kernels read in pairs or by bulk copies.
 bool vectors_wide(const NormArgs& g) { return ((uintptr_t)g.gamma & 7) == 0 && ((uintptr_t)g.beta & 7) == 0 && (!g.film || aligned16(g.film)); }
 
@@ -218,6 +262,7 @@ cudaError_t norm_forward(NormArgs& g, int sms, int device, cudaStream_t s) {
   const int unit = V > 1 && set_fits(g.C, g.groups, 32) ? 32 : V;      // (with or without copies: the same plan, the same bits)
   int items, bytes;
   if constexpr (V > 1) {
+    if (vectors_wide(g) && warp_plan(g, V, 32 / V, 2, sms, items)) return norm_warp<T>(g, items, s);
     if (vectors_wide(g) && slab_plan(g, V, unit, sizeof(T), sms, false, false, items, bytes))
       return items <= 1 ? norm_slab<T, 1>(g, bytes, device, s) : (items <= 2 ? norm_slab<T, 2>(g, bytes, device, s) : norm_slab<T, 4>(g, bytes, device, s));
   }
@@ -228,10 +273,12 @@ cudaError_t norm_forward(NormArgs& g, int sms, int device, cudaStream_t s) {
   return e != cudaSuccess ? e : launch(group_norm_kernel<T, V>, g, smem, s);
 }
 
+enum { GRAD_STREAM = 0, GRAD_WARPS = 1, GRAD_SLABS = 2 };
 template <typename T, int V, bool COPY>
-cudaError_t norm_backward(NormArgs& g, bool slab, int items, int bytes, int device, cudaStream_t s) {
+cudaError_t norm_backward(NormArgs& g, int form, int items, int bytes, int device, cudaStream_t s) {
   if constexpr (V > 1) {
-    if (slab)
+    if (form == GRAD_WARPS) return norm_warp_grad<T, COPY>(g, items, device, s);
+    if (form == GRAD_SLABS)
       return items <= 1 ? norm_slab_grad<T, 1, COPY>(g, bytes, device, s)
                         : (items <= 2 ? norm_slab_grad<T, 2, COPY>(g, bytes, device, s) : norm_slab_grad<T, 4, COPY>(g, bytes, device, s));
   }
@@ -355,7 +402,7 @@ size_t tsdp_group_norm_grad_workspace(int device, const tsdp_norm_t* shape) {
   if (device < 0 || device >= MAX_DEVICES || !norm_ok(shape)) return 0;
   size_t most = 16;
   const int elem = (int)esize(shape->dtype), sms = device_sms(device);
-  for (int form = 0; form < 6; ++form) {                 // one value at a time, 16 bytes, four forms of slabs
+  for (int form = 0; form < 7; ++form) {                 // one value at a time, 16 bytes, four forms of slabs, warps
     const int V = form == 0 ? 1 : 16 / elem;
     if (!set_fits(shape->C, shape->groups, V)) continue;
     NormArgs g{};
@@ -364,7 +411,7 @@ size_t tsdp_group_norm_grad_workspace(int device, const tsdp_norm_t* shape) {
     g.N = shape->N < 1 ? 1 : shape->N; g.L = shape->L; g.C = shape->C; g.groups = shape->groups;
     g.dfilm = form & 1 ? &some : nullptr;
     if (form < 2) norm_plan(g, V, V, elem, sms, true);
-    else if (!slab_plan(g, GN_GRAD_V, V, elem, sms, true, form >= 4, items, bytes)) continue;
+    else if (form == 6 ? !warp_plan(g, GN_GRAD_V, elem == 2 ? 8 : 4, 2, sms, items) : !slab_plan(g, GN_GRAD_V, V, elem, sms, true, form >= 4, items, bytes)) continue;
     if (norm_grad_bytes(g) > most) most = norm_grad_bytes(g);
   }
   return most;
@@ -403,15 +450,19 @@ int tsdp_group_norm_grad(int device, const tsdp_norm_t* shape, const void* d_dy,
   const bool wide = set_fits(C, g.groups, 16 / (int)esize(dtype)) && rows_wide(g.dy, dtype, C) && rows_wide(g.dx, dtype, C) && (copy ? ((uintptr_t)g.cx.q & 7) == 0 : rows_wide(g.x, dtype, C));
   const int V = wide ? 16 / (int)esize(dtype) : 1;
   int items = 0, bytes = 0;
-  const bool slab = wide && vectors_wide(g) && (!copy || aligned16(g.cx.q)) && slab_plan(g, GN_GRAD_V, V, (int)esize(dtype), sms, true, copy, items, bytes);
-  if (!slab) norm_plan(g, V, V, (int)esize(dtype), sms, true);
+  int form = GRAD_STREAM;
+  if (wide && vectors_wide(g) && ((uintptr_t)d_dfilm & 7) == 0 && ((uintptr_t)d_workspace & 7) == 0) {
+    if ((!copy || aligned16(g.cx.q)) && warp_plan(g, GN_GRAD_V, dtype == TSDP_TYPE_BF16 ? 8 : 4, 2, sms, items)) form = GRAD_WARPS;
+    else if ((!copy || aligned16(g.cx.q)) && slab_plan(g, GN_GRAD_V, V, (int)esize(dtype), sms, true, copy, items, bytes)) form = GRAD_SLABS;
+  }
+  if (form == GRAD_STREAM) norm_plan(g, V, V, (int)esize(dtype), sms, true);
   if (workspace_bytes < norm_grad_bytes(g)) return TSDP_ERR_ARG;
   if (dtype == TSDP_TYPE_BF16) {
-    if (wide) e = copy ? norm_backward<__nv_bfloat16, 8, true>(g, slab, items, bytes, device, s) : norm_backward<__nv_bfloat16, 8, false>(g, slab, items, bytes, device, s);
-    else e = copy ? norm_backward<__nv_bfloat16, 1, true>(g, slab, items, bytes, device, s) : norm_backward<__nv_bfloat16, 1, false>(g, slab, items, bytes, device, s);
+    if (wide) e = copy ? norm_backward<__nv_bfloat16, 8, true>(g, form, items, bytes, device, s) : norm_backward<__nv_bfloat16, 8, false>(g, form, items, bytes, device, s);
+    else e = copy ? norm_backward<__nv_bfloat16, 1, true>(g, form, items, bytes, device, s) : norm_backward<__nv_bfloat16, 1, false>(g, form, items, bytes, device, s);
   } else {
-    if (wide) e = copy ? norm_backward<float, 4, true>(g, slab, items, bytes, device, s) : norm_backward<float, 4, false>(g, slab, items, bytes, device, s);
-    else e = copy ? norm_backward<float, 1, true>(g, slab, items, bytes, device, s) : norm_backward<float, 1, false>(g, slab, items, bytes, device, s);
+    if (wide) e = copy ? norm_backward<float, 4, true>(g, form, items, bytes, device, s) : norm_backward<float, 4, false>(g, form, items, bytes, device, s);
+    else e = copy ? norm_backward<float, 1, true>(g, form, items, bytes, device, s) : norm_backward<float, 1, false>(g, form, items, bytes, device, s);
   }
   if (e == cudaSuccess) {
     group_norm_join_kernel<<<dim3((C + GN_JOIN_CH - 1) / GN_JOIN_CH, 2), GN_JOIN_CH * GN_JOIN_LANES, 0, s>>>(g.part, g.splits, C, d_dgamma, d_dbeta);

@@ -304,7 +304,6 @@ EncodeTiledFn encode_fn() {
   return reinterpret_cast<EncodeTiledFn>(fn);
 }
 
-constexpr int BIAS_SHARES = 64;
 struct WgradPlan { int bn, ctas; size_t share_bytes, bytes; };
 
 WgradPlan wgrad_plan(WgradArgs& g, bool fp32, int sms) {
@@ -316,7 +315,7 @@ WgradPlan wgrad_plan(WgradArgs& g, bool fp32, int sms) {
   g.line = g.stages * g.taps * g.tiles_k * g.tiles_o;
   p.ctas = (int)min((long long)sms, max(1ll, g.line / 2));
   p.share_bytes = (size_t)2 * p.ctas * WG_BM * p.bn * 4;
-  p.bytes = p.share_bytes + (size_t)BIAS_SHARES * g.O * 4;
+  p.bytes = p.share_bytes + (size_t)(p.ctas + (long long)g.taps * g.tiles_k * g.tiles_o) * WG_BIAS * 4;
   return p;
 }
 
@@ -326,7 +325,8 @@ cudaError_t wgrad_launch(const CUtensorMap& map, const WgradArgs& g, int ctas, i
   const cudaError_t e = allow_smem(weight_grad_kernel<BN, DYK>, wg_smem_bytes(BN, DYK), device, done);
   if (e != cudaSuccess) return e;
   weight_grad_kernel<BN, DYK><<<ctas, WG_THREADS, wg_smem_bytes(BN, DYK), s>>>(map, g);
-  weight_grad_join_kernel<BN><<<(unsigned)(4ll * g.taps * g.tiles_k * g.tiles_o), 256, 0, s>>>(g, ctas);
+  const int tiles = g.taps * g.tiles_k * g.tiles_o;
+  weight_grad_join_kernel<BN><<<(unsigned)(tiles * (BN / 32) + (g.db ? g.tiles_o : 0)), 256, 0, s>>>(g, ctas, tiles);
   return cudaGetLastError();
 }
 
@@ -498,8 +498,10 @@ int tsdp_weight_grad(int device, int dtype, const tsdp_saved_t* saved_x, const v
   g.dW = d_dW;
   const bool fp32 = dtype == TSDP_TYPE_FP32;
   const WgradPlan p = wgrad_plan(g, fp32, device_sms(device));
-  if (workspace_bytes < p.bytes || 4ll * g.taps * g.tiles_k * g.tiles_o >= (1ll << 31)) return TSDP_ERR_ARG;
+  if (workspace_bytes < p.bytes || 9ll * g.taps * g.tiles_k * g.tiles_o >= (1ll << 31)) return TSDP_ERR_ARG;
   g.share = reinterpret_cast<float*>(d_workspace);
+  g.db = d_db;
+  g.bias = reinterpret_cast<float*>(reinterpret_cast<char*>(d_workspace) + p.share_bytes);
   CUtensorMap map{};
   const bool tma = !fp32 && aligned16(d_dy) && dy_l % 8 == 0 && dy_l >= O && dy_l < (1ll << 38);
   if (tma) {
@@ -516,14 +518,6 @@ int tsdp_weight_grad(int device, int dtype, const tsdp_saved_t* saved_x, const v
   else if (p.bn == 64) e = tma ? wgrad_launch<64, WG_DY_TMA>(map, g, p.ctas, device, s) : wgrad_launch<64, WG_DY_BF16>(map, g, p.ctas, device, s);
   else if (p.bn == 128) e = tma ? wgrad_launch<128, WG_DY_TMA>(map, g, p.ctas, device, s) : wgrad_launch<128, WG_DY_BF16>(map, g, p.ctas, device, s);
   else e = tma ? wgrad_launch<256, WG_DY_TMA>(map, g, p.ctas, device, s) : wgrad_launch<256, WG_DY_BF16>(map, g, p.ctas, device, s);
-  if (e == cudaSuccess && d_db) {
-    float* part = reinterpret_cast<float*>(reinterpret_cast<char*>(d_workspace) + p.share_bytes);
-    const dim3 grid((O + 31) / 32, BIAS_SHARES);
-    if (fp32) bias_grad_kernel<float><<<grid, 256, 0, s>>>(reinterpret_cast<const float*>(d_dy), dy_l, g.M, O, part);
-    else bias_grad_kernel<__nv_bfloat16><<<grid, 256, 0, s>>>(reinterpret_cast<const __nv_bfloat16*>(d_dy), dy_l, g.M, O, part);
-    bias_grad_join_kernel<<<(O + 255) / 256, 256, 0, s>>>(part, BIAS_SHARES, O, d_db);
-    e = cudaGetLastError();
-  }
   return e == cudaSuccess ? TSDP_OK : fail_cuda("tsdp_weight_grad", e);
 }
 

@@ -9,12 +9,17 @@
 // A tile of dW is 128 input channels x BN output channels of one tap; the reduction runs over rows (n, l), 64 to a stage.  Both
 // operands come row by row, that is with the reduction index slowest: the tensor core reads them "MN-major" from rows of 128 bytes
 // in the 128-byte swizzle.
-//   warps 2..9   x^: a thread fetches 32 channels of one row (q and one byte b, a stage ahead), turns them into bf16 and stores them into
-//                the swizzled tile; the tap's shift and the zeros outside a sequence are made here.  dy goes the same way where TMA cannot
-//                take it (fp32, unaligned rows).
+//   warps 2..9   x^: a thread fetches 32 channels of one row (q and one byte b, three stages ahead), turns them into bf16 and stores them
+//                into the swizzled tile; the tap's shift and the zeros outside a sequence are made here.  dy goes the same way where TMA
+//                cannot take it (fp32, unaligned rows).
 //   warp 0       dy by TMA otherwise
 //   warp 1       one thread issues tcgen05.mma into one of two accumulators in tensor memory
 //   warps 10..13 epilogue: the accumulator to dW, or to this CTA's share of it
+//   warps 14..17 the bias gradient, from the dy tile that is in shared memory anyway; the tiles of one column of dW (other input channels) take
+//                turns at the stages
+// The tensor core cuts a sum of fp32 where fp32 arithmetic rounds it: 4 10^-9 of the result a step, all to one side.  So an accumulator
+// takes WG_CHUNK stages and is then added, rounded, to this CTA's share in the L2, while the other accumulator fills (2048 rows: 5 10^-7 off;
+// 4400 in one go were 1.2 10^-6, 9700 3.7 10^-6).
 // Work is the line of all (tile, stage) pairs, cut into equal pieces, one per CTA, so that no CTA is idle whatever the sizes; a tile that
 // more than one CTA worked on is added up from their shares in the order of the line: the same bits on every run.
 // Every wait is bounded; a CTA whose wait runs out leaves NaN in what it had to write.
@@ -24,8 +29,9 @@
 
 namespace tsdp {
 
-constexpr int WG_BM = 128, WG_BK = 64, WG_THREADS = 448, WG_LOADERS = 256, WG_STAGE_A = WG_BK * WG_BM * 2;
+constexpr int WG_BM = 128, WG_BK = 64, WG_THREADS = 576, WG_LOADERS = 256, WG_AHEAD = 3, WG_BIAS = 256, WG_STAGE_A = WG_BK * WG_BM * 2;
 enum { WG_DY_TMA = 0, WG_DY_BF16 = 1, WG_DY_FP32 = 2 };
+__host__ __device__ constexpr int wg_chunk(int dyk) { return dyk == WG_DY_FP32 ? 8 : 32; }      // (three products a stage in fp32)
 __host__ __device__ constexpr int wg_parts(int dyk) { return dyk == WG_DY_FP32 ? 3 : 1; }
 __host__ __device__ constexpr int wg_stage_bytes(int BN, int dyk) { return WG_STAGE_A + wg_parts(dyk) * WG_BK * BN * 2; }
 __host__ __device__ constexpr int wg_stages(int BN, int dyk) {
@@ -41,7 +47,8 @@ struct WgradArgs {
   int tiles_k, tiles_o;                     // tile = (tap, kt, ot), ot fastest
   long long stages, line;                   // of a tile; of all tiles
   float* dW;                                // [taps, K, O]
-  float* share;                             // [2 grid][128][BN]: what a CTA has of its first / of its last tile
+  float* share;                             // [2 grid][BN / 4][128][4]: what a CTA has of its first / of its last tile
+  float *db, *bias;                         // [O] or null; [grid + tiles][WG_BIAS]: shares of it, of CTA i in tile t at i + t
 };
 // The line's piece of CTA i of n.
 __host__ __device__ inline long long wg_begin(long long line, int i, int n) { return line / n * i + min((long long)i, line % n); }
@@ -73,7 +80,7 @@ __device__ __forceinline__ void st_shared16(uint32_t addr, uint32_t a, uint32_t 
 template <int BN, int DYK>
 __global__ void __launch_bounds__(WG_THREADS, 1)
 weight_grad_kernel(const __grid_constant__ CUtensorMap tmDy, WgradArgs g) {
-  constexpr int STAGES = wg_stages(BN, DYK), STAGE_BYTES = wg_stage_bytes(BN, DYK), PARTS = wg_parts(DYK);
+  constexpr int STAGES = wg_stages(BN, DYK), STAGE_BYTES = wg_stage_bytes(BN, DYK), PARTS = wg_parts(DYK), CHUNK = wg_chunk(DYK);
   constexpr uint32_t TMEM_COLS = 2 * BN < 32 ? 32 : 2 * BN;
   constexpr uint32_t IDESC = umma_idesc_bf16(BN, WG_BM) | (1u << 15) | (1u << 16);      // both operands MN-major
   extern __shared__ uint8_t wg_raw[];
@@ -86,7 +93,7 @@ weight_grad_kernel(const __grid_constant__ CUtensorMap tmDy, WgradArgs g) {
   const uint32_t slot = bar0 + 8u * (2 * STAGES + 4);
   const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
   if (threadIdx.x == 0) {
-    for (int s = 0; s < STAGES; ++s) { ptx::mbar_init(full(s), WG_LOADERS / 32 + (DYK == WG_DY_TMA ? 1 : 0)); ptx::mbar_init(empty(s), 1); }
+    for (int s = 0; s < STAGES; ++s) { ptx::mbar_init(full(s), WG_LOADERS / 32 + (DYK == WG_DY_TMA ? 1 : 0)); ptx::mbar_init(empty(s), g.db ? 5 : 1); }
     for (int b = 0; b < 2; ++b) { ptx::mbar_init(tfull(b), 1); ptx::mbar_init(tempty(b), 4); }
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -120,7 +127,7 @@ weight_grad_kernel(const __grid_constant__ CUtensorMap tmDy, WgradArgs g) {
   } else if (warp == 1) {
     if (ptx::elect_one()) {
       long long t = t_first;
-      int st = (int)(begin - t * g.stages), s = 0, buf = 0;
+      int st = (int)(begin - t * g.stages), s = 0, buf = 0, chunk = 0;
       uint32_t ph = 0, tph = 1;
       bool fresh = true;
       for (long long i = begin; i < end; ++i) {
@@ -138,9 +145,11 @@ weight_grad_kernel(const __grid_constant__ CUtensorMap tmDy, WgradArgs g) {
         fresh = false;
         ptx::tc_commit(empty(s));
         if (++s == STAGES) { s = 0; ph ^= 1; }
-        if (++st == g.stages || i + 1 == end) {
+        const bool done = ++st == g.stages;
+        if (++chunk == CHUNK || done || i + 1 == end) {
           ptx::tc_commit(tfull(buf));
-          st = 0; ++t; fresh = true;
+          chunk = 0; fresh = true;
+          if (done) { st = 0; ++t; }
           if (++buf == 2) { buf = 0; tph ^= 1; }
         }
       }
@@ -149,56 +158,71 @@ weight_grad_kernel(const __grid_constant__ CUtensorMap tmDy, WgradArgs g) {
     // x^ (and dy where it does not come by TMA): row of the stage, block of 32 channels
     const int tid = threadIdx.x - 64, r = tid >> 2, bq = tid & 3, nb = copy_blocks(g.K);
     const bool wide = (g.K & 15) == 0 && ((uintptr_t)g.x.q & 15) == 0;
-    struct Fetch { uint32_t w[8]; uint32_t b; } f;
-    long long t = t_first;
-    int st = (int)(begin - t * g.stages);
-    int l = (int)(((long long)st * WG_BK + r) % g.L);                    // position of the row in its sequence
+    struct Fetch { uint32_t w[8]; uint32_t b; } f[WG_AHEAD];
+    // where the next fetch reads: tile t, stage st, position l of this thread's row in its sequence
+    long long t = t_first, m = 0;
+    int st = (int)(begin - t * g.stages), l = 0, shift = 0, c = 0;
     const int l_step = WG_BK % g.L;
+    const signed char* qp = nullptr;
+    const unsigned char* bp = nullptr;
+    auto place = [&] {
+      const int tk = (int)(t / g.tiles_o), tap = tk / g.tiles_k;
+      shift = tap - g.taps / 2;
+      c = (tk - tap * g.tiles_k) * WG_BM + bq * 32;
+      m = (long long)st * WG_BK + r;
+      l = (int)(m % g.L);
+      qp = g.x.q + (m + shift) * g.K + c;
+      bp = g.x.b + (m + shift) * nb + (c >> 5);
+    };
     auto fetch = [&](Fetch& o) {
-      const int kt = (int)((t / g.tiles_o) % g.tiles_k), tap = (int)(t / g.tiles_o / g.tiles_k);
-      const int shift = tap - g.taps / 2, ls = l + shift;
-      const long long m = (long long)st * WG_BK + r, ms = m + shift;
-      const int c = kt * WG_BM + bq * 32;
-      const bool in = m < g.M && ls >= 0 && ls < g.L && c < g.K;
-      o.b = in ? (uint32_t)g.x.b[ms * nb + (c >> 5)] : 0u;
+      const bool in = m < g.M && (unsigned)(l + shift) < (unsigned)g.L && c < g.K;
+      o.b = in ? (uint32_t)*bp : 0u;
 #pragma unroll
       for (int j = 0; j < 8; ++j) o.w[j] = 0u;
       if (in) {
-        const signed char* q = g.x.q + ms * g.K + c;
         if (wide) {
-          const uint4 u = *reinterpret_cast<const uint4*>(q);
+          const uint4 u = *reinterpret_cast<const uint4*>(qp);
           o.w[0] = u.x; o.w[1] = u.y; o.w[2] = u.z; o.w[3] = u.w;
           if (c + 16 < g.K) {
-            const uint4 v = *reinterpret_cast<const uint4*>(q + 16);
+            const uint4 v = *reinterpret_cast<const uint4*>(qp + 16);
             o.w[4] = v.x; o.w[5] = v.y; o.w[6] = v.z; o.w[7] = v.w;
           }
         } else {
 #pragma unroll
           for (int j = 0; j < 32; ++j)
-            if (c + j < g.K) o.w[j >> 2] |= (uint32_t)(unsigned char)q[j] << (8 * (j & 3));
+            if (c + j < g.K) o.w[j >> 2] |= (uint32_t)(unsigned char)qp[j] << (8 * (j & 3));
         }
       }
+      if (++st == g.stages) { st = 0; ++t; place(); }
+      else {
+        m += WG_BK;
+        qp += (long long)WG_BK * g.K;
+        bp += (long long)WG_BK * nb;
+        l += l_step;
+        if (l >= g.L) l -= g.L;
+      }
     };
-    auto step = [&] {
-      l += l_step;
-      if (l >= g.L) l -= g.L;
-      if (++st == g.stages) { st = 0; ++t; l = r % g.L; }
-    };
+    place();
     // rows of 128 bytes per 64 channels; the two halves of a row take their 16-byte pieces in another order, so that the eight threads of
     // a store phase (two rows, four blocks) touch eight different pieces
     const uint32_t half = (uint32_t)(bq >> 1), row_off = half * (WG_BK * 128) + (uint32_t)r * 128;
     const uint32_t ch0 = (uint32_t)(bq & 1) * 4, rx = (uint32_t)(r & 7);
     int s = 0;
     uint32_t ph = 1;
-    if (begin < end) fetch(f);
-    for (long long i = begin; i < end && ok; ++i) {
-      Fetch cur = f;
-      const long long m_cur = (long long)st * WG_BK + r;
-      const int o0 = (int)(t % g.tiles_o) * BN;
-      step();
-      if (i + 1 < end) fetch(f);
+    [[maybe_unused]] long long t_cur = t_first;               // the stage that is stored, for a dy that is read here
+    [[maybe_unused]] int st_cur = st;
+#pragma unroll
+    for (int d = 0; d < WG_AHEAD; ++d)
+      if (begin + d < end) fetch(f[d]);
+    for (long long i0 = begin; i0 < end && ok; i0 += WG_AHEAD)
+#pragma unroll
+    for (int d = 0; d < WG_AHEAD; ++d) {
+      const long long i = i0 + d;
+      if (i >= end || !ok) continue;
+      const Fetch cur = f[d];
       ok = ptx::mbar_wait_warp(empty(s), ph);
-      if (!ok) break;
+      if (!ok) continue;
+      if (i + WG_AHEAD < end) fetch(f[d]);
       const uint32_t a0 = base + s * STAGE_BYTES;
       const uint32_t sb = cur.b == 255u ? 0x7fc0u : cur.b << 7, sb2 = sb | sb << 16;
       const __nv_bfloat162 stp = *reinterpret_cast<const __nv_bfloat162*>(&sb2);
@@ -212,6 +236,9 @@ weight_grad_kernel(const __grid_constant__ CUtensorMap tmDy, WgradArgs g) {
       }
       if constexpr (DYK != WG_DY_TMA) {
         // eight output channels at a time
+        const long long m_cur = (long long)st_cur * WG_BK + r;
+        const int o0 = (int)(t_cur % g.tiles_o) * BN;
+        if (++st_cur == g.stages) { st_cur = 0; ++t_cur; }
         const bool row_in = m_cur < g.M;
         const uint32_t b0 = a0 + WG_STAGE_A;
         for (int u = bq; u < BN / 8; u += 4) {
@@ -255,7 +282,7 @@ weight_grad_kernel(const __grid_constant__ CUtensorMap tmDy, WgradArgs g) {
       if (lane == 0) ptx::mbar_arrive(full(s));
       if (++s == STAGES) { s = 0; ph ^= 1; }
     }
-  } else {
+  } else if (warp < 14) {
     const int quad = warp & 3, row = quad * 32 + lane;                   // tensor-memory lane quadrant of this warp; input channel of the tile
     long long i = begin, t = t_first;
     int buf = 0;
@@ -263,39 +290,90 @@ weight_grad_kernel(const __grid_constant__ CUtensorMap tmDy, WgradArgs g) {
     while (i < end) {
       const long long t_end = min((t + 1) * g.stages, end);
       const bool whole = i == t * g.stages && t_end == (t + 1) * g.stages;
-      const bool good = ok && ptx::mbar_wait_warp(tfull(buf), ph);
-      ptx::tc_fence_after();
-      const int o0 = (int)(t % g.tiles_o) * BN, kt = (int)((t / g.tiles_o) % g.tiles_k), tap = (int)(t / g.tiles_o / g.tiles_k);
-      const int k = kt * WG_BM + row;
-      float* out = whole ? g.dW + ((long long)tap * g.K + k) * g.O + o0 : g.share + ((2ll * blockIdx.x + (t == t_first ? 0 : 1)) * WG_BM + row) * BN;
-      const int cols = whole ? min(BN, g.O - o0) : BN;
-      const bool vec = !whole || ((g.O & 3) == 0 && ((uintptr_t)g.dW & 15) == 0);
-      for (int c0 = 0; c0 < BN; c0 += 32) {
-        uint32_t v[32];
-        if (good) {
-          ptx::tmem_ld32(tmem + buf * BN + ((uint32_t)(quad * 32) << 16) + c0, v);
-          ptx::tmem_ld_wait();
-        } else {
+      const int o0 = (int)(t % g.tiles_o) * BN, tk = (int)(t / g.tiles_o), tap = tk / g.tiles_k, k = (tk - tap * g.tiles_k) * WG_BM + row;
+      float* share = g.share + (2ll * blockIdx.x + (t == t_first ? 0 : 1)) * (WG_BM * BN) + row * 4;
+      float* out = g.dW + ((long long)tap * g.K + k) * g.O + o0;
+      const int cols = min(BN, g.O - o0);
+      const bool vec = (g.O & 3) == 0 && ((uintptr_t)g.dW & 15) == 0;
+      for (bool first = true; i < t_end; first = false) {
+        i = min(i + CHUNK, t_end);
+        const bool last = i == t_end;
+        ok = ok && ptx::mbar_wait_warp(tfull(buf), ph);
+        ptx::tc_fence_after();
+        for (int c0 = 0; c0 < BN; c0 += 32) {
+          uint32_t v[32];
+          if (ok) {
+            ptx::tmem_ld32(tmem + buf * BN + ((uint32_t)(quad * 32) << 16) + c0, v);
+            ptx::tmem_ld_wait();
+          } else {
 #pragma unroll
-          for (int j = 0; j < 32; ++j) v[j] = 0x7fc00000u;
+            for (int j = 0; j < 32; ++j) v[j] = 0x7fc00000u;
+          }
+          float* sh = share + c0 * WG_BM;                                  // the share, four columns of 128 rows at a time
+          if (!first) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+              const float4 u = *reinterpret_cast<const float4*>(sh + j * 4 * WG_BM);
+              v[4 * j] = __float_as_uint(__uint_as_float(v[4 * j]) + u.x); v[4 * j + 1] = __float_as_uint(__uint_as_float(v[4 * j + 1]) + u.y);
+              v[4 * j + 2] = __float_as_uint(__uint_as_float(v[4 * j + 2]) + u.z); v[4 * j + 3] = __float_as_uint(__uint_as_float(v[4 * j + 3]) + u.w);
+            }
+          }
+          if (!(last && whole)) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) *reinterpret_cast<uint4*>(sh + j * 4 * WG_BM) = make_uint4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
+          } else if (k < g.K && vec) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+              if (c0 + 4 * j < cols) *reinterpret_cast<uint4*>(out + c0 + 4 * j) = make_uint4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
+          } else if (k < g.K) {
+#pragma unroll
+            for (int j = 0; j < 32; ++j)
+              if (c0 + j < cols) out[c0 + j] = __uint_as_float(v[j]);
+          }
         }
-        if (whole && k >= g.K) continue;
-        if (vec) {
-#pragma unroll
-          for (int j = 0; j < 8; ++j)
-            if (c0 + 4 * j < cols) *reinterpret_cast<uint4*>(out + c0 + 4 * j) = make_uint4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
-        } else {
-#pragma unroll
-          for (int j = 0; j < 32; ++j)
-            if (c0 + j < cols) out[c0 + j] = __uint_as_float(v[j]);
-        }
+        ptx::tc_fence_before();
+        __syncwarp();
+        if (lane == 0) ptx::mbar_arrive(tempty(buf));
+        if (++buf == 2) { buf = 0; ph ^= 1; }
       }
-      if (!good) ok = false;
-      ptx::tc_fence_before();
+      ++t;
+    }
+  } else if (g.db) {
+    // two columns of the dy tile a thread; with fewer columns than threads they share the rows
+    constexpr int PAIRS = BN / 2, GROUPS = 128 / PAIRS, ROWS = WG_BK / GROUPS;
+    const int tb = threadIdx.x - 448, pair = tb % PAIRS, grp = tb / PAIRS;
+    const uint32_t at = (uint32_t)(pair >> 5) * (WG_BK * 128) + (uint32_t)grp * ROWS * 128 + (uint32_t)(pair & 3) * 4, unit = (uint32_t)(pair & 31) >> 2;
+    long long t = t_first;
+    int st = (int)(begin - t * g.stages), s = 0;
+    uint32_t ph = 0;
+    float2 sum = make_float2(0.f, 0.f);
+    for (long long i = begin; i < end; ++i) {
+      const int tk = (int)(t / g.tiles_o), tap = tk / g.tiles_k, kt = tk - tap * g.tiles_k;
+      const bool centre = tap == g.taps / 2;
+      ok = ptx::mbar_wait_warp(full(s), ph);
+      if (!ok) break;
+      if (centre && st % g.tiles_k == kt) {
+        float2 part = make_float2(0.f, 0.f);                               // (of a stage apart: fewer additions to the long sum)
+#pragma unroll
+        for (int p = 0; p < PARTS; ++p) {
+          const uint8_t* b0 = wg_raw + (base - ptx::smem_u32(wg_raw)) + s * STAGE_BYTES + WG_STAGE_A + p * (WG_BK * BN * 2) + at;
+#pragma unroll 8
+          for (int r = 0; r < ROWS; ++r) {
+            const uint32_t u = *reinterpret_cast<const uint32_t*>(b0 + r * 128 + ((unit ^ (uint32_t)(r & 7)) << 4));
+            part = __fadd2_rn(part, make_float2(__uint_as_float(u << 16), __uint_as_float(u & 0xffff0000u)));
+          }
+        }
+        sum = __fadd2_rn(sum, part);
+      }
       __syncwarp();
-      if (lane == 0) ptx::mbar_arrive(tempty(buf));
-      if (++buf == 2) { buf = 0; ph ^= 1; }
-      i = t_end; ++t;
+      if (lane == 0) ptx::mbar_arrive(empty(s));
+      if (++s == STAGES) { s = 0; ph ^= 1; }
+      const bool done = ++st == g.stages;
+      if (done || i + 1 == end) {
+        if (centre) *reinterpret_cast<float2*>(g.bias + (blockIdx.x + t) * WG_BIAS + grp * BN + 2 * pair) = sum;
+        sum = make_float2(0.f, 0.f);
+        if (done) { st = 0; ++t; }
+      }
     }
   }
   if (!ok) {
@@ -308,60 +386,62 @@ weight_grad_kernel(const __grid_constant__ CUtensorMap tmDy, WgradArgs g) {
   if (warp == 1) ptx::tmem_dealloc(tmem, TMEM_COLS);
 }
 
-// Tiles that several CTAs worked on: their shares, in the order of the line.  One block per tile and 32 of its rows.
+// CTAs first .. last of the line's pieces that hold stages of tile t.
+__device__ __forceinline__ void wg_owners(const WgradArgs& g, int ctas, long long t, int& first, int& last) {
+  const long long q = g.line / ctas, rem = g.line % ctas, a = t * g.stages, b = a + g.stages - 1;
+  auto owner = [&](long long i) { return (int)(i < rem * (q + 1) ? i / (q + 1) : rem + (i - rem * (q + 1)) / q); };
+  first = owner(a); last = owner(b);
+}
+
+// Tiles that several CTAs worked on: their shares, in the order of the line; a block has 32 columns of a tile, a warp 8 rows x 16 columns at
+// a time (128 bytes of a share, 64 bytes of a row of dW).  The last tiles_o blocks (with db): the bias gradient of a column of tiles.
 template <int BN>
 __global__ void __launch_bounds__(256)
-weight_grad_join_kernel(WgradArgs g, int ctas) {
-  const long long t = blockIdx.x >> 2;
-  const long long a = t * g.stages, b = a + g.stages;
-  // the CTA that holds stage a: pieces differ by one in length, so the quotient is off by one at most
-  int i = (int)min((long long)ctas - 1, a / (g.line / ctas + 1));
-  while (i + 1 < ctas && wg_begin(g.line, i + 1, ctas) <= a) ++i;
-  if (wg_begin(g.line, i + 1, ctas) >= b) return;                        // one CTA had all of it
-  const int o0 = (int)(t % g.tiles_o) * BN, kt = (int)((t / g.tiles_o) % g.tiles_k), tap = (int)(t / g.tiles_o / g.tiles_k);
-  const int row0 = (blockIdx.x & 3) * 32;
-  for (int e = threadIdx.x * 4; e < 32 * BN; e += 256 * 4) {
-    const int row = row0 + e / BN, c = e % BN, k = kt * WG_BM + row;
+weight_grad_join_kernel(WgradArgs g, int ctas, int tiles) {
+  const int parts = BN / 32;
+  int first, last;
+  if ((int)blockIdx.x >= tiles * parts) {
+    __shared__ float s_db[WG_BIAS];
+    const int ot = blockIdx.x - tiles * parts, col = threadIdx.x % BN;
+    float v = 0.f;
+    for (int kt = 0; kt < g.tiles_k; ++kt) {
+      const long long t = ((long long)(g.taps / 2) * g.tiles_k + kt) * g.tiles_o + ot;
+      wg_owners(g, ctas, t, first, last);
+#pragma unroll 4
+      for (int i = first; i <= last; ++i) v += g.bias[(i + t) * WG_BIAS + threadIdx.x];
+    }
+    s_db[threadIdx.x] = v;
+    __syncthreads();
+    if (threadIdx.x >= BN || ot * BN + col >= g.O) return;
+    for (int i = 1; i < WG_BIAS / BN; ++i) v += s_db[i * BN + col];
+    g.db[ot * BN + col] = v;
+    return;
+  }
+  const long long t = blockIdx.x / parts;
+  wg_owners(g, ctas, t, first, last);
+  if (first == last) return;                                             // one CTA had all of it
+  const int o0 = (int)(t % g.tiles_o) * BN, tk = (int)(t / g.tiles_o), tap = tk / g.tiles_k, k0 = (tk - tap * g.tiles_k) * WG_BM;
+  const int which0 = wg_begin(g.line, first, ctas) / g.stages == t ? 0 : 1;          // of the first; the others begin in this tile
+  const bool vec = (g.O & 3) == 0 && ((uintptr_t)g.dW & 15) == 0;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const int e = j * 256 + threadIdx.x, row = ((e >> 5) & 15) * 8 + (e & 7), quad = (e >> 9) * 4 + ((e >> 3) & 3);
+    const int c = (blockIdx.x % parts) * 32 + quad * 4, k = k0 + row;
     if (k >= g.K || o0 + c >= g.O) continue;
-    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-    for (int j = i; j < ctas && wg_begin(g.line, j, ctas) < b; ++j) {
-      const int which = wg_begin(g.line, j, ctas) / g.stages == t ? 0 : 1;
-      const float4 u = *reinterpret_cast<const float4*>(g.share + ((2ll * j + which) * WG_BM + row) * BN + c);
+    const float* sh = g.share + (c >> 2) * (WG_BM * 4) + row * 4;
+    float4 v = *reinterpret_cast<const float4*>(sh + (2ll * first + which0) * (WG_BM * BN));
+#pragma unroll 4
+    for (int i = first + 1; i <= last; ++i) {
+      const float4 u = *reinterpret_cast<const float4*>(sh + 2ll * i * (WG_BM * BN));
       v.x += u.x; v.y += u.y; v.z += u.z; v.w += u.w;
     }
     float* out = g.dW + ((long long)tap * g.K + k) * g.O + o0 + c;
-    if ((g.O & 3) == 0 && ((uintptr_t)g.dW & 15) == 0) *reinterpret_cast<float4*>(out) = v;
+    if (vec) *reinterpret_cast<float4*>(out) = v;
     else {
       const float w[4] = {v.x, v.y, v.z, v.w};
-      for (int j = 0; j < 4; ++j) if (o0 + c + j < g.O) out[j] = w[j];
+      for (int i = 0; i < 4; ++i) if (o0 + c + i < g.O) out[i] = w[i];
     }
   }
-}
-
-// db[o] = sum of dy over the rows: a block takes 32 columns and a share of the rows, the shares are joined by group_norm_join's scheme.
-template <typename T>
-__global__ void __launch_bounds__(256)
-bias_grad_kernel(const T* dy, long long ldy, long long M, int O, float* part) {
-  __shared__ float s[8][32];
-  const int o = blockIdx.x * 32 + (threadIdx.x & 31), lane = threadIdx.x >> 5;
-  const long long share = (M + gridDim.y - 1) / gridDim.y, lo = blockIdx.y * share, hi = min(M, lo + share);
-  float v = 0.f;
-  if (o < O)
-    for (long long m = lo + lane; m < hi; m += 8) v += to_f(dy[m * ldy + o]);
-  s[lane][threadIdx.x & 31] = v;
-  __syncthreads();
-  if (lane == 0 && o < O) {
-    for (int i = 1; i < 8; ++i) v += s[i][threadIdx.x];
-    part[(long long)blockIdx.y * O + o] = v;
-  }
-}
-__global__ void __launch_bounds__(256)
-bias_grad_join_kernel(const float* part, int shares, int O, float* db) {
-  const int o = blockIdx.x * 256 + threadIdx.x;
-  if (o >= O) return;
-  float v = 0.f;
-  for (int i = 0; i < shares; ++i) v += part[(long long)i * O + o];
-  db[o] = v;
 }
 
 }  // namespace tsdp

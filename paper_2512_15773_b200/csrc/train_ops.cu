@@ -311,9 +311,10 @@ WgradPlan wgrad_plan(WgradArgs& g, bool fp32, int sms) {
   p.bn = g.O <= 64 ? 64 : (g.O <= 128 || fp32 ? 128 : 256);
   g.tiles_k = (g.K + WG_BM - 1) / WG_BM;
   g.tiles_o = (g.O + p.bn - 1) / p.bn;
-  g.stages = (g.M + WG_BK - 1) / WG_BK;
-  g.line = g.stages * g.taps * g.tiles_k * g.tiles_o;
-  p.ctas = (int)min((long long)sms, max(1ll, g.line / 2));
+  g.stages = (int)((g.M + WG_BK - 1) / WG_BK);
+  const long long line = (long long)g.stages * g.taps * g.tiles_k * g.tiles_o;
+  g.line = line < (1ll << 31) - 4096 ? (int)line : 0;
+  p.ctas = (int)min((long long)sms, max(1ll, line / 2));
   p.share_bytes = (size_t)2 * p.ctas * WG_BM * p.bn * 4;
   p.bytes = p.share_bytes + (size_t)(p.ctas + (long long)g.taps * g.tiles_k * g.tiles_o) * WG_BIAS * 4;
   return p;
@@ -326,7 +327,7 @@ cudaError_t wgrad_launch(const CUtensorMap& map, const WgradArgs& g, int ctas, i
   if (e != cudaSuccess) return e;
   weight_grad_kernel<BN, DYK><<<ctas, WG_THREADS, wg_smem_bytes(BN, DYK), s>>>(map, g);
   const int tiles = g.taps * g.tiles_k * g.tiles_o;
-  weight_grad_join_kernel<BN><<<(unsigned)(tiles * (BN / 32) + (g.db ? g.tiles_o : 0)), 256, 0, s>>>(g, ctas, tiles);
+  weight_grad_join_kernel<BN><<<(unsigned)(tiles * (BN / 16) + (g.db ? g.tiles_o : 0)), 256, 0, s>>>(g, ctas, tiles);
   return cudaGetLastError();
 }
 
@@ -475,7 +476,8 @@ size_t tsdp_weight_grad_workspace(int device, int dtype, int N, int L, int K, in
   if (device < 0 || device >= MAX_DEVICES || !wgrad_ok(dtype, N, L, K, O, taps)) return 0;
   WgradArgs g{};
   g.M = (long long)(N < 1 ? 1 : N) * L; g.K = K; g.O = O; g.taps = taps;
-  return wgrad_plan(g, dtype == TSDP_TYPE_FP32, device_sms(device)).bytes;
+  const size_t bytes = wgrad_plan(g, dtype == TSDP_TYPE_FP32, device_sms(device)).bytes;
+  return g.line ? bytes : 0;
 }
 
 int tsdp_weight_grad(int device, int dtype, const tsdp_saved_t* saved_x, const void* d_dy, int64_t dy_l, int N, int L, int K, int O, int taps, float* d_dW,
@@ -498,7 +500,7 @@ int tsdp_weight_grad(int device, int dtype, const tsdp_saved_t* saved_x, const v
   g.dW = d_dW;
   const bool fp32 = dtype == TSDP_TYPE_FP32;
   const WgradPlan p = wgrad_plan(g, fp32, device_sms(device));
-  if (workspace_bytes < p.bytes || 9ll * g.taps * g.tiles_k * g.tiles_o >= (1ll << 31)) return TSDP_ERR_ARG;
+  if (g.line == 0 || workspace_bytes < p.bytes || 17ll * g.taps * g.tiles_k * g.tiles_o >= (1ll << 31)) return TSDP_ERR_ARG;
   g.share = reinterpret_cast<float*>(d_workspace);
   g.db = d_db;
   g.bias = reinterpret_cast<float*>(reinterpret_cast<char*>(d_workspace) + p.share_bytes);

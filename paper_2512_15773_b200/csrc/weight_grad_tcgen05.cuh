@@ -9,14 +9,14 @@
 // A tile of dW is 128 input channels x BN output channels of one tap; the reduction runs over rows (n, l), 64 to a stage.  Both
 // operands come row by row, that is with the reduction index slowest: the tensor core reads them "MN-major" from rows of 128 bytes
 // in the 128-byte swizzle.
-//   warps 2..9   x^: a thread fetches 32 channels of one row (q and one byte b, three stages ahead), turns them into bf16 and stores them
-//                into the swizzled tile; the tap's shift and the zeros outside a sequence are made here.  dy goes the same way where TMA
-//                cannot take it (fp32, unaligned rows).
-//   warp 0       dy by TMA otherwise
+//   warp 0       dy by TMA
 //   warp 1       one thread issues tcgen05.mma into one of two accumulators in tensor memory
-//   warps 10..13 epilogue: the accumulator to dW, or to this CTA's share of it
-//   warps 14..17 the bias gradient, from the dy tile that is in shared memory anyway; the tiles of one column of dW (other input channels) take
+//   warps 2..5   epilogue: the accumulator to dW, or to this CTA's share of it
+//   warps 6..9   the bias gradient, from the dy tile that is in shared memory anyway; the tiles of one column of dW (other input channels) take
 //                turns at the stages
+//   warps 10..25 x^, eight warps a stage: a thread fetches 32 channels of one row (q and one byte b, four stages ahead), turns them into bf16
+//                and stores them into the swizzled tile; the tap's shift and the zeros outside a sequence are made here.  dy goes the
+//                same way where TMA cannot take it (fp32, unaligned rows).
 // The tensor core cuts a sum of fp32 where fp32 arithmetic rounds it: 4 10^-9 of the result a step, all to one side.  So an accumulator
 // takes WG_CHUNK stages and is then added, rounded, to this CTA's share in the L2, while the other accumulator fills (2048 rows: 5 10^-7 off;
 // 4400 in one go were 1.2 10^-6, 9700 3.7 10^-6).
@@ -29,7 +29,7 @@
 
 namespace tsdp {
 
-constexpr int WG_BM = 128, WG_BK = 64, WG_THREADS = 576, WG_LOADERS = 256, WG_AHEAD = 3, WG_BIAS = 256, WG_STAGE_A = WG_BK * WG_BM * 2;
+constexpr int WG_BM = 128, WG_BK = 64, WG_LOADERS = 256, WG_GROUPS = 2, WG_THREADS = 320 + WG_GROUPS * WG_LOADERS, WG_AHEAD = 2, WG_BIAS = 1024, WG_STAGE_A = WG_BK * WG_BM * 2;
 enum { WG_DY_TMA = 0, WG_DY_BF16 = 1, WG_DY_FP32 = 2 };
 __host__ __device__ constexpr int wg_chunk(int dyk) { return dyk == WG_DY_FP32 ? 8 : 32; }      // (three products a stage in fp32)
 __host__ __device__ constexpr int wg_parts(int dyk) { return dyk == WG_DY_FP32 ? 3 : 1; }
@@ -45,13 +45,13 @@ struct WgradArgs {
   long long M;                              // rows = sequences x L
   int L, K, O, taps;
   int tiles_k, tiles_o;                     // tile = (tap, kt, ot), ot fastest
-  long long stages, line;                   // of a tile; of all tiles
+  int stages, line;                         // of a tile; of all tiles (line + grid < 2^31)
   float* dW;                                // [taps, K, O]
   float* share;                             // [2 grid][BN / 4][128][4]: what a CTA has of its first / of its last tile
-  float *db, *bias;                         // [O] or null; [grid + tiles][WG_BIAS]: shares of it, of CTA i in tile t at i + t
+  float *db, *bias;                         // [O] or null; [grid + tiles][WG_BIAS / BN][BN]: shares of it, of CTA i in tile t at i + t
 };
 // The line's piece of CTA i of n.
-__host__ __device__ inline long long wg_begin(long long line, int i, int n) { return line / n * i + min((long long)i, line % n); }
+__host__ __device__ inline int wg_begin(int line, int i, int n) { return line / n * i + min(i, line % n); }
 
 // Descriptor of an operand tile whose reduction index is the slow one: rows (one reduction index) of 64 elements, 128 bytes apart, groups of
 // eight rows 1024 bytes apart (stride byte offset); further columns of 64 elements start `lead` bytes on (leading byte offset).
@@ -75,6 +75,11 @@ __device__ __forceinline__ uint32_t wg_pair(uint32_t word, uint32_t sel, __nv_bf
 }
 __device__ __forceinline__ void st_shared16(uint32_t addr, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
   asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
+}
+
+__device__ __forceinline__ void red_add4(float* p, const uint32_t* v) {
+  asm volatile("red.global.add.v4.f32 [%0], {%1, %2, %3, %4};" ::"l"(p), "f"(__uint_as_float(v[0])), "f"(__uint_as_float(v[1])), "f"(__uint_as_float(v[2])),
+               "f"(__uint_as_float(v[3])) : "memory");
 }
 
 template <int BN, int DYK>
@@ -104,19 +109,18 @@ weight_grad_kernel(const __grid_constant__ CUtensorMap tmDy, WgradArgs g) {
   ptx::tc_fence_after();
   const uint32_t tmem = *reinterpret_cast<volatile uint32_t*>(wg_raw + (slot - ptx::smem_u32(wg_raw)));
 
-  const long long begin = wg_begin(g.line, blockIdx.x, gridDim.x), end = wg_begin(g.line, blockIdx.x + 1, gridDim.x);
-  const long long t_first = begin / g.stages;
+  const int begin = wg_begin(g.line, blockIdx.x, gridDim.x), end = wg_begin(g.line, blockIdx.x + 1, gridDim.x);
+  const int t_first = begin / g.stages;
   bool ok = true;
 
   if (warp == 0) {
     if (DYK == WG_DY_TMA && ptx::elect_one()) {
-      long long t = t_first;
-      int st = (int)(begin - t * g.stages), s = 0;
+      int t = t_first, st = begin - t * g.stages, s = 0;
       uint32_t ph = 1;
-      for (long long i = begin; i < end; ++i) {
+      for (int i = begin; i < end; ++i) {
         if (!ptx::mbar_wait_thread(empty(s), ph)) { ok = false; break; }
         const uint32_t b0 = base + s * STAGE_BYTES + WG_STAGE_A;
-        const int o0 = (int)(t % g.tiles_o) * BN;
+        const int o0 = t % g.tiles_o * BN;
         ptx::mbar_expect_tx(full(s), BN * WG_BK * 2);
 #pragma unroll
         for (int j = 0; j < BN / 64; ++j) ptx::tma_load_2d(b0 + j * WG_BK * 128, &tmDy, o0 + 64 * j, st * WG_BK, full(s));
@@ -126,11 +130,10 @@ weight_grad_kernel(const __grid_constant__ CUtensorMap tmDy, WgradArgs g) {
     }
   } else if (warp == 1) {
     if (ptx::elect_one()) {
-      long long t = t_first;
-      int st = (int)(begin - t * g.stages), s = 0, buf = 0, chunk = 0;
+      int t = t_first, st = begin - t * g.stages, s = 0, buf = 0, chunk = 0;
       uint32_t ph = 0, tph = 1;
       bool fresh = true;
-      for (long long i = begin; i < end; ++i) {
+      for (int i = begin; i < end; ++i) {
         if (fresh && !ptx::mbar_wait_thread(tempty(buf), tph)) { ok = false; break; }
         if (!ptx::mbar_wait_thread(full(s), ph)) { ok = false; break; }
         ptx::tc_fence_after();
@@ -154,19 +157,19 @@ weight_grad_kernel(const __grid_constant__ CUtensorMap tmDy, WgradArgs g) {
         }
       }
     }
-  } else if (warp < 10) {
+  } else if (warp >= 10) {
     // x^ (and dy where it does not come by TMA): row of the stage, block of 32 channels
-    const int tid = threadIdx.x - 64, r = tid >> 2, bq = tid & 3, nb = copy_blocks(g.K);
+    const int group = (warp - 10) / (WG_LOADERS / 32), tid = (threadIdx.x - 320) % WG_LOADERS, r = tid >> 2, bq = tid & 3, nb = copy_blocks(g.K);
     const bool wide = (g.K & 15) == 0 && ((uintptr_t)g.x.q & 15) == 0;
     struct Fetch { uint32_t w[8]; uint32_t b; } f[WG_AHEAD];
     // where the next fetch reads: tile t, stage st, position l of this thread's row in its sequence
-    long long t = t_first, m = 0;
-    int st = (int)(begin - t * g.stages), l = 0, shift = 0, c = 0;
-    const int l_step = WG_BK % g.L;
+    int t = (begin + group) / g.stages, st = begin + group - t * g.stages, l = 0, shift = 0, c = 0;
+    long long m = 0;
+    const int l_step = WG_GROUPS * WG_BK % g.L;
     const signed char* qp = nullptr;
     const unsigned char* bp = nullptr;
     auto place = [&] {
-      const int tk = (int)(t / g.tiles_o), tap = tk / g.tiles_k;
+      const int tk = t / g.tiles_o, tap = tk / g.tiles_k;
       shift = tap - g.taps / 2;
       c = (tk - tap * g.tiles_k) * WG_BM + bq * 32;
       m = (long long)st * WG_BK + r;
@@ -193,11 +196,14 @@ weight_grad_kernel(const __grid_constant__ CUtensorMap tmDy, WgradArgs g) {
             if (c + j < g.K) o.w[j >> 2] |= (uint32_t)(unsigned char)qp[j] << (8 * (j & 3));
         }
       }
-      if (++st == g.stages) { st = 0; ++t; place(); }
-      else {
-        m += WG_BK;
-        qp += (long long)WG_BK * g.K;
-        bp += (long long)WG_BK * nb;
+      st += WG_GROUPS;
+      if (st >= g.stages) {
+        while (st >= g.stages) { st -= g.stages; ++t; }
+        place();
+      } else {
+        m += WG_GROUPS * WG_BK;
+        qp += (long long)WG_GROUPS * WG_BK * g.K;
+        bp += (long long)WG_GROUPS * WG_BK * nb;
         l += l_step;
         if (l >= g.L) l -= g.L;
       }
@@ -207,22 +213,22 @@ weight_grad_kernel(const __grid_constant__ CUtensorMap tmDy, WgradArgs g) {
     // a store phase (two rows, four blocks) touch eight different pieces
     const uint32_t half = (uint32_t)(bq >> 1), row_off = half * (WG_BK * 128) + (uint32_t)r * 128;
     const uint32_t ch0 = (uint32_t)(bq & 1) * 4, rx = (uint32_t)(r & 7);
-    int s = 0;
+    int s = group;
     uint32_t ph = 1;
-    [[maybe_unused]] long long t_cur = t_first;               // the stage that is stored, for a dy that is read here
+    [[maybe_unused]] int t_cur = t;                           // the stage that is stored, for a dy that is read here
     [[maybe_unused]] int st_cur = st;
 #pragma unroll
     for (int d = 0; d < WG_AHEAD; ++d)
-      if (begin + d < end) fetch(f[d]);
-    for (long long i0 = begin; i0 < end && ok; i0 += WG_AHEAD)
+      if (begin + group + d * WG_GROUPS < end) fetch(f[d]);
+    for (int i0 = begin + group; i0 < end && ok; i0 += WG_AHEAD * WG_GROUPS)
 #pragma unroll
     for (int d = 0; d < WG_AHEAD; ++d) {
-      const long long i = i0 + d;
+      const int i = i0 + d * WG_GROUPS;
       if (i >= end || !ok) continue;
       const Fetch cur = f[d];
       ok = ptx::mbar_wait_warp(empty(s), ph);
       if (!ok) continue;
-      if (i + WG_AHEAD < end) fetch(f[d]);
+      if (i + WG_AHEAD * WG_GROUPS < end) fetch(f[d]);
       const uint32_t a0 = base + s * STAGE_BYTES;
       const uint32_t sb = cur.b == 255u ? 0x7fc0u : cur.b << 7, sb2 = sb | sb << 16;
       const __nv_bfloat162 stp = *reinterpret_cast<const __nv_bfloat162*>(&sb2);
@@ -237,8 +243,9 @@ weight_grad_kernel(const __grid_constant__ CUtensorMap tmDy, WgradArgs g) {
       if constexpr (DYK != WG_DY_TMA) {
         // eight output channels at a time
         const long long m_cur = (long long)st_cur * WG_BK + r;
-        const int o0 = (int)(t_cur % g.tiles_o) * BN;
-        if (++st_cur == g.stages) { st_cur = 0; ++t_cur; }
+        const int o0 = t_cur % g.tiles_o * BN;
+        st_cur += WG_GROUPS;
+        while (st_cur >= g.stages) { st_cur -= g.stages; ++t_cur; }
         const bool row_in = m_cur < g.M;
         const uint32_t b0 = a0 + WG_STAGE_A;
         for (int u = bq; u < BN / 8; u += 4) {
@@ -280,17 +287,17 @@ weight_grad_kernel(const __grid_constant__ CUtensorMap tmDy, WgradArgs g) {
       ptx::fence_async_smem();
       __syncwarp();
       if (lane == 0) ptx::mbar_arrive(full(s));
-      if (++s == STAGES) { s = 0; ph ^= 1; }
+      s += WG_GROUPS;
+      if (s >= STAGES) { s -= STAGES; ph ^= 1; }
     }
-  } else if (warp < 14) {
+  } else if (warp < 6) {
     const int quad = warp & 3, row = quad * 32 + lane;                   // tensor-memory lane quadrant of this warp; input channel of the tile
-    long long i = begin, t = t_first;
-    int buf = 0;
+    int i = begin, t = t_first, buf = 0;
     uint32_t ph = 0;
     while (i < end) {
-      const long long t_end = min((t + 1) * g.stages, end);
+      const int t_end = min((t + 1) * g.stages, end);
       const bool whole = i == t * g.stages && t_end == (t + 1) * g.stages;
-      const int o0 = (int)(t % g.tiles_o) * BN, tk = (int)(t / g.tiles_o), tap = tk / g.tiles_k, k = (tk - tap * g.tiles_k) * WG_BM + row;
+      const int o0 = t % g.tiles_o * BN, tk = t / g.tiles_o, tap = tk / g.tiles_k, k = (tk - tap * g.tiles_k) * WG_BM + row;
       float* share = g.share + (2ll * blockIdx.x + (t == t_first ? 0 : 1)) * (WG_BM * BN) + row * 4;
       float* out = g.dW + ((long long)tap * g.K + k) * g.O + o0;
       const int cols = min(BN, g.O - o0);
@@ -300,34 +307,40 @@ weight_grad_kernel(const __grid_constant__ CUtensorMap tmDy, WgradArgs g) {
         const bool last = i == t_end;
         ok = ok && ptx::mbar_wait_warp(tfull(buf), ph);
         ptx::tc_fence_after();
-        for (int c0 = 0; c0 < BN; c0 += 32) {
-          uint32_t v[32];
+        for (int c0 = 0; c0 < BN; c0 += 16) {
+          uint32_t v[16];
           if (ok) {
-            ptx::tmem_ld32(tmem + buf * BN + ((uint32_t)(quad * 32) << 16) + c0, v);
+            ptx::tmem_ld16(tmem + buf * BN + ((uint32_t)(quad * 32) << 16) + c0, v);
             ptx::tmem_ld_wait();
           } else {
 #pragma unroll
-            for (int j = 0; j < 32; ++j) v[j] = 0x7fc00000u;
+            for (int j = 0; j < 16; ++j) v[j] = 0x7fc00000u;
           }
           float* sh = share + c0 * WG_BM;                                  // the share, four columns of 128 rows at a time
+          if (!(last && whole)) {
+            // (an addition that does not wait for what it adds to; one thread's, so in its order)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              if (first) *reinterpret_cast<uint4*>(sh + j * 4 * WG_BM) = make_uint4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
+              else red_add4(sh + j * 4 * WG_BM, v + 4 * j);
+            }
+            continue;
+          }
           if (!first) {
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
+            for (int j = 0; j < 4; ++j) {
               const float4 u = *reinterpret_cast<const float4*>(sh + j * 4 * WG_BM);
               v[4 * j] = __float_as_uint(__uint_as_float(v[4 * j]) + u.x); v[4 * j + 1] = __float_as_uint(__uint_as_float(v[4 * j + 1]) + u.y);
               v[4 * j + 2] = __float_as_uint(__uint_as_float(v[4 * j + 2]) + u.z); v[4 * j + 3] = __float_as_uint(__uint_as_float(v[4 * j + 3]) + u.w);
             }
           }
-          if (!(last && whole)) {
+          if (k < g.K && vec) {
 #pragma unroll
-            for (int j = 0; j < 8; ++j) *reinterpret_cast<uint4*>(sh + j * 4 * WG_BM) = make_uint4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
-          } else if (k < g.K && vec) {
-#pragma unroll
-            for (int j = 0; j < 8; ++j)
+            for (int j = 0; j < 4; ++j)
               if (c0 + 4 * j < cols) *reinterpret_cast<uint4*>(out + c0 + 4 * j) = make_uint4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
           } else if (k < g.K) {
 #pragma unroll
-            for (int j = 0; j < 32; ++j)
+            for (int j = 0; j < 16; ++j)
               if (c0 + j < cols) out[c0 + j] = __uint_as_float(v[j]);
           }
         }
@@ -339,40 +352,54 @@ weight_grad_kernel(const __grid_constant__ CUtensorMap tmDy, WgradArgs g) {
       ++t;
     }
   } else if (g.db) {
-    // two columns of the dy tile a thread; with fewer columns than threads they share the rows
-    constexpr int PAIRS = BN / 2, GROUPS = 128 / PAIRS, ROWS = WG_BK / GROUPS;
-    const int tb = threadIdx.x - 448, pair = tb % PAIRS, grp = tb / PAIRS;
-    const uint32_t at = (uint32_t)(pair >> 5) * (WG_BK * 128) + (uint32_t)grp * ROWS * 128 + (uint32_t)(pair & 3) * 4, unit = (uint32_t)(pair & 31) >> 2;
-    long long t = t_first;
-    int st = (int)(begin - t * g.stages), s = 0;
+    // eight columns of the dy tile and a share of its rows a thread
+    constexpr int UNITS = BN / 8, GROUPS = 128 / UNITS, ROWS = WG_BK / GROUPS;
+    const int tb = threadIdx.x - 192, unit = tb % UNITS, grp = tb / UNITS;
+    const uint32_t at = (uint32_t)(unit >> 3) * (WG_BK * 128) + (uint32_t)grp * ROWS * 128;
+    int t = t_first, st = begin - t * g.stages, s = 0;
     uint32_t ph = 0;
-    float2 sum = make_float2(0.f, 0.f);
-    for (long long i = begin; i < end; ++i) {
-      const int tk = (int)(t / g.tiles_o), tap = tk / g.tiles_k, kt = tk - tap * g.tiles_k;
-      const bool centre = tap == g.taps / 2;
+    float2 sum[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) sum[j] = make_float2(0.f, 0.f);
+    int tk = t / g.tiles_o, kt = tk % g.tiles_k, turn = st % g.tiles_k;
+    bool centre = tk / g.tiles_k == g.taps / 2;
+    for (int i = begin; i < end; ++i) {
       ok = ptx::mbar_wait_warp(full(s), ph);
       if (!ok) break;
-      if (centre && st % g.tiles_k == kt) {
-        float2 part = make_float2(0.f, 0.f);                               // (of a stage apart: fewer additions to the long sum)
+      if (centre && turn == kt) {
+        float2 part[4];                                                    // (of a stage apart: fewer additions to the long sum)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) part[j] = make_float2(0.f, 0.f);
 #pragma unroll
         for (int p = 0; p < PARTS; ++p) {
           const uint8_t* b0 = wg_raw + (base - ptx::smem_u32(wg_raw)) + s * STAGE_BYTES + WG_STAGE_A + p * (WG_BK * BN * 2) + at;
 #pragma unroll 8
           for (int r = 0; r < ROWS; ++r) {
-            const uint32_t u = *reinterpret_cast<const uint32_t*>(b0 + r * 128 + ((unit ^ (uint32_t)(r & 7)) << 4));
-            part = __fadd2_rn(part, make_float2(__uint_as_float(u << 16), __uint_as_float(u & 0xffff0000u)));
+            const uint4 u = *reinterpret_cast<const uint4*>(b0 + r * 128 + ((((uint32_t)unit ^ (uint32_t)(grp * ROWS + r)) & 7) << 4));
+            const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+            for (int j = 0; j < 4; ++j) part[j] = __fadd2_rn(part[j], make_float2(__uint_as_float(w[j] << 16), __uint_as_float(w[j] & 0xffff0000u)));
           }
         }
-        sum = __fadd2_rn(sum, part);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) sum[j] = __fadd2_rn(sum[j], part[j]);
       }
       __syncwarp();
       if (lane == 0) ptx::mbar_arrive(empty(s));
       if (++s == STAGES) { s = 0; ph ^= 1; }
+      if (++turn == g.tiles_k) turn = 0;
       const bool done = ++st == g.stages;
       if (done || i + 1 == end) {
-        if (centre) *reinterpret_cast<float2*>(g.bias + (blockIdx.x + t) * WG_BIAS + grp * BN + 2 * pair) = sum;
-        sum = make_float2(0.f, 0.f);
-        if (done) { st = 0; ++t; }
+        if (centre)
+#pragma unroll
+          for (int j = 0; j < 4; ++j) *reinterpret_cast<float2*>(g.bias + (size_t)(blockIdx.x + t) * WG_BIAS + grp * BN + unit * 8 + 2 * j) = sum[j];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) sum[j] = make_float2(0.f, 0.f);
+        if (done) {
+          st = turn = 0; ++t;
+          tk = t / g.tiles_o; kt = tk % g.tiles_k;
+          centre = tk / g.tiles_k == g.taps / 2;
+        }
       }
     }
   }
@@ -387,46 +414,49 @@ weight_grad_kernel(const __grid_constant__ CUtensorMap tmDy, WgradArgs g) {
 }
 
 // CTAs first .. last of the line's pieces that hold stages of tile t.
-__device__ __forceinline__ void wg_owners(const WgradArgs& g, int ctas, long long t, int& first, int& last) {
-  const long long q = g.line / ctas, rem = g.line % ctas, a = t * g.stages, b = a + g.stages - 1;
-  auto owner = [&](long long i) { return (int)(i < rem * (q + 1) ? i / (q + 1) : rem + (i - rem * (q + 1)) / q); };
+__device__ __forceinline__ void wg_owners(const WgradArgs& g, int ctas, int t, int& first, int& last) {
+  const unsigned q = (unsigned)g.line / ctas, rem = (unsigned)g.line % ctas, a = (unsigned)t * g.stages, b = a + g.stages - 1;
+  auto owner = [&](unsigned i) { return (int)(i < rem * (q + 1) ? i / (q + 1) : rem + (i - rem * (q + 1)) / q); };
   first = owner(a); last = owner(b);
 }
 
-// Tiles that several CTAs worked on: their shares, in the order of the line; a block has 32 columns of a tile, a warp 8 rows x 16 columns at
+// Tiles that several CTAs worked on: their shares, in the order of the line; a block has 16 columns of a tile, a warp 8 rows x 16 columns at
 // a time (128 bytes of a share, 64 bytes of a row of dW).  The last tiles_o blocks (with db): the bias gradient of a column of tiles.
 template <int BN>
 __global__ void __launch_bounds__(256)
 weight_grad_join_kernel(WgradArgs g, int ctas, int tiles) {
-  const int parts = BN / 32;
+  constexpr int PARTS = BN / 16;
   int first, last;
-  if ((int)blockIdx.x >= tiles * parts) {
+  if ((int)blockIdx.x >= tiles * PARTS) {
     __shared__ float s_db[WG_BIAS];
-    const int ot = blockIdx.x - tiles * parts, col = threadIdx.x % BN;
-    float v = 0.f;
+    const int ot = blockIdx.x - tiles * PARTS;
+    float v[4] = {};
     for (int kt = 0; kt < g.tiles_k; ++kt) {
-      const long long t = ((long long)(g.taps / 2) * g.tiles_k + kt) * g.tiles_o + ot;
+      const int t = ((g.taps / 2) * g.tiles_k + kt) * g.tiles_o + ot;
       wg_owners(g, ctas, t, first, last);
 #pragma unroll 4
-      for (int i = first; i <= last; ++i) v += g.bias[(i + t) * WG_BIAS + threadIdx.x];
+      for (int i = first; i <= last; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) v[j] += g.bias[(size_t)(i + t) * WG_BIAS + j * 256 + threadIdx.x];
     }
-    s_db[threadIdx.x] = v;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) s_db[j * 256 + threadIdx.x] = v[j];
     __syncthreads();
-    if (threadIdx.x >= BN || ot * BN + col >= g.O) return;
-    for (int i = 1; i < WG_BIAS / BN; ++i) v += s_db[i * BN + col];
-    g.db[ot * BN + col] = v;
+    const int col = threadIdx.x;
+    if (col >= BN || ot * BN + col >= g.O) return;
+    float sum = 0.f;
+    for (int i = 0; i < WG_BIAS / BN; ++i) sum += s_db[i * BN + col];
+    g.db[ot * BN + col] = sum;
     return;
   }
-  const long long t = blockIdx.x / parts;
+  const int t = blockIdx.x / PARTS;
   wg_owners(g, ctas, t, first, last);
   if (first == last) return;                                             // one CTA had all of it
-  const int o0 = (int)(t % g.tiles_o) * BN, tk = (int)(t / g.tiles_o), tap = tk / g.tiles_k, k0 = (tk - tap * g.tiles_k) * WG_BM;
+  const int o0 = t % g.tiles_o * BN, tk = t / g.tiles_o, tap = tk / g.tiles_k, k0 = (tk - tap * g.tiles_k) * WG_BM;
   const int which0 = wg_begin(g.line, first, ctas) / g.stages == t ? 0 : 1;          // of the first; the others begin in this tile
-  const bool vec = (g.O & 3) == 0 && ((uintptr_t)g.dW & 15) == 0;
 #pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    const int e = j * 256 + threadIdx.x, row = ((e >> 5) & 15) * 8 + (e & 7), quad = (e >> 9) * 4 + ((e >> 3) & 3);
-    const int c = (blockIdx.x % parts) * 32 + quad * 4, k = k0 + row;
+  for (int j = 0; j < 2; ++j) {
+    const int e = j * 256 + threadIdx.x, row = (e >> 5) * 8 + (e & 7), c = (blockIdx.x % PARTS) * 16 + ((e >> 3) & 3) * 4, k = k0 + row;
     if (k >= g.K || o0 + c >= g.O) continue;
     const float* sh = g.share + (c >> 2) * (WG_BM * 4) + row * 4;
     float4 v = *reinterpret_cast<const float4*>(sh + (2ll * first + which0) * (WG_BM * BN));
@@ -436,7 +466,7 @@ weight_grad_join_kernel(WgradArgs g, int ctas, int tiles) {
       v.x += u.x; v.y += u.y; v.z += u.z; v.w += u.w;
     }
     float* out = g.dW + ((long long)tap * g.K + k) * g.O + o0 + c;
-    if (vec) *reinterpret_cast<float4*>(out) = v;
+    if ((g.O & 3) == 0 && ((uintptr_t)g.dW & 15) == 0) *reinterpret_cast<float4*>(out) = v;
     else {
       const float w[4] = {v.x, v.y, v.z, v.w};
       for (int i = 0; i < 4; ++i) if (o0 + c + i < g.O) out[i] = w[i];

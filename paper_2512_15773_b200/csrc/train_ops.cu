@@ -321,11 +321,11 @@ WgradPlan wgrad_plan(WgradArgs& g, bool fp32, int sms) {
 }
 
 template <int BN, int DYK>
-cudaError_t wgrad_launch(const CUtensorMap& map, const WgradArgs& g, int ctas, int device, cudaStream_t s) {
+cudaError_t wgrad_launch(const CUtensorMap& map, const CUtensorMap& qmap, const WgradArgs& g, int ctas, int device, cudaStream_t s) {
   static std::atomic<unsigned long long> done{0};
   const cudaError_t e = allow_smem(weight_grad_kernel<BN, DYK>, wg_smem_bytes(BN, DYK), device, done);
   if (e != cudaSuccess) return e;
-  weight_grad_kernel<BN, DYK><<<ctas, WG_THREADS, wg_smem_bytes(BN, DYK), s>>>(map, g);
+  weight_grad_kernel<BN, DYK><<<ctas, WG_THREADS, wg_smem_bytes(BN, DYK), s>>>(map, qmap, g);
   const int tiles = g.taps * g.tiles_k * g.tiles_o;
   weight_grad_join_kernel<BN><<<(unsigned)(tiles * (BN / 16) + (g.db ? g.tiles_o : 0)), 256, 0, s>>>(g, ctas, tiles);
   return cudaGetLastError();
@@ -504,22 +504,26 @@ int tsdp_weight_grad(int device, int dtype, const tsdp_saved_t* saved_x, const v
   g.share = reinterpret_cast<float*>(d_workspace);
   g.db = d_db;
   g.bias = reinterpret_cast<float*>(reinterpret_cast<char*>(d_workspace) + p.share_bytes);
-  CUtensorMap map{};
+  CUtensorMap map{}, qmap{};
   const bool tma = !fp32 && aligned16(d_dy) && dy_l % 8 == 0 && dy_l >= O && dy_l < (1ll << 38);
-  if (tma) {
-    EncodeTiledFn encode = encode_fn();
-    if (!encode) { fprintf(stderr, "tsdp_weight_grad: cuTensorMapEncodeTiled unavailable\n"); return TSDP_ERR_CUDA; }
-    cuuint64_t gdim[2] = {(cuuint64_t)O, (cuuint64_t)g.M};
-    cuuint64_t gstr[1] = {(cuuint64_t)dy_l * 2};
-    cuuint32_t box[2] = {64, WG_BK}, estr[2] = {1, 1};
-    const CUresult r = encode(&map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(d_dy), gdim, gstr, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
-                              CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
-    if (r != CUDA_SUCCESS) { fprintf(stderr, "tsdp_weight_grad: cuTensorMapEncodeTiled failed with code %d\n", (int)r); return TSDP_ERR_CUDA; }
-  }
-  if (fp32) e = p.bn == 64 ? wgrad_launch<64, WG_DY_FP32>(map, g, p.ctas, device, s) : wgrad_launch<128, WG_DY_FP32>(map, g, p.ctas, device, s);
-  else if (p.bn == 64) e = tma ? wgrad_launch<64, WG_DY_TMA>(map, g, p.ctas, device, s) : wgrad_launch<64, WG_DY_BF16>(map, g, p.ctas, device, s);
-  else if (p.bn == 128) e = tma ? wgrad_launch<128, WG_DY_TMA>(map, g, p.ctas, device, s) : wgrad_launch<128, WG_DY_BF16>(map, g, p.ctas, device, s);
-  else e = tma ? wgrad_launch<256, WG_DY_TMA>(map, g, p.ctas, device, s) : wgrad_launch<256, WG_DY_BF16>(map, g, p.ctas, device, s);
+  g.q_tma = K % 16 == 0 && aligned16(g.x.q);
+  EncodeTiledFn encode = encode_fn();
+  if (!encode) { fprintf(stderr, "tsdp_weight_grad: cuTensorMapEncodeTiled unavailable\n"); return TSDP_ERR_CUDA; }
+  auto tiled = [&](CUtensorMap* m, const void* p2, bool bf16, int cols, long long pitch, int box_cols) {      // rows x cols, boxes of 64 rows
+    cuuint64_t gdim[2] = {(cuuint64_t)cols, (cuuint64_t)g.M}, gstr[1] = {(cuuint64_t)pitch};
+    cuuint32_t box[2] = {(cuuint32_t)box_cols, WG_BK}, estr[2] = {1, 1};
+    return encode(m, bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void*>(p2), gdim, gstr, box, estr,
+                  CU_TENSOR_MAP_INTERLEAVE_NONE, bf16 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_128B,
+                  CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  };
+  CUresult r = CUDA_SUCCESS;
+  if (tma) r = tiled(&map, d_dy, true, O, dy_l * 2, 64);
+  if (r == CUDA_SUCCESS && g.q_tma) r = tiled(&qmap, g.x.q, false, K, K, WG_BM);
+  if (r != CUDA_SUCCESS) { fprintf(stderr, "tsdp_weight_grad: cuTensorMapEncodeTiled failed with code %d\n", (int)r); return TSDP_ERR_CUDA; }
+  if (fp32) e = p.bn == 64 ? wgrad_launch<64, WG_DY_FP32>(map, qmap, g, p.ctas, device, s) : wgrad_launch<128, WG_DY_FP32>(map, qmap, g, p.ctas, device, s);
+  else if (p.bn == 64) e = tma ? wgrad_launch<64, WG_DY_TMA>(map, qmap, g, p.ctas, device, s) : wgrad_launch<64, WG_DY_BF16>(map, qmap, g, p.ctas, device, s);
+  else if (p.bn == 128) e = tma ? wgrad_launch<128, WG_DY_TMA>(map, qmap, g, p.ctas, device, s) : wgrad_launch<128, WG_DY_BF16>(map, qmap, g, p.ctas, device, s);
+  else e = tma ? wgrad_launch<256, WG_DY_TMA>(map, qmap, g, p.ctas, device, s) : wgrad_launch<256, WG_DY_BF16>(map, qmap, g, p.ctas, device, s);
   return e == cudaSuccess ? TSDP_OK : fail_cuda("tsdp_weight_grad", e);
 }
 

@@ -9,14 +9,15 @@
 // A tile of dW is 128 input channels x BN output channels of one tap; the reduction runs over rows (n, l), 64 to a stage.  Both
 // operands come row by row, that is with the reduction index slowest: the tensor core reads them "MN-major" from rows of 128 bytes
 // in the 128-byte swizzle.
-//   warp 0       dy by TMA
+//   warp 0       dy by TMA into a ring of its own
 //   warp 1       one thread issues tcgen05.mma into one of two accumulators in tensor memory
 //   warps 2..5   epilogue: the accumulator to dW, or to this CTA's share of it
 //   warps 6..9   the bias gradient, from the dy tile that is in shared memory anyway; the tiles of one column of dW (other input channels) take
 //                turns at the stages
-//   warps 10..25 x^, eight warps a stage: a thread fetches 32 channels of one row (q and one byte b, four stages ahead), turns them into bf16
-//                and stores them into the swizzled tile; the tap's shift and the zeros outside a sequence are made here.  dy goes the
-//                same way where TMA cannot take it (fp32, unaligned rows).
+//   warps 10..25 x^, eight warps a stage: a thread takes 16 channels of two rows from the ring of q, multiplies them with their steps (fetched
+//                four stages ahead) and stores them into the swizzled tile as bf16; a row outside its sequence has a step of zero.  dy goes
+//                the same way where TMA cannot take it (fp32, unaligned rows).
+//   warp 26      q by TMA, six stages ahead, rows moved by the tap's shift
 // The tensor core cuts a sum of fp32 where fp32 arithmetic rounds it: 4 10^-9 of the result a step, all to one side.  So an accumulator
 // takes WG_CHUNK stages and is then added, rounded, to this CTA's share in the L2, while the other accumulator fills (2048 rows: 5 10^-7 off;
 // 4400 in one go were 1.2 10^-6, 9700 3.7 10^-6).
@@ -29,21 +30,25 @@
 
 namespace tsdp {
 
-constexpr int WG_BM = 128, WG_BK = 64, WG_LOADERS = 256, WG_GROUPS = 2, WG_THREADS = 320 + WG_GROUPS * WG_LOADERS, WG_AHEAD = 2, WG_BIAS = 1024, WG_STAGE_A = WG_BK * WG_BM * 2;
+constexpr int WG_BM = 128, WG_BK = 64, WG_LOADERS = 256, WG_GROUPS = 2, WG_THREADS = 352 + WG_GROUPS * WG_LOADERS, WG_AHEAD = 2, WG_BIAS = 1024;
+constexpr int WG_TILE_A = WG_BK * WG_BM * 2, WG_TILE_Q = WG_BK * WG_BM;
 enum { WG_DY_TMA = 0, WG_DY_BF16 = 1, WG_DY_FP32 = 2 };
 __host__ __device__ constexpr int wg_chunk(int dyk) { return dyk == WG_DY_FP32 ? 8 : 32; }      // (three products a stage in fp32)
 __host__ __device__ constexpr int wg_parts(int dyk) { return dyk == WG_DY_FP32 ? 3 : 1; }
-__host__ __device__ constexpr int wg_stage_bytes(int BN, int dyk) { return WG_STAGE_A + wg_parts(dyk) * WG_BK * BN * 2; }
-__host__ __device__ constexpr int wg_stages(int BN, int dyk) {
-  return 200 * 1024 / wg_stage_bytes(BN, dyk) < 6 ? 200 * 1024 / wg_stage_bytes(BN, dyk) : 6;
+__host__ __device__ constexpr int wg_tile_b(int BN, int dyk) { return wg_parts(dyk) * WG_BK * BN * 2; }
+// stages of the three rings: x^, dy, q
+constexpr int WG_SA = 4, WG_SQ = 6;
+__host__ __device__ constexpr int wg_sb(int BN, int dyk) { return wg_tile_b(BN, dyk) > 32768 ? 2 : (wg_tile_b(BN, dyk) > 24576 ? 3 : 4); }
+__host__ __device__ constexpr int wg_smem_bytes(int BN, int dyk) {
+  return WG_SA * WG_TILE_A + wg_sb(BN, dyk) * wg_tile_b(BN, dyk) + WG_SQ * WG_TILE_Q + 512 + 1024;
 }
-__host__ __device__ constexpr int wg_smem_bytes(int BN, int dyk) { return wg_stages(BN, dyk) * wg_stage_bytes(BN, dyk) + 256 + 1024; }
 
 struct WgradArgs {
   Copy8 x;                                  // [M, K]
   const void* dy; long long ldy;            // [M, O]
   long long M;                              // rows = sequences x L
   int L, K, O, taps;
+  int q_tma;                                // rows of q come in 16-byte pieces
   int tiles_k, tiles_o;                     // tile = (tap, kt, ot), ot fastest
   int stages, line;                         // of a tile; of all tiles (line + grid < 2^31)
   float* dW;                                // [taps, K, O]
@@ -84,21 +89,30 @@ __device__ __forceinline__ void red_add4(float* p, const uint32_t* v) {
 
 template <int BN, int DYK>
 __global__ void __launch_bounds__(WG_THREADS, 1)
-weight_grad_kernel(const __grid_constant__ CUtensorMap tmDy, WgradArgs g) {
-  constexpr int STAGES = wg_stages(BN, DYK), STAGE_BYTES = wg_stage_bytes(BN, DYK), PARTS = wg_parts(DYK), CHUNK = wg_chunk(DYK);
+weight_grad_kernel(const __grid_constant__ CUtensorMap tmDy, const __grid_constant__ CUtensorMap tmQ, WgradArgs g) {
+  constexpr int SA = WG_SA, SB = wg_sb(BN, DYK), SQ = WG_SQ, PARTS = wg_parts(DYK), CHUNK = wg_chunk(DYK), TILE_B = wg_tile_b(BN, DYK);
   constexpr uint32_t TMEM_COLS = 2 * BN < 32 ? 32 : 2 * BN;
   constexpr uint32_t IDESC = umma_idesc_bf16(BN, WG_BM) | (1u << 15) | (1u << 16);      // both operands MN-major
   extern __shared__ uint8_t wg_raw[];
   const uint32_t base = (ptx::smem_u32(wg_raw) + 1023u) & ~1023u;
-  const uint32_t bar0 = base + STAGES * STAGE_BYTES;
-  auto full = [&](int s) { return bar0 + 8u * s; };
-  auto empty = [&](int s) { return bar0 + 8u * (STAGES + s); };
-  auto tfull = [&](int b) { return bar0 + 8u * (2 * STAGES + b); };
-  auto tempty = [&](int b) { return bar0 + 8u * (2 * STAGES + 2 + b); };
-  const uint32_t slot = bar0 + 8u * (2 * STAGES + 4);
+  uint8_t* const raw = wg_raw + (base - ptx::smem_u32(wg_raw));
+  constexpr uint32_t OFF_B = SA * WG_TILE_A, OFF_Q = OFF_B + SB * TILE_B, OFF_BAR = OFF_Q + SQ * WG_TILE_Q;
+  const uint32_t bar0 = base + OFF_BAR;
+  auto full_a = [&](int s) { return bar0 + 8u * s; };
+  auto empty_a = [&](int s) { return bar0 + 8u * (SA + s); };
+  auto full_b = [&](int s) { return bar0 + 8u * (2 * SA + s); };
+  auto empty_b = [&](int s) { return bar0 + 8u * (2 * SA + SB + s); };
+  auto full_q = [&](int s) { return bar0 + 8u * (2 * SA + 2 * SB + s); };
+  auto empty_q = [&](int s) { return bar0 + 8u * (2 * SA + 2 * SB + SQ + s); };
+  auto tfull = [&](int b) { return bar0 + 8u * (2 * SA + 2 * SB + 2 * SQ + b); };
+  auto tempty = [&](int b) { return bar0 + 8u * (2 * SA + 2 * SB + 2 * SQ + 2 + b); };
+  const uint32_t slot = bar0 + 8u * (2 * SA + 2 * SB + 2 * SQ + 4);
+  static_assert(8 * (2 * SA + 2 * SB + 2 * SQ + 4) + 4 <= 512, "the barriers have 512 bytes");
   const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
   if (threadIdx.x == 0) {
-    for (int s = 0; s < STAGES; ++s) { ptx::mbar_init(full(s), WG_LOADERS / 32 + (DYK == WG_DY_TMA ? 1 : 0)); ptx::mbar_init(empty(s), g.db ? 5 : 1); }
+    for (int s = 0; s < SA; ++s) { ptx::mbar_init(full_a(s), WG_LOADERS / 32); ptx::mbar_init(empty_a(s), 1); }
+    for (int s = 0; s < SB; ++s) { ptx::mbar_init(full_b(s), DYK == WG_DY_TMA ? 1 : WG_LOADERS / 32); ptx::mbar_init(empty_b(s), g.db ? 5 : 1); }
+    for (int s = 0; s < SQ; ++s) { ptx::mbar_init(full_q(s), 1); ptx::mbar_init(empty_q(s), WG_LOADERS / 32); }
     for (int b = 0; b < 2; ++b) { ptx::mbar_init(tfull(b), 1); ptx::mbar_init(tempty(b), 4); }
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -107,7 +121,7 @@ weight_grad_kernel(const __grid_constant__ CUtensorMap tmDy, WgradArgs g) {
   ptx::tc_fence_before();
   __syncthreads();
   ptx::tc_fence_after();
-  const uint32_t tmem = *reinterpret_cast<volatile uint32_t*>(wg_raw + (slot - ptx::smem_u32(wg_raw)));
+  const uint32_t tmem = *reinterpret_cast<volatile uint32_t*>(raw + (slot - base));
 
   const int begin = wg_begin(g.line, blockIdx.x, gridDim.x), end = wg_begin(g.line, blockIdx.x + 1, gridDim.x);
   const int t_first = begin / g.stages;
@@ -118,36 +132,49 @@ weight_grad_kernel(const __grid_constant__ CUtensorMap tmDy, WgradArgs g) {
       int t = t_first, st = begin - t * g.stages, s = 0;
       uint32_t ph = 1;
       for (int i = begin; i < end; ++i) {
-        if (!ptx::mbar_wait_thread(empty(s), ph)) { ok = false; break; }
-        const uint32_t b0 = base + s * STAGE_BYTES + WG_STAGE_A;
+        if (!ptx::mbar_wait_thread(empty_b(s), ph)) { ok = false; break; }
         const int o0 = t % g.tiles_o * BN;
-        ptx::mbar_expect_tx(full(s), BN * WG_BK * 2);
+        ptx::mbar_expect_tx(full_b(s), BN * WG_BK * 2);
 #pragma unroll
-        for (int j = 0; j < BN / 64; ++j) ptx::tma_load_2d(b0 + j * WG_BK * 128, &tmDy, o0 + 64 * j, st * WG_BK, full(s));
-        if (++s == STAGES) { s = 0; ph ^= 1; }
+        for (int j = 0; j < BN / 64; ++j) ptx::tma_load_2d(base + OFF_B + s * TILE_B + j * WG_BK * 128, &tmDy, o0 + 64 * j, st * WG_BK, full_b(s));
+        if (++s == SB) { s = 0; ph ^= 1; }
+        if (++st == g.stages) { st = 0; ++t; }
+      }
+    }
+  } else if (warp == 26) {
+    if (g.q_tma && ptx::elect_one()) {
+      int t = t_first, st = begin - t * g.stages, s = 0;
+      uint32_t ph = 1;
+      for (int i = begin; i < end; ++i) {
+        if (!ptx::mbar_wait_thread(empty_q(s), ph)) { ok = false; break; }
+        const int tk = t / g.tiles_o, tap = tk / g.tiles_k;
+        ptx::mbar_expect_tx(full_q(s), WG_TILE_Q);
+        ptx::tma_load_2d(base + OFF_Q + s * WG_TILE_Q, &tmQ, (tk - tap * g.tiles_k) * WG_BM, st * WG_BK + tap - g.taps / 2, full_q(s));
+        if (++s == SQ) { s = 0; ph ^= 1; }
         if (++st == g.stages) { st = 0; ++t; }
       }
     }
   } else if (warp == 1) {
     if (ptx::elect_one()) {
-      int t = t_first, st = begin - t * g.stages, s = 0, buf = 0, chunk = 0;
-      uint32_t ph = 0, tph = 1;
+      int t = t_first, st = begin - t * g.stages, sa = 0, sb = 0, buf = 0, chunk = 0;
+      uint32_t pa = 0, pb = 0, tph = 1;
       bool fresh = true;
       for (int i = begin; i < end; ++i) {
         if (fresh && !ptx::mbar_wait_thread(tempty(buf), tph)) { ok = false; break; }
-        if (!ptx::mbar_wait_thread(full(s), ph)) { ok = false; break; }
+        if (!ptx::mbar_wait_thread(full_b(sb), pb) || !ptx::mbar_wait_thread(full_a(sa), pa)) { ok = false; break; }
         ptx::tc_fence_after();
-        const uint32_t a0 = base + s * STAGE_BYTES, d = tmem + buf * BN;
+        const uint32_t a0 = base + sa * WG_TILE_A, b0 = base + OFF_B + sb * TILE_B, d = tmem + buf * BN;
 #pragma unroll
         for (int p = 0; p < PARTS; ++p)
 #pragma unroll
           for (int k = 0; k < WG_BK / 16; ++k)      // 16 rows = 2048 bytes of every column of 64 channels
-            ptx::tc_mma_bf16(d, umma_desc_mn_sw128(a0 + k * 2048, WG_BK * 128),
-                             umma_desc_mn_sw128(a0 + WG_STAGE_A + p * (WG_BK * BN * 2) + k * 2048, WG_BK * 128), IDESC,
+            ptx::tc_mma_bf16(d, umma_desc_mn_sw128(a0 + k * 2048, WG_BK * 128), umma_desc_mn_sw128(b0 + p * (WG_BK * BN * 2) + k * 2048, WG_BK * 128), IDESC,
                              fresh && p == 0 && k == 0 ? 0u : 1u);
         fresh = false;
-        ptx::tc_commit(empty(s));
-        if (++s == STAGES) { s = 0; ph ^= 1; }
+        ptx::tc_commit(empty_a(sa));
+        ptx::tc_commit(empty_b(sb));
+        if (++sa == SA) { sa = 0; pa ^= 1; }
+        if (++sb == SB) { sb = 0; pb ^= 1; }
         const bool done = ++st == g.stages;
         if (++chunk == CHUNK || done || i + 1 == end) {
           ptx::tc_commit(tfull(buf));
@@ -158,112 +185,117 @@ weight_grad_kernel(const __grid_constant__ CUtensorMap tmDy, WgradArgs g) {
       }
     }
   } else if (warp >= 10) {
-    // x^ (and dy where it does not come by TMA): row of the stage, block of 32 channels
-    const int group = (warp - 10) / (WG_LOADERS / 32), tid = (threadIdx.x - 320) % WG_LOADERS, r = tid >> 2, bq = tid & 3, nb = copy_blocks(g.K);
-    const bool wide = (g.K & 15) == 0 && ((uintptr_t)g.x.q & 15) == 0;
-    struct Fetch { uint32_t w[8]; uint32_t b; } f[WG_AHEAD];
-    // where the next fetch reads: tile t, stage st, position l of this thread's row in its sequence
-    int t = (begin + group) / g.stages, st = begin + group - t * g.stages, l = 0, shift = 0, c = 0;
-    long long m = 0;
-    const int l_step = WG_GROUPS * WG_BK % g.L;
-    const signed char* qp = nullptr;
+    // x^ (and dy where it does not come by TMA): 16 channels (piece p) of rows r and r + 32 of the stage
+    const int group = (warp - 10) / (WG_LOADERS / 32), tid = (threadIdx.x - 320) % WG_LOADERS, r = tid >> 3, p = tid & 7, nb = copy_blocks(g.K);
+    // where the next steps are: tile t, stage st, positions of this thread's rows in their sequences
+    int t = (begin + group) / g.stages, st = begin + group - t * g.stages, l0 = 0, l1 = 0, shift = 0, c = 0;
+    int left = 0;                                             // rows from this thread's first to the end
     const unsigned char* bp = nullptr;
+    const int l_step = WG_GROUPS * WG_BK % g.L;
     auto place = [&] {
       const int tk = t / g.tiles_o, tap = tk / g.tiles_k;
       shift = tap - g.taps / 2;
-      c = (tk - tap * g.tiles_k) * WG_BM + bq * 32;
-      m = (long long)st * WG_BK + r;
-      l = (int)(m % g.L);
-      qp = g.x.q + (m + shift) * g.K + c;
+      c = (tk - tap * g.tiles_k) * WG_BM + p * 16;
+      const long long m = (long long)st * WG_BK + r;
+      left = (int)(g.M - m);
+      l0 = (int)(m % g.L) + shift;
+      l1 = (int)((m + 32) % g.L) + shift;
       bp = g.x.b + (m + shift) * nb + (c >> 5);
     };
-    auto fetch = [&](Fetch& o) {
-      const bool in = m < g.M && (unsigned)(l + shift) < (unsigned)g.L && c < g.K;
-      o.b = in ? (uint32_t)*bp : 0u;
-#pragma unroll
-      for (int j = 0; j < 8; ++j) o.w[j] = 0u;
-      if (in) {
-        if (wide) {
-          const uint4 u = *reinterpret_cast<const uint4*>(qp);
-          o.w[0] = u.x; o.w[1] = u.y; o.w[2] = u.z; o.w[3] = u.w;
-          if (c + 16 < g.K) {
-            const uint4 v = *reinterpret_cast<const uint4*>(qp + 16);
-            o.w[4] = v.x; o.w[5] = v.y; o.w[6] = v.z; o.w[7] = v.w;
-          }
-        } else {
-#pragma unroll
-          for (int j = 0; j < 32; ++j)
-            if (c + j < g.K) o.w[j >> 2] |= (uint32_t)(unsigned char)qp[j] << (8 * (j & 3));
-        }
+    auto steps_of = [&](uint32_t (&o)[2]) {
+      o[0] = o[1] = 0u;
+      if (c < g.K) {
+        if (left > 0 && (unsigned)l0 < (unsigned)g.L) o[0] = bp[0];
+        if (left > 32 && (unsigned)l1 < (unsigned)g.L) o[1] = bp[32 * nb];
       }
       st += WG_GROUPS;
       if (st >= g.stages) {
         while (st >= g.stages) { st -= g.stages; ++t; }
         place();
       } else {
-        m += WG_GROUPS * WG_BK;
-        qp += (long long)WG_GROUPS * WG_BK * g.K;
-        bp += (long long)WG_GROUPS * WG_BK * nb;
-        l += l_step;
-        if (l >= g.L) l -= g.L;
+        left -= WG_GROUPS * WG_BK;
+        bp += WG_GROUPS * WG_BK * (long long)nb;
+        l0 += l_step; l1 += l_step;
+        if (l0 - shift >= g.L) l0 -= g.L;
+        if (l1 - shift >= g.L) l1 -= g.L;
       }
     };
     place();
-    // rows of 128 bytes per 64 channels; the two halves of a row take their 16-byte pieces in another order, so that the eight threads of
-    // a store phase (two rows, four blocks) touch eight different pieces
-    const uint32_t half = (uint32_t)(bq >> 1), row_off = half * (WG_BK * 128) + (uint32_t)r * 128;
-    const uint32_t ch0 = (uint32_t)(bq & 1) * 4, rx = (uint32_t)(r & 7);
-    int s = group;
-    uint32_t ph = 1;
-    [[maybe_unused]] int t_cur = t;                           // the stage that is stored, for a dy that is read here
-    [[maybe_unused]] int st_cur = st;
+    // the stage that is worked on, where its bytes do not come by TMA
+    int t_cur = t, st_cur = st;
+    // rows of 128 bytes per 64 channels; the pieces of the two halves of a row store theirs in another order, so that the eight threads
+    // of a store phase (one row) touch eight different 16-byte units
+    const uint32_t half = (uint32_t)(p >> 2), rx = (uint32_t)(r & 7), row_off = half * (WG_BK * 128) + (uint32_t)r * 128;
+    const uint32_t u0 = (((uint32_t)(p & 3) * 2 + half) ^ rx) << 4, u1 = (((uint32_t)(p & 3) * 2 + (half ^ 1)) ^ rx) << 4;
+    int sa = group, sb = group % SB, sq = group;
+    uint32_t pa = 1, pb = group >= SB ? 0 : 1, pq = 0;
+    uint32_t ahead[WG_AHEAD][2];
 #pragma unroll
     for (int d = 0; d < WG_AHEAD; ++d)
-      if (begin + group + d * WG_GROUPS < end) fetch(f[d]);
+      if (begin + group + d * WG_GROUPS < end) steps_of(ahead[d]);
     for (int i0 = begin + group; i0 < end && ok; i0 += WG_AHEAD * WG_GROUPS)
 #pragma unroll
     for (int d = 0; d < WG_AHEAD; ++d) {
       const int i = i0 + d * WG_GROUPS;
       if (i >= end || !ok) continue;
-      const Fetch cur = f[d];
-      ok = ptx::mbar_wait_warp(empty(s), ph);
-      if (!ok) continue;
-      if (i + WG_AHEAD * WG_GROUPS < end) fetch(f[d]);
-      const uint32_t a0 = base + s * STAGE_BYTES;
-      const uint32_t sb = cur.b == 255u ? 0x7fc0u : cur.b << 7, sb2 = sb | sb << 16;
-      const __nv_bfloat162 stp = *reinterpret_cast<const __nv_bfloat162*>(&sb2);
+      const uint32_t cur[2] = {ahead[d][0], ahead[d][1]};
+      if (i + WG_AHEAD * WG_GROUPS < end) steps_of(ahead[d]);
+      uint4 w[2];
+      if (g.q_tma) {
+        ok = ptx::mbar_wait_warp(full_q(sq), pq);
+        if (!ok) continue;
+        const uint8_t* q = raw + OFF_Q + sq * WG_TILE_Q + r * WG_BM + p * 16;
+        w[0] = *reinterpret_cast<const uint4*>(q);
+        w[1] = *reinterpret_cast<const uint4*>(q + 32 * WG_BM);
+      } else {
+        const int tk = t_cur / g.tiles_o, tap = tk / g.tiles_k, ch = (tk - tap * g.tiles_k) * WG_BM + p * 16;
 #pragma unroll
-      for (int jj = 0; jj < 4; ++jj) {
-        const uint32_t j = (uint32_t)jj ^ (2 * half);
-        // (a select between two words: an index known at run time would move the array to local memory)
-        const uint32_t w0 = half ? cur.w[2 * (jj ^ 2)] : cur.w[2 * jj], w1 = half ? cur.w[2 * (jj ^ 2) + 1] : cur.w[2 * jj + 1];
-        st_shared16(a0 + row_off + (((ch0 + j) ^ rx) << 4), wg_pair(w0, 0x4140, stp), wg_pair(w0, 0x4342, stp), wg_pair(w1, 0x4140, stp),
-                    wg_pair(w1, 0x4342, stp));
+        for (int h = 0; h < 2; ++h) {
+          const long long ms = (long long)st_cur * WG_BK + r + 32 * h + tap - g.taps / 2;
+          uint32_t v[4] = {0u, 0u, 0u, 0u};
+          if (ms >= 0 && ms < g.M)
+#pragma unroll
+            for (int j = 0; j < 16; ++j)
+              if (ch + j < g.K) v[j >> 2] |= (uint32_t)(unsigned char)g.x.q[ms * g.K + ch + j] << (8 * (j & 3));
+          w[h] = make_uint4(v[0], v[1], v[2], v[3]);
+        }
+      }
+      ok = ptx::mbar_wait_warp(empty_a(sa), pa);
+      if (!ok) continue;
+      const uint32_t a0 = base + sa * WG_TILE_A + row_off;
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const uint32_t step = cur[h] == 255u ? 0x7fc07fc0u : cur[h] * 0x00800080u;      // the byte as the exponent of two bf16 values
+        const __nv_bfloat162 k = *reinterpret_cast<const __nv_bfloat162*>(&step);
+        const uint32_t x0 = half ? w[h].z : w[h].x, x1 = half ? w[h].w : w[h].y, y0 = half ? w[h].x : w[h].z, y1 = half ? w[h].y : w[h].w;
+        st_shared16(a0 + h * (32 * 128) + u0, wg_pair(x0, 0x4140, k), wg_pair(x0, 0x4342, k), wg_pair(x1, 0x4140, k), wg_pair(x1, 0x4342, k));
+        st_shared16(a0 + h * (32 * 128) + u1, wg_pair(y0, 0x4140, k), wg_pair(y0, 0x4342, k), wg_pair(y1, 0x4140, k), wg_pair(y1, 0x4342, k));
       }
       if constexpr (DYK != WG_DY_TMA) {
         // eight output channels at a time
-        const long long m_cur = (long long)st_cur * WG_BK + r;
+        ok = ptx::mbar_wait_warp(empty_b(sb), pb);
+        if (!ok) continue;
+        const int rd = tid >> 2, bq = tid & 3;
+        const long long m_cur = (long long)st_cur * WG_BK + rd;
         const int o0 = t_cur % g.tiles_o * BN;
-        st_cur += WG_GROUPS;
-        while (st_cur >= g.stages) { st_cur -= g.stages; ++t_cur; }
         const bool row_in = m_cur < g.M;
-        const uint32_t b0 = a0 + WG_STAGE_A;
+        const uint32_t b0 = base + OFF_B + sb * TILE_B;
         for (int u = bq; u < BN / 8; u += 4) {
           const int o = o0 + 8 * u;
           uint32_t part[3][4];
           if constexpr (DYK == WG_DY_BF16) {
-            const unsigned short* p = reinterpret_cast<const unsigned short*>(g.dy) + m_cur * g.ldy + o;
+            const unsigned short* src = reinterpret_cast<const unsigned short*>(g.dy) + m_cur * g.ldy + o;
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-              const uint32_t x0 = row_in && o + 2 * j < g.O ? p[2 * j] : 0u, x1 = row_in && o + 2 * j + 1 < g.O ? p[2 * j + 1] : 0u;
+              const uint32_t x0 = row_in && o + 2 * j < g.O ? src[2 * j] : 0u, x1 = row_in && o + 2 * j + 1 < g.O ? src[2 * j + 1] : 0u;
               part[0][j] = x0 | x1 << 16;
             }
           } else {
-            const float* p = reinterpret_cast<const float*>(g.dy) + m_cur * g.ldy + o;
+            const float* src = reinterpret_cast<const float*>(g.dy) + m_cur * g.ldy + o;
             uint32_t e[3][8];
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-              const float v = row_in && o + j < g.O ? p[j] : 0.f;
+              const float v = row_in && o + j < g.O ? src[j] : 0.f;
               const uint32_t bits = __float_as_uint(v), h0 = bits & 0xffff0000u;
               const float r1 = v - __uint_as_float(h0);
               const uint32_t h1 = __float_as_uint(r1) & 0xffff0000u;
@@ -280,15 +312,24 @@ weight_grad_kernel(const __grid_constant__ CUtensorMap tmDy, WgradArgs g) {
           }
 #pragma unroll
           for (int k = 0; k < PARTS; ++k)
-            st_shared16(b0 + k * (WG_BK * BN * 2) + (u >> 3) * (WG_BK * 128) + r * 128 + ((((uint32_t)u & 7) ^ rx) << 4), part[k][0], part[k][1],
-                        part[k][2], part[k][3]);
+            st_shared16(b0 + k * (WG_BK * BN * 2) + (u >> 3) * (WG_BK * 128) + rd * 128 + ((((uint32_t)u & 7) ^ (uint32_t)(rd & 7)) << 4), part[k][0],
+                        part[k][1], part[k][2], part[k][3]);
         }
+      }
+      if (DYK != WG_DY_TMA || !g.q_tma) {
+        st_cur += WG_GROUPS;
+        while (st_cur >= g.stages) { st_cur -= g.stages; ++t_cur; }
       }
       ptx::fence_async_smem();
       __syncwarp();
-      if (lane == 0) ptx::mbar_arrive(full(s));
-      s += WG_GROUPS;
-      if (s >= STAGES) { s -= STAGES; ph ^= 1; }
+      if (lane == 0) {
+        ptx::mbar_arrive(full_a(sa));
+        if (DYK != WG_DY_TMA) ptx::mbar_arrive(full_b(sb));
+        if (g.q_tma) ptx::mbar_arrive(empty_q(sq));
+      }
+      sa += WG_GROUPS; if (sa >= SA) { sa -= SA; pa ^= 1; }
+      sb += WG_GROUPS; if (sb >= SB) { sb -= SB; pb ^= 1; }
+      sq += WG_GROUPS; if (sq >= SQ) { sq -= SQ; pq ^= 1; }
     }
   } else if (warp < 6) {
     const int quad = warp & 3, row = quad * 32 + lane;                   // tensor-memory lane quadrant of this warp; input channel of the tile
@@ -364,7 +405,7 @@ weight_grad_kernel(const __grid_constant__ CUtensorMap tmDy, WgradArgs g) {
     int tk = t / g.tiles_o, kt = tk % g.tiles_k, turn = st % g.tiles_k;
     bool centre = tk / g.tiles_k == g.taps / 2;
     for (int i = begin; i < end; ++i) {
-      ok = ptx::mbar_wait_warp(full(s), ph);
+      ok = ptx::mbar_wait_warp(full_b(s), ph);
       if (!ok) break;
       if (centre && turn == kt) {
         float2 part[4];                                                    // (of a stage apart: fewer additions to the long sum)
@@ -372,7 +413,7 @@ weight_grad_kernel(const __grid_constant__ CUtensorMap tmDy, WgradArgs g) {
         for (int j = 0; j < 4; ++j) part[j] = make_float2(0.f, 0.f);
 #pragma unroll
         for (int p = 0; p < PARTS; ++p) {
-          const uint8_t* b0 = wg_raw + (base - ptx::smem_u32(wg_raw)) + s * STAGE_BYTES + WG_STAGE_A + p * (WG_BK * BN * 2) + at;
+          const uint8_t* b0 = raw + OFF_B + s * TILE_B + p * (WG_BK * BN * 2) + at;
 #pragma unroll 8
           for (int r = 0; r < ROWS; ++r) {
             const uint4 u = *reinterpret_cast<const uint4*>(b0 + r * 128 + ((((uint32_t)unit ^ (uint32_t)(grp * ROWS + r)) & 7) << 4));
@@ -385,8 +426,8 @@ weight_grad_kernel(const __grid_constant__ CUtensorMap tmDy, WgradArgs g) {
         for (int j = 0; j < 4; ++j) sum[j] = __fadd2_rn(sum[j], part[j]);
       }
       __syncwarp();
-      if (lane == 0) ptx::mbar_arrive(empty(s));
-      if (++s == STAGES) { s = 0; ph ^= 1; }
+      if (lane == 0) ptx::mbar_arrive(empty_b(s));
+      if (++s == SB) { s = 0; ph ^= 1; }
       if (++turn == g.tiles_k) turn = 0;
       const bool done = ++st == g.stages;
       if (done || i + 1 == end) {

@@ -90,8 +90,8 @@ def group_norm_grad(dy, x, gamma, beta, groups, mean, rstd, name="mish", film=No
 # ------------------------------------------------------------------------------------------- weight gradient
 def weight_grad(x, dy, taps, length):
     """(dW [taps, K, O], db [O]) of x [rows, K], dy [rows, O]; sequences of `length` rows, zeros beyond their ends."""
-    K, out = x.shape[1], dy.shape[1]
-    xs, ds = x.reshape(-1, length, K), dy.reshape(-1, length, out)
+    K = x.shape[1]
+    xs = x.reshape(-1, length, K)
     side = np.zeros((xs.shape[0], taps // 2, K))
     xp = np.concatenate([side, xs, side], axis=1)
-    return np.stack([np.einsum("nlk,nlo->ko", xp[:, j:j + length], ds) for j in range(taps)]), dy.sum(0)
+    return np.stack([xp[:, j:j + length].reshape(-1, K).T @ dy for j in range(taps)]), dy.sum(0)

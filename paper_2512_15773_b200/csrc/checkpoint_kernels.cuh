@@ -87,6 +87,7 @@ constexpr int COPY_THREADS = 256;
 template <typename T>
 __global__ void __launch_bounds__(COPY_THREADS)
 checkpoint_pack_kernel(Rows x, Copy8 out, int N, int L, int C) {
+  pdl_wait();
   const int units = 4 * copy_blocks(C), per = min(units, COPY_THREADS);      // threads on a row
   const int lanes = COPY_THREADS / per, lane = threadIdx.x / per;
   const long long rows = (long long)N * L;
@@ -120,6 +121,7 @@ checkpoint_pack_kernel(Rows x, Copy8 out, int N, int L, int C) {
 template <typename T>
 __global__ void __launch_bounds__(COPY_THREADS)
 checkpoint_pack_any_kernel(Rows x, Copy8 out, int N, int L, int C) {
+  pdl_wait();
   const int nb = copy_blocks(C), lane = threadIdx.x & 31;
   const long long blocks = (long long)N * L * nb;
   for (long long i = (long long)blockIdx.x * (COPY_THREADS / 32) + (threadIdx.x >> 5); i < blocks; i += (long long)gridDim.x * (COPY_THREADS / 32)) {
@@ -136,6 +138,7 @@ checkpoint_pack_any_kernel(Rows x, Copy8 out, int N, int L, int C) {
 template <typename T>
 __global__ void __launch_bounds__(COPY_THREADS)
 checkpoint_unpack_kernel(Copy8 in, Rows x, int N, int L, int C) {
+  pdl_wait();
   const int units = C >> 3, per = min(units, COPY_THREADS);
   const int lanes = COPY_THREADS / per, lane = threadIdx.x / per;
   const long long rows = (long long)N * L;
@@ -158,6 +161,7 @@ checkpoint_unpack_kernel(Copy8 in, Rows x, int N, int L, int C) {
 template <typename T>
 __global__ void __launch_bounds__(COPY_THREADS)
 checkpoint_unpack_any_kernel(Copy8 in, Rows x, int N, int L, int C) {
+  pdl_wait();
   const int nb = copy_blocks(C), lane = threadIdx.x & 31;
   const long long blocks = (long long)N * L * nb;
   for (long long i = (long long)blockIdx.x * (COPY_THREADS / 32) + (threadIdx.x >> 5); i < blocks; i += (long long)gridDim.x * (COPY_THREADS / 32)) {

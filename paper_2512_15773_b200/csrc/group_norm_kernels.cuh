@@ -107,6 +107,7 @@ template <typename T, int V>
 __global__ void __launch_bounds__(GN_THREADS)
 group_norm_kernel(NormArgs g) {
   extern __shared__ __align__(16) float gn_smem[];
+  pdl_wait();
   const int cg = g.C / g.groups;
   float* s_mean = gn_smem;                                  // [lanes][tile channels]
   float* s_m2 = s_mean + GN_THREADS * V;                    // the same
@@ -317,6 +318,7 @@ template <typename T, int V, bool COPY>
 __global__ void __launch_bounds__(GN_THREADS)
 group_norm_grad_kernel(NormArgs g) {
   extern __shared__ __align__(16) float gn_smem[];
+  pdl_wait();
   const int cg = g.C / g.groups;
   float* s_lane = gn_smem;                                  // [4][lanes][tile channels]: sums of a lane
   float* s_sum = s_lane + 4 * GN_THREADS * V;               // [4][width]: of the CTA
@@ -420,13 +422,15 @@ group_norm_grad_kernel(NormArgs g) {
 }
 
 // dbeta, dgamma: the shares of the splits, in their order.
-constexpr int GN_JOIN_CH = 32, GN_JOIN_LANES = 8;
+constexpr int GN_JOIN_CH = 32, GN_JOIN_LANES = 32;
 __global__ void __launch_bounds__(GN_JOIN_CH * GN_JOIN_LANES)
 group_norm_join_kernel(const float* part, int splits, int C, float* dgamma, float* dbeta) {
+  pdl_wait();
   __shared__ float s[GN_JOIN_LANES][GN_JOIN_CH];
-  const int c = blockIdx.x * GN_JOIN_CH + (threadIdx.x % GN_JOIN_CH), k = blockIdx.y, lane = threadIdx.x / GN_JOIN_CH;
+  const int c = (blockIdx.x >> 1) * GN_JOIN_CH + (threadIdx.x % GN_JOIN_CH), k = blockIdx.x & 1, lane = threadIdx.x / GN_JOIN_CH;
   float v = 0.f;
   if (c < C)
+#pragma unroll 8
     for (int i = lane; i < splits; i += GN_JOIN_LANES) v += part[((long long)i * 2 + k) * C + c];
   s[lane][threadIdx.x % GN_JOIN_CH] = v;
   __syncthreads();

@@ -140,6 +140,7 @@ group_norm_slab_kernel(NormArgs g) {
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
   }
   __syncthreads();
+  pdl_wait();
   if (threadIdx.x < 32)
     for (int s = 0; s < GN_RING; ++s)
       if (split + s * g.splits < g.N) issue(split + s * g.splits, s);
@@ -266,6 +267,7 @@ group_norm_slab_grad_kernel(NormArgs g) {
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
   }
   __syncthreads();
+  pdl_wait();
   if (threadIdx.x < 32)
     for (int s = 0; s < GN_RING; ++s)
       if (split + s * g.splits < g.N) issue(split + s * g.splits, s);

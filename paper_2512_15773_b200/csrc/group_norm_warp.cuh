@@ -15,6 +15,7 @@ group_norm_warp_kernel(NormArgs g) {
   constexpr int V = 16 / sizeof(T), P = V / 2;
   const int gw = blockIdx.x * (GN_WARP_THREADS / 32) + (threadIdx.x >> 5), wl = threadIdx.x & 31;
   const int grp = gw % g.groups, split = gw / g.groups;
+  pdl_wait();
   if (split >= g.splits) return;
   const int cg = g.C / g.groups, gcols = cg / V, R = 32 / gcols;             // lanes on a position, positions at a time
   const int lr = wl / gcols, c = grp * cg + (wl - lr * gcols) * V;
@@ -124,6 +125,8 @@ group_norm_warp_grad_kernel(NormArgs g) {
   extern __shared__ __align__(16) uint8_t gw_raw[];
   const int gw = blockIdx.x * (GN_WARP_THREADS / 32) + (threadIdx.x >> 5), wl = threadIdx.x & 31;
   const int grp = gw % g.groups, split = gw / g.groups;
+  pdl_trigger(true);                            // the join of the shares: its blocks wait beside this grid, which runs at once as a whole
+  pdl_wait();
   if (split >= g.splits) return;
   const int cg = g.C / g.groups, gcols = cg / V, R = 32 / gcols, nb = copy_blocks(g.C), gb = cg / 32;
   const int lr = wl / gcols, cc = (wl - lr * gcols) * V, c = grp * cg + cc;

@@ -55,6 +55,25 @@ template <typename F> cudaError_t allow_smem(F kern, int bytes, int device, std:
   return e;
 }
 
+// Every kernel here may be launched while its predecessor in the stream still drains (programmatic dependent launch): it begins with
+// griddepcontrol.wait.
+template <typename F, typename... A>
+cudaError_t launch(F kern, unsigned grid, int threads, int cluster, int smem, cudaStream_t s, const A&... args) {
+  cudaLaunchConfig_t cfg{};
+  cudaLaunchAttribute at[2];
+  cfg.gridDim = dim3(grid);
+  cfg.blockDim = dim3((unsigned)threads);
+  cfg.dynamicSmemBytes = (size_t)smem;
+  cfg.stream = s;
+  at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at[0].val.programmaticStreamSerializationAllowed = 1;
+  at[1].id = cudaLaunchAttributeClusterDimension;
+  at[1].val.clusterDim.x = (unsigned)cluster; at[1].val.clusterDim.y = 1; at[1].val.clusterDim.z = 1;
+  cfg.attrs = at;
+  cfg.numAttrs = cluster > 1 ? 2 : 1;
+  return cudaLaunchKernelEx(&cfg, kern, args...);
+}
+
 bool aligned16(const void* p) { return ((uintptr_t)p & 15) == 0; }
 size_t esize(int dtype) { return dtype == TSDP_TYPE_BF16 ? 2 : 4; }
 bool dtype_ok(int dtype) { return dtype == TSDP_TYPE_FP32 || dtype == TSDP_TYPE_BF16; }
@@ -86,12 +105,12 @@ cudaError_t pack(const Rows& x, Copy8 out, int N, int L, int C, int sms, cudaStr
   if (wide) {
     const int lanes = COPY_THREADS / min(4 * copy_blocks(C), COPY_THREADS);
     const long long blocks = min((rows + lanes - 1) / lanes, (long long)sms * 32);
-    checkpoint_pack_kernel<T><<<(unsigned)blocks, COPY_THREADS, 0, s>>>(x, out, N, L, C);
-  } else {
-    const long long blocks = min((rows * copy_blocks(C) + 7) / 8, (long long)sms * 64);
-    checkpoint_pack_any_kernel<T><<<(unsigned)blocks, COPY_THREADS, 0, s>>>(x, out, N, L, C);
+    return launch(checkpoint_pack_kernel<T>, (unsigned)blocks, COPY_THREADS, 1, 0, s, x, out, N, L, C);
   }
-  return cudaGetLastError();
+  {
+    const long long blocks = min((rows * copy_blocks(C) + 7) / 8, (long long)sms * 64);
+    return launch(checkpoint_pack_any_kernel<T>, (unsigned)blocks, COPY_THREADS, 1, 0, s, x, out, N, L, C);
+  }
 }
 
 template <typename T>
@@ -101,12 +120,12 @@ cudaError_t unpack(Copy8 in, const Rows& x, int N, int L, int C, int sms, cudaSt
   if (wide) {
     const int lanes = COPY_THREADS / min(C / 8, COPY_THREADS);
     const long long blocks = min((rows + lanes - 1) / lanes, (long long)sms * 32);
-    checkpoint_unpack_kernel<T><<<(unsigned)blocks, COPY_THREADS, 0, s>>>(in, x, N, L, C);
-  } else {
-    const long long blocks = min((rows * copy_blocks(C) + 7) / 8, (long long)sms * 64);
-    checkpoint_unpack_any_kernel<T><<<(unsigned)blocks, COPY_THREADS, 0, s>>>(in, x, N, L, C);
+    return launch(checkpoint_unpack_kernel<T>, (unsigned)blocks, COPY_THREADS, 1, 0, s, in, x, N, L, C);
   }
-  return cudaGetLastError();
+  {
+    const long long blocks = min((rows * copy_blocks(C) + 7) / 8, (long long)sms * 64);
+    return launch(checkpoint_unpack_any_kernel<T>, (unsigned)blocks, COPY_THREADS, 1, 0, s, in, x, N, L, C);
+  }
 }
 
 // ---------------------------------------------------------------------------------------------------------- GroupNorm
@@ -196,39 +215,23 @@ bool warp_plan(NormArgs& g, int V, int most, int ctas, int sms, int& items) {
   return true;
 }
 
-template <typename F>
-cudaError_t launch(F kern, const NormArgs& g, int smem, cudaStream_t s) {
-  cudaLaunchConfig_t cfg{};
-  cudaLaunchAttribute at[1];
-  cfg.gridDim = dim3((unsigned)((long long)g.splits * g.sets * g.ranks));
-  cfg.blockDim = dim3(GN_THREADS);
-  cfg.dynamicSmemBytes = smem;
-  cfg.stream = s;
-  at[0].id = cudaLaunchAttributeClusterDimension;
-  at[0].val.clusterDim.x = g.ranks; at[0].val.clusterDim.y = 1; at[0].val.clusterDim.z = 1;
-  cfg.attrs = at;
-  cfg.numAttrs = g.ranks > 1 ? 1 : 0;
-  return cudaLaunchKernelEx(&cfg, kern, g);
-}
-
 template <typename T, int ITEMS>
 cudaError_t norm_slab(const NormArgs& g, int smem, int device, cudaStream_t s) {
   static std::atomic<unsigned long long> done{0};
   const cudaError_t e = allow_smem(group_norm_slab_kernel<T, ITEMS>, SLAB_SMEM, device, done);
-  return e != cudaSuccess ? e : launch(group_norm_slab_kernel<T, ITEMS>, g, smem, s);
+  return e != cudaSuccess ? e : launch(group_norm_slab_kernel<T, ITEMS>, (unsigned)(g.splits * g.sets), GN_THREADS, 1, smem, s, g);
 }
 template <typename T, int ITEMS, bool COPY>
 cudaError_t norm_slab_grad(const NormArgs& g, int smem, int device, cudaStream_t s) {
   static std::atomic<unsigned long long> done{0};
   const cudaError_t e = allow_smem(group_norm_slab_grad_kernel<T, ITEMS, COPY>, SLAB_SMEM, device, done);
-  return e != cudaSuccess ? e : launch(group_norm_slab_grad_kernel<T, ITEMS, COPY>, g, smem, s);
+  return e != cudaSuccess ? e : launch(group_norm_slab_grad_kernel<T, ITEMS, COPY>, (unsigned)(g.splits * g.sets), GN_THREADS, 1, smem, s, g);
 }
 
 template <typename F>
 cudaError_t launch_warps(F kern, const NormArgs& g, int smem, cudaStream_t s) {
   const long long warps = (long long)g.splits * g.groups;
-  kern<<<(unsigned)((warps + GN_WARP_THREADS / 32 - 1) / (GN_WARP_THREADS / 32)), GN_WARP_THREADS, smem, s>>>(g);
-  return cudaGetLastError();
+  return launch(kern, (unsigned)((warps + GN_WARP_THREADS / 32 - 1) / (GN_WARP_THREADS / 32)), GN_WARP_THREADS, 1, smem, s, g);
 }
 template <typename T>
 cudaError_t norm_warp(const NormArgs& g, int items, cudaStream_t s) {
@@ -270,7 +273,7 @@ cudaError_t norm_forward(NormArgs& g, int sms, int device, cudaStream_t s) {
   static std::atomic<unsigned long long> done{0};
   const int smem = (2 * GN_THREADS * V + 4 * g.per_set) * 4;
   const cudaError_t e = allow_smem(group_norm_kernel<T, V>, (2 * GN_THREADS * V + 4 * GN_MAX_WIDTH) * 4, device, done);
-  return e != cudaSuccess ? e : launch(group_norm_kernel<T, V>, g, smem, s);
+  return e != cudaSuccess ? e : launch(group_norm_kernel<T, V>, (unsigned)((long long)g.splits * g.sets * g.ranks), GN_THREADS, g.ranks, smem, s, g);
 }
 
 enum { GRAD_STREAM = 0, GRAD_WARPS = 1, GRAD_SLABS = 2 };
@@ -285,7 +288,7 @@ cudaError_t norm_backward(NormArgs& g, int form, int items, int bytes, int devic
   static std::atomic<unsigned long long> done{0};
   const int smem = (4 * GN_THREADS * V + 8 * g.width + 2 * g.per_set) * 4;
   const cudaError_t e = allow_smem(group_norm_grad_kernel<T, V, COPY>, (4 * GN_THREADS * V + 10 * GN_MAX_WIDTH) * 4, device, done);
-  return e != cudaSuccess ? e : launch(group_norm_grad_kernel<T, V, COPY>, g, smem, s);
+  return e != cudaSuccess ? e : launch(group_norm_grad_kernel<T, V, COPY>, (unsigned)((long long)g.splits * g.sets * g.ranks), GN_THREADS, g.ranks, smem, s, g);
 }
 
 size_t norm_grad_bytes(const NormArgs& g) { return (size_t)g.splits * 2 * g.C * 4; }
@@ -304,31 +307,36 @@ EncodeTiledFn encode_fn() {
   return reinterpret_cast<EncodeTiledFn>(fn);
 }
 
-struct WgradPlan { int bn, ctas; size_t share_bytes, bytes; };
+struct WgradPlan { int bn, cg, units; size_t share_bytes, bytes; };
 
-WgradPlan wgrad_plan(WgradArgs& g, bool fp32, int sms) {
+// pair: the two-CTA form may be taken (dy and q by TMA).
+WgradPlan wgrad_plan(WgradArgs& g, bool fp32, bool pair, int sms) {
   WgradPlan p;
   p.bn = g.O <= 64 ? 64 : (g.O <= 128 || fp32 ? 128 : 256);
-  g.tiles_k = (g.K + WG_BM - 1) / WG_BM;
-  g.tiles_o = (g.O + p.bn - 1) / p.bn;
+  const int k128 = (g.K + WG_BM - 1) / WG_BM;
   g.stages = (int)((g.M + WG_BK - 1) / WG_BK);
-  const long long line = (long long)g.stages * g.taps * g.tiles_k * g.tiles_o;
-  g.line = line < (1ll << 31) - 4096 ? (int)line : 0;
-  p.ctas = (int)min((long long)sms, max(1ll, line / 2));
-  p.share_bytes = (size_t)2 * p.ctas * WG_BM * p.bn * 4;
-  p.bytes = p.share_bytes + (size_t)(p.ctas + (long long)g.taps * g.tiles_k * g.tiles_o) * WG_BIAS * 4;
+  g.tiles_o = (g.O + p.bn - 1) / p.bn;
+  // pairs where 256-wide tiles leave little of K unused and the line keeps them busy
+  p.cg = pair && !fp32 && p.bn == 256 && (k128 % 2 == 0 || k128 >= 7) && (long long)g.stages * g.taps * (k128 / 2) * g.tiles_o >= 16ll * sms ? 2 : 1;
+  g.tiles_k = (k128 + p.cg - 1) / p.cg;
+  const long long tiles = (long long)g.taps * g.tiles_k * g.tiles_o, line = g.stages * tiles;
+  g.line = line < (1ll << 31) - 4096 && 32 * tiles < (1ll << 31) ? (int)line : 0;
+  p.units = (int)min((long long)(sms / p.cg), max(1ll, line / 2));
+  p.share_bytes = (size_t)2 * p.units * p.cg * WG_BM * p.bn * 4;
+  p.bytes = p.share_bytes + (size_t)(p.units + tiles) * p.cg * WG_BIAS * 4;
   return p;
 }
 
-template <int BN, int DYK>
-cudaError_t wgrad_launch(const CUtensorMap& map, const CUtensorMap& qmap, const WgradArgs& g, int ctas, int device, cudaStream_t s) {
+template <int BN, int DYK, int CG>
+cudaError_t wgrad_launch(const CUtensorMap& map, const CUtensorMap& qmap, const WgradArgs& g, int units, int device, cudaStream_t s) {
   static std::atomic<unsigned long long> done{0};
-  const cudaError_t e = allow_smem(weight_grad_kernel<BN, DYK>, wg_smem_bytes(BN, DYK), device, done);
+  constexpr int smem = wg_smem_bytes(BN, DYK, CG);
+  cudaError_t e = allow_smem(weight_grad_kernel<BN, DYK, CG>, smem, device, done);
   if (e != cudaSuccess) return e;
-  weight_grad_kernel<BN, DYK><<<ctas, WG_THREADS, wg_smem_bytes(BN, DYK), s>>>(map, qmap, g);
+  e = launch(weight_grad_kernel<BN, DYK, CG>, (unsigned)(units * CG), WG_THREADS, CG, smem, s, map, qmap, g);
+  if (e != cudaSuccess) return e;
   const int tiles = g.taps * g.tiles_k * g.tiles_o;
-  weight_grad_join_kernel<BN><<<(unsigned)(tiles * (BN / 16) + (g.db ? g.tiles_o : 0)), 256, 0, s>>>(g, ctas, tiles);
-  return cudaGetLastError();
+  return launch(weight_grad_join_kernel<BN, CG>, (unsigned)(tiles * (BN / 16 * CG) + (g.db ? g.tiles_o : 0)), 256, 1, 0, s, g, units, tiles);
 }
 
 bool wgrad_ok(int dtype, long long N, int L, int K, int O, int taps) {
@@ -466,8 +474,7 @@ int tsdp_group_norm_grad(int device, const tsdp_norm_t* shape, const void* d_dy,
     else e = copy ? norm_backward<float, 1, true>(g, form, items, bytes, device, s) : norm_backward<float, 1, false>(g, form, items, bytes, device, s);
   }
   if (e == cudaSuccess) {
-    group_norm_join_kernel<<<dim3((C + GN_JOIN_CH - 1) / GN_JOIN_CH, 2), GN_JOIN_CH * GN_JOIN_LANES, 0, s>>>(g.part, g.splits, C, d_dgamma, d_dbeta);
-    e = cudaGetLastError();
+    e = launch(group_norm_join_kernel, (unsigned)(2 * ((C + GN_JOIN_CH - 1) / GN_JOIN_CH)), GN_JOIN_CH * GN_JOIN_LANES, 1, 0, s, (const float*)g.part, g.splits, C, d_dgamma, d_dbeta);
   }
   return e == cudaSuccess ? TSDP_OK : fail_cuda("tsdp_group_norm_grad", e);
 }
@@ -476,8 +483,13 @@ size_t tsdp_weight_grad_workspace(int device, int dtype, int N, int L, int K, in
   if (device < 0 || device >= MAX_DEVICES || !wgrad_ok(dtype, N, L, K, O, taps)) return 0;
   WgradArgs g{};
   g.M = (long long)(N < 1 ? 1 : N) * L; g.K = K; g.O = O; g.taps = taps;
-  const size_t bytes = wgrad_plan(g, dtype == TSDP_TYPE_FP32, device_sms(device)).bytes;
-  return g.line ? bytes : 0;
+  size_t most = 0;
+  for (bool pair : {false, true}) {                      // (which of them a call takes depends on alignment)
+    const WgradPlan p = wgrad_plan(g, dtype == TSDP_TYPE_FP32, pair, device_sms(device));
+    if (g.line == 0) return 0;
+    if (p.bytes > most) most = p.bytes;
+  }
+  return most;
 }
 
 int tsdp_weight_grad(int device, int dtype, const tsdp_saved_t* saved_x, const void* d_dy, int64_t dy_l, int N, int L, int K, int O, int taps, float* d_dW,
@@ -499,14 +511,14 @@ int tsdp_weight_grad(int device, int dtype, const tsdp_saved_t* saved_x, const v
   g.M = (long long)N * L; g.L = L; g.K = K; g.O = O; g.taps = taps;
   g.dW = d_dW;
   const bool fp32 = dtype == TSDP_TYPE_FP32;
-  const WgradPlan p = wgrad_plan(g, fp32, device_sms(device));
-  if (g.line == 0 || workspace_bytes < p.bytes || 17ll * g.taps * g.tiles_k * g.tiles_o >= (1ll << 31)) return TSDP_ERR_ARG;
+  const bool tma = !fp32 && aligned16(d_dy) && dy_l % 8 == 0 && dy_l >= O && dy_l < (1ll << 38);
+  g.q_tma = K % 16 == 0 && aligned16(g.x.q);
+  const WgradPlan p = wgrad_plan(g, fp32, tma && g.q_tma, device_sms(device));
+  if (g.line == 0 || workspace_bytes < p.bytes) return TSDP_ERR_ARG;
   g.share = reinterpret_cast<float*>(d_workspace);
   g.db = d_db;
   g.bias = reinterpret_cast<float*>(reinterpret_cast<char*>(d_workspace) + p.share_bytes);
   CUtensorMap map{}, qmap{};
-  const bool tma = !fp32 && aligned16(d_dy) && dy_l % 8 == 0 && dy_l >= O && dy_l < (1ll << 38);
-  g.q_tma = K % 16 == 0 && aligned16(g.x.q);
   EncodeTiledFn encode = encode_fn();
   if (!encode) { fprintf(stderr, "tsdp_weight_grad: cuTensorMapEncodeTiled unavailable\n"); return TSDP_ERR_CUDA; }
   auto tiled = [&](CUtensorMap* m, const void* p2, bool bf16, int cols, long long pitch, int box_cols) {      // rows x cols, boxes of 64 rows
@@ -520,10 +532,11 @@ int tsdp_weight_grad(int device, int dtype, const tsdp_saved_t* saved_x, const v
   if (tma) r = tiled(&map, d_dy, true, O, dy_l * 2, 64);
   if (r == CUDA_SUCCESS && g.q_tma) r = tiled(&qmap, g.x.q, false, K, K, WG_BM);
   if (r != CUDA_SUCCESS) { fprintf(stderr, "tsdp_weight_grad: cuTensorMapEncodeTiled failed with code %d\n", (int)r); return TSDP_ERR_CUDA; }
-  if (fp32) e = p.bn == 64 ? wgrad_launch<64, WG_DY_FP32>(map, qmap, g, p.ctas, device, s) : wgrad_launch<128, WG_DY_FP32>(map, qmap, g, p.ctas, device, s);
-  else if (p.bn == 64) e = tma ? wgrad_launch<64, WG_DY_TMA>(map, qmap, g, p.ctas, device, s) : wgrad_launch<64, WG_DY_BF16>(map, qmap, g, p.ctas, device, s);
-  else if (p.bn == 128) e = tma ? wgrad_launch<128, WG_DY_TMA>(map, qmap, g, p.ctas, device, s) : wgrad_launch<128, WG_DY_BF16>(map, qmap, g, p.ctas, device, s);
-  else e = tma ? wgrad_launch<256, WG_DY_TMA>(map, qmap, g, p.ctas, device, s) : wgrad_launch<256, WG_DY_BF16>(map, qmap, g, p.ctas, device, s);
+  if (fp32) e = p.bn == 64 ? wgrad_launch<64, WG_DY_FP32, 1>(map, qmap, g, p.units, device, s) : wgrad_launch<128, WG_DY_FP32, 1>(map, qmap, g, p.units, device, s);
+  else if (p.cg == 2) e = wgrad_launch<256, WG_DY_TMA, 2>(map, qmap, g, p.units, device, s);
+  else if (p.bn == 64) e = tma ? wgrad_launch<64, WG_DY_TMA, 1>(map, qmap, g, p.units, device, s) : wgrad_launch<64, WG_DY_BF16, 1>(map, qmap, g, p.units, device, s);
+  else if (p.bn == 128) e = tma ? wgrad_launch<128, WG_DY_TMA, 1>(map, qmap, g, p.units, device, s) : wgrad_launch<128, WG_DY_BF16, 1>(map, qmap, g, p.units, device, s);
+  else e = tma ? wgrad_launch<256, WG_DY_TMA, 1>(map, qmap, g, p.units, device, s) : wgrad_launch<256, WG_DY_BF16, 1>(map, qmap, g, p.units, device, s);
   return e == cudaSuccess ? TSDP_OK : fail_cuda("tsdp_weight_grad", e);
 }
 

@@ -23,6 +23,9 @@
 // 4400 in one go were 1.2 10^-6, 9700 3.7 10^-6).
 // Work is the line of all (tile, stage) pairs, cut into equal pieces, one per CTA, so that no CTA is idle whatever the sizes; a tile that
 // more than one CTA worked on is added up from their shares in the order of the line: the same bits on every run.
+// Pair form (CG = 2, cta_group::2): a tile of 256 x 256 on two SMs.  Each CTA makes x^ of its own 128 input channels and loads half of the
+// dy columns, so that a stage brings 16 KB less into each SM's shared memory and the tensor core reads 16 KB less of it.  Everything but the
+// MMAs stays within a CTA: the second CTA's idle MMA warp passes on to the first that its stage is complete.
 // Every wait is bounded; a CTA whose wait runs out leaves NaN in what it had to write.
 #pragma once
 #include "checkpoint_kernels.cuh"
@@ -35,12 +38,15 @@ constexpr int WG_TILE_A = WG_BK * WG_BM * 2, WG_TILE_Q = WG_BK * WG_BM;
 enum { WG_DY_TMA = 0, WG_DY_BF16 = 1, WG_DY_FP32 = 2 };
 __host__ __device__ constexpr int wg_chunk(int dyk) { return dyk == WG_DY_FP32 ? 8 : 32; }      // (three products a stage in fp32)
 __host__ __device__ constexpr int wg_parts(int dyk) { return dyk == WG_DY_FP32 ? 3 : 1; }
-__host__ __device__ constexpr int wg_tile_b(int BN, int dyk) { return wg_parts(dyk) * WG_BK * BN * 2; }
+__host__ __device__ constexpr int wg_tile_b(int BN, int dyk, int CG) { return wg_parts(dyk) * WG_BK * (BN / CG) * 2; }
 // stages of the three rings: x^, dy, q
-constexpr int WG_SA = 4, WG_SQ = 6;
-__host__ __device__ constexpr int wg_sb(int BN, int dyk) { return wg_tile_b(BN, dyk) > 32768 ? 2 : (wg_tile_b(BN, dyk) > 24576 ? 3 : 4); }
-__host__ __device__ constexpr int wg_smem_bytes(int BN, int dyk) {
-  return WG_SA * WG_TILE_A + wg_sb(BN, dyk) * wg_tile_b(BN, dyk) + WG_SQ * WG_TILE_Q + 512 + 1024;
+constexpr int WG_SQ = 6;
+__host__ __device__ constexpr int wg_sa(int CG) { return CG == 2 ? 5 : 4; }
+__host__ __device__ constexpr int wg_sb(int BN, int dyk, int CG) {
+  return CG == 2 ? 5 : (wg_tile_b(BN, dyk, CG) > 32768 ? 2 : (wg_tile_b(BN, dyk, CG) > 24576 ? 3 : 4));
+}
+__host__ __device__ constexpr int wg_smem_bytes(int BN, int dyk, int CG) {
+  return wg_sa(CG) * WG_TILE_A + wg_sb(BN, dyk, CG) * wg_tile_b(BN, dyk, CG) + WG_SQ * WG_TILE_Q + 512 + 1024;
 }
 
 struct WgradArgs {
@@ -52,8 +58,8 @@ struct WgradArgs {
   int tiles_k, tiles_o;                     // tile = (tap, kt, ot), ot fastest
   int stages, line;                         // of a tile; of all tiles (line + grid < 2^31)
   float* dW;                                // [taps, K, O]
-  float* share;                             // [2 grid][BN / 4][128][4]: what a CTA has of its first / of its last tile
-  float *db, *bias;                         // [O] or null; [grid + tiles][WG_BIAS / BN][BN]: shares of it, of CTA i in tile t at i + t
+  float* share;                             // [grid][2][BN / 4][128][4]: what a CTA has of its first / of its last tile
+  float *db, *bias;                         // [O] or null; [units + tiles][CG][WG_BIAS]: shares of it, of unit (CTA or pair) i in tile t at i + t
 };
 // The line's piece of CTA i of n.
 __host__ __device__ inline int wg_begin(int line, int i, int n) { return line / n * i + min(i, line % n); }
@@ -87,12 +93,20 @@ __device__ __forceinline__ void red_add4(float* p, const uint32_t* v) {
                "f"(__uint_as_float(v[3])) : "memory");
 }
 
-template <int BN, int DYK>
+// The second CTA of a pair to the first: "my stage is complete".  What it passes on was written to its own shared memory and is read there by
+// its own tensor core, so the arrival is ordered behind this CTA's; a release to the whole cluster (.release.cluster) at every stage costs
+// more than the stage: 45056 x 512 -> 2048 177 us in place of 110.
+__device__ __forceinline__ void wg_pass_on(uint32_t bar_of_first) {
+  asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(bar_of_first) : "memory");
+}
+
+template <int BN, int DYK, int CG>
 __global__ void __launch_bounds__(WG_THREADS, 1)
 weight_grad_kernel(const __grid_constant__ CUtensorMap tmDy, const __grid_constant__ CUtensorMap tmQ, WgradArgs g) {
-  constexpr int SA = WG_SA, SB = wg_sb(BN, DYK), SQ = WG_SQ, PARTS = wg_parts(DYK), CHUNK = wg_chunk(DYK), TILE_B = wg_tile_b(BN, DYK);
+  constexpr int SA = wg_sa(CG), SB = wg_sb(BN, DYK, CG), SQ = WG_SQ, PARTS = wg_parts(DYK), CHUNK = wg_chunk(DYK), TILE_B = wg_tile_b(BN, DYK, CG);
+  constexpr int BH = BN / CG;                                // columns of dy in this CTA
   constexpr uint32_t TMEM_COLS = 2 * BN < 32 ? 32 : 2 * BN;
-  constexpr uint32_t IDESC = umma_idesc_bf16(BN, WG_BM) | (1u << 15) | (1u << 16);      // both operands MN-major
+  constexpr uint32_t IDESC = umma_idesc_bf16(BN, WG_BM * CG) | (1u << 15) | (1u << 16);      // both operands MN-major
   extern __shared__ uint8_t wg_raw[];
   const uint32_t base = (ptx::smem_u32(wg_raw) + 1023u) & ~1023u;
   uint8_t* const raw = wg_raw + (base - ptx::smem_u32(wg_raw));
@@ -106,24 +120,32 @@ weight_grad_kernel(const __grid_constant__ CUtensorMap tmDy, const __grid_consta
   auto empty_q = [&](int s) { return bar0 + 8u * (2 * SA + 2 * SB + SQ + s); };
   auto tfull = [&](int b) { return bar0 + 8u * (2 * SA + 2 * SB + 2 * SQ + b); };
   auto tempty = [&](int b) { return bar0 + 8u * (2 * SA + 2 * SB + 2 * SQ + 2 + b); };
-  const uint32_t slot = bar0 + 8u * (2 * SA + 2 * SB + 2 * SQ + 4);
-  static_assert(8 * (2 * SA + 2 * SB + 2 * SQ + 4) + 4 <= 512, "the barriers have 512 bytes");
+  auto peer = [&](int s) { return bar0 + 8u * (2 * SA + 2 * SB + 2 * SQ + 4 + s); };
+  const uint32_t slot = bar0 + 8u * (3 * SA + 2 * SB + 2 * SQ + 4);
+  static_assert(8 * (3 * SA + 2 * SB + 2 * SQ + 4) + 4 <= 512, "the barriers have 512 bytes");
   const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
   if (threadIdx.x == 0) {
-    for (int s = 0; s < SA; ++s) { ptx::mbar_init(full_a(s), WG_LOADERS / 32); ptx::mbar_init(empty_a(s), 1); }
+    for (int s = 0; s < SA; ++s) { ptx::mbar_init(full_a(s), WG_LOADERS / 32); ptx::mbar_init(empty_a(s), 1); ptx::mbar_init(peer(s), 1); }
     for (int s = 0; s < SB; ++s) { ptx::mbar_init(full_b(s), DYK == WG_DY_TMA ? 1 : WG_LOADERS / 32); ptx::mbar_init(empty_b(s), g.db ? 5 : 1); }
     for (int s = 0; s < SQ; ++s) { ptx::mbar_init(full_q(s), 1); ptx::mbar_init(empty_q(s), WG_LOADERS / 32); }
-    for (int b = 0; b < 2; ++b) { ptx::mbar_init(tfull(b), 1); ptx::mbar_init(tempty(b), 4); }
+    for (int b = 0; b < 2; ++b) { ptx::mbar_init(tfull(b), 1); ptx::mbar_init(tempty(b), 4 * CG); }
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
   }
-  if (warp == 1) { ptx::tmem_alloc(slot, TMEM_COLS); ptx::tmem_relinquish(); }
+  if (warp == 1) {
+    if (CG == 2) { ptx::tmem_alloc_pair(slot, TMEM_COLS); ptx::tmem_relinquish_pair(); }
+    else { ptx::tmem_alloc(slot, TMEM_COLS); ptx::tmem_relinquish(); }
+  }
   ptx::tc_fence_before();
   __syncthreads();
+  if (CG == 2) ptx::cluster_sync_all();                     // the peer's barriers exist
   ptx::tc_fence_after();
   const uint32_t tmem = *reinterpret_cast<volatile uint32_t*>(raw + (slot - base));
+  pdl_trigger(true);                                        // the join of the shares: its blocks wait beside this grid, which runs at once as a whole
+  pdl_wait();
 
-  const int begin = wg_begin(g.line, blockIdx.x, gridDim.x), end = wg_begin(g.line, blockIdx.x + 1, gridDim.x);
+  const int rank = CG == 2 ? (int)ptx::cluster_rank() : 0, unit = blockIdx.x / CG, units = gridDim.x / CG;
+  const int begin = wg_begin(g.line, unit, units), end = wg_begin(g.line, unit + 1, units);
   const int t_first = begin / g.stages;
   bool ok = true;
 
@@ -133,10 +155,10 @@ weight_grad_kernel(const __grid_constant__ CUtensorMap tmDy, const __grid_consta
       uint32_t ph = 1;
       for (int i = begin; i < end; ++i) {
         if (!ptx::mbar_wait_thread(empty_b(s), ph)) { ok = false; break; }
-        const int o0 = t % g.tiles_o * BN;
-        ptx::mbar_expect_tx(full_b(s), BN * WG_BK * 2);
+        const int o0 = t % g.tiles_o * BN + rank * BH;
+        ptx::mbar_expect_tx(full_b(s), BH * WG_BK * 2);
 #pragma unroll
-        for (int j = 0; j < BN / 64; ++j) ptx::tma_load_2d(base + OFF_B + s * TILE_B + j * WG_BK * 128, &tmDy, o0 + 64 * j, st * WG_BK, full_b(s));
+        for (int j = 0; j < BH / 64; ++j) ptx::tma_load_2d(base + OFF_B + s * TILE_B + j * WG_BK * 128, &tmDy, o0 + 64 * j, st * WG_BK, full_b(s));
         if (++s == SB) { s = 0; ph ^= 1; }
         if (++st == g.stages) { st = 0; ++t; }
       }
@@ -149,9 +171,20 @@ weight_grad_kernel(const __grid_constant__ CUtensorMap tmDy, const __grid_consta
         if (!ptx::mbar_wait_thread(empty_q(s), ph)) { ok = false; break; }
         const int tk = t / g.tiles_o, tap = tk / g.tiles_k;
         ptx::mbar_expect_tx(full_q(s), WG_TILE_Q);
-        ptx::tma_load_2d(base + OFF_Q + s * WG_TILE_Q, &tmQ, (tk - tap * g.tiles_k) * WG_BM, st * WG_BK + tap - g.taps / 2, full_q(s));
+        ptx::tma_load_2d(base + OFF_Q + s * WG_TILE_Q, &tmQ, ((tk - tap * g.tiles_k) * CG + rank) * WG_BM, st * WG_BK + tap - g.taps / 2, full_q(s));
         if (++s == SQ) { s = 0; ph ^= 1; }
         if (++st == g.stages) { st = 0; ++t; }
+      }
+    }
+  } else if (warp == 1 && rank != 0) {
+    if (ptx::elect_one()) {
+      int sa = 0, sb = 0;
+      uint32_t pa = 0, pb = 0;
+      for (int i = begin; i < end; ++i) {
+        if (!ptx::mbar_wait_thread(full_b(sb), pb) || !ptx::mbar_wait_thread(full_a(sa), pa)) { ok = false; break; }
+        wg_pass_on(ptx::mapa_rank(peer(sa), 0));
+        if (++sa == SA) { sa = 0; pa ^= 1; }
+        if (++sb == SB) { sb = 0; pb ^= 1; }
       }
     }
   } else if (warp == 1) {
@@ -159,25 +192,29 @@ weight_grad_kernel(const __grid_constant__ CUtensorMap tmDy, const __grid_consta
       int t = t_first, st = begin - t * g.stages, sa = 0, sb = 0, buf = 0, chunk = 0;
       uint32_t pa = 0, pb = 0, tph = 1;
       bool fresh = true;
+      auto commit = [&](uint32_t bar) { if (CG == 2) ptx::tc_commit_pair(bar); else ptx::tc_commit(bar); };
       for (int i = begin; i < end; ++i) {
         if (fresh && !ptx::mbar_wait_thread(tempty(buf), tph)) { ok = false; break; }
-        if (!ptx::mbar_wait_thread(full_b(sb), pb) || !ptx::mbar_wait_thread(full_a(sa), pa)) { ok = false; break; }
+        if (!ptx::mbar_wait_thread(full_b(sb), pb) || !ptx::mbar_wait_thread(full_a(sa), pa) || (CG == 2 && !ptx::mbar_wait_thread(peer(sa), pa))) { ok = false; break; }
         ptx::tc_fence_after();
         const uint32_t a0 = base + sa * WG_TILE_A, b0 = base + OFF_B + sb * TILE_B, d = tmem + buf * BN;
 #pragma unroll
         for (int p = 0; p < PARTS; ++p)
 #pragma unroll
           for (int k = 0; k < WG_BK / 16; ++k)      // 16 rows = 2048 bytes of every column of 64 channels
-            ptx::tc_mma_bf16(d, umma_desc_mn_sw128(a0 + k * 2048, WG_BK * 128), umma_desc_mn_sw128(b0 + p * (WG_BK * BN * 2) + k * 2048, WG_BK * 128), IDESC,
-                             fresh && p == 0 && k == 0 ? 0u : 1u);
+          {
+            const uint64_t da = umma_desc_mn_sw128(a0 + k * 2048, WG_BK * 128), db = umma_desc_mn_sw128(b0 + p * (WG_BK * BH * 2) + k * 2048, WG_BK * 128);
+            const uint32_t acc = fresh && p == 0 && k == 0 ? 0u : 1u;
+            if (CG == 2) ptx::tc_mma_bf16_pair(d, da, db, IDESC, acc); else ptx::tc_mma_bf16(d, da, db, IDESC, acc);
+          }
         fresh = false;
-        ptx::tc_commit(empty_a(sa));
-        ptx::tc_commit(empty_b(sb));
+        commit(empty_a(sa));
+        commit(empty_b(sb));
         if (++sa == SA) { sa = 0; pa ^= 1; }
         if (++sb == SB) { sb = 0; pb ^= 1; }
         const bool done = ++st == g.stages;
         if (++chunk == CHUNK || done || i + 1 == end) {
-          ptx::tc_commit(tfull(buf));
+          commit(tfull(buf));
           chunk = 0; fresh = true;
           if (done) { st = 0; ++t; }
           if (++buf == 2) { buf = 0; tph ^= 1; }
@@ -195,7 +232,7 @@ weight_grad_kernel(const __grid_constant__ CUtensorMap tmDy, const __grid_consta
     auto place = [&] {
       const int tk = t / g.tiles_o, tap = tk / g.tiles_k;
       shift = tap - g.taps / 2;
-      c = (tk - tap * g.tiles_k) * WG_BM + p * 16;
+      c = ((tk - tap * g.tiles_k) * CG + rank) * WG_BM + p * 16;
       const long long m = (long long)st * WG_BK + r;
       left = (int)(g.M - m);
       l0 = (int)(m % g.L) + shift;
@@ -248,7 +285,7 @@ weight_grad_kernel(const __grid_constant__ CUtensorMap tmDy, const __grid_consta
         w[0] = *reinterpret_cast<const uint4*>(q);
         w[1] = *reinterpret_cast<const uint4*>(q + 32 * WG_BM);
       } else {
-        const int tk = t_cur / g.tiles_o, tap = tk / g.tiles_k, ch = (tk - tap * g.tiles_k) * WG_BM + p * 16;
+        const int tk = t_cur / g.tiles_o, tap = tk / g.tiles_k, ch = ((tk - tap * g.tiles_k) * CG + rank) * WG_BM + p * 16;
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
           const long long ms = (long long)st_cur * WG_BK + r + 32 * h + tap - g.taps / 2;
@@ -338,7 +375,7 @@ weight_grad_kernel(const __grid_constant__ CUtensorMap tmDy, const __grid_consta
     while (i < end) {
       const int t_end = min((t + 1) * g.stages, end);
       const bool whole = i == t * g.stages && t_end == (t + 1) * g.stages;
-      const int o0 = t % g.tiles_o * BN, tk = t / g.tiles_o, tap = tk / g.tiles_k, k = (tk - tap * g.tiles_k) * WG_BM + row;
+      const int o0 = t % g.tiles_o * BN, tk = t / g.tiles_o, tap = tk / g.tiles_k, k = ((tk - tap * g.tiles_k) * CG + rank) * WG_BM + row;
       float* share = g.share + (2ll * blockIdx.x + (t == t_first ? 0 : 1)) * (WG_BM * BN) + row * 4;
       float* out = g.dW + ((long long)tap * g.K + k) * g.O + o0;
       const int cols = min(BN, g.O - o0);
@@ -387,16 +424,19 @@ weight_grad_kernel(const __grid_constant__ CUtensorMap tmDy, const __grid_consta
         }
         ptx::tc_fence_before();
         __syncwarp();
-        if (lane == 0) ptx::mbar_arrive(tempty(buf));
+        if (lane == 0) {
+          if (CG == 2 && rank != 0) ptx::mbar_arrive_cluster(ptx::mapa_rank(tempty(buf), 0));
+          else ptx::mbar_arrive(tempty(buf));
+        }
         if (++buf == 2) { buf = 0; ph ^= 1; }
       }
       ++t;
     }
   } else if (g.db) {
     // eight columns of the dy tile and a share of its rows a thread
-    constexpr int UNITS = BN / 8, GROUPS = 128 / UNITS, ROWS = WG_BK / GROUPS;
-    const int tb = threadIdx.x - 192, unit = tb % UNITS, grp = tb / UNITS;
-    const uint32_t at = (uint32_t)(unit >> 3) * (WG_BK * 128) + (uint32_t)grp * ROWS * 128;
+    constexpr int UNITS = BH / 8, GROUPS = 128 / UNITS, ROWS = WG_BK / GROUPS;
+    const int tb = threadIdx.x - 192, piece = tb % UNITS, grp = tb / UNITS;
+    const uint32_t at = (uint32_t)(piece >> 3) * (WG_BK * 128) + (uint32_t)grp * ROWS * 128;
     int t = t_first, st = begin - t * g.stages, s = 0;
     uint32_t ph = 0;
     float2 sum[4];
@@ -413,10 +453,10 @@ weight_grad_kernel(const __grid_constant__ CUtensorMap tmDy, const __grid_consta
         for (int j = 0; j < 4; ++j) part[j] = make_float2(0.f, 0.f);
 #pragma unroll
         for (int p = 0; p < PARTS; ++p) {
-          const uint8_t* b0 = raw + OFF_B + s * TILE_B + p * (WG_BK * BN * 2) + at;
+          const uint8_t* b0 = raw + OFF_B + s * TILE_B + p * (WG_BK * BH * 2) + at;
 #pragma unroll 8
           for (int r = 0; r < ROWS; ++r) {
-            const uint4 u = *reinterpret_cast<const uint4*>(b0 + r * 128 + ((((uint32_t)unit ^ (uint32_t)(grp * ROWS + r)) & 7) << 4));
+            const uint4 u = *reinterpret_cast<const uint4*>(b0 + r * 128 + ((((uint32_t)piece ^ (uint32_t)(grp * ROWS + r)) & 7) << 4));
             const uint32_t w[4] = {u.x, u.y, u.z, u.w};
 #pragma unroll
             for (int j = 0; j < 4; ++j) part[j] = __fadd2_rn(part[j], make_float2(__uint_as_float(w[j] << 16), __uint_as_float(w[j] & 0xffff0000u)));
@@ -433,7 +473,7 @@ weight_grad_kernel(const __grid_constant__ CUtensorMap tmDy, const __grid_consta
       if (done || i + 1 == end) {
         if (centre)
 #pragma unroll
-          for (int j = 0; j < 4; ++j) *reinterpret_cast<float2*>(g.bias + (size_t)(blockIdx.x + t) * WG_BIAS + grp * BN + unit * 8 + 2 * j) = sum[j];
+          for (int j = 0; j < 4; ++j) *reinterpret_cast<float2*>(g.bias + ((size_t)(unit + t) * CG + rank) * WG_BIAS + grp * BH + piece * 8 + 2 * j) = sum[j];
 #pragma unroll
         for (int j = 0; j < 4; ++j) sum[j] = make_float2(0.f, 0.f);
         if (done) {
@@ -450,8 +490,11 @@ weight_grad_kernel(const __grid_constant__ CUtensorMap tmDy, const __grid_consta
   }
   ptx::tc_fence_before();
   __syncthreads();
+  if (CG == 2) ptx::cluster_sync_all();                     // neither CTA leaves while the other may still signal or read it
   ptx::tc_fence_after();
-  if (warp == 1) ptx::tmem_dealloc(tmem, TMEM_COLS);
+  if (warp == 1) {
+    if (CG == 2) ptx::tmem_dealloc_pair(tmem, TMEM_COLS); else ptx::tmem_dealloc(tmem, TMEM_COLS);
+  }
 }
 
 // CTAs first .. last of the line's pieces that hold stages of tile t.
@@ -463,47 +506,52 @@ __device__ __forceinline__ void wg_owners(const WgradArgs& g, int ctas, int t, i
 
 // Tiles that several CTAs worked on: their shares, in the order of the line; a block has 16 columns of a tile, a warp 8 rows x 16 columns at
 // a time (128 bytes of a share, 64 bytes of a row of dW).  The last tiles_o blocks (with db): the bias gradient of a column of tiles.
-template <int BN>
+template <int BN, int CG>
 __global__ void __launch_bounds__(256)
-weight_grad_join_kernel(WgradArgs g, int ctas, int tiles) {
-  constexpr int PARTS = BN / 16;
+weight_grad_join_kernel(WgradArgs g, int units, int tiles) {
+  constexpr int PARTS = BN / 16 * CG, BH = BN / CG;
+  pdl_wait();
   int first, last;
   if ((int)blockIdx.x >= tiles * PARTS) {
-    __shared__ float s_db[WG_BIAS];
+    __shared__ float s_db[CG][WG_BIAS];
     const int ot = blockIdx.x - tiles * PARTS;
-    float v[4] = {};
+    float v[CG][4] = {};
     for (int kt = 0; kt < g.tiles_k; ++kt) {
       const int t = ((g.taps / 2) * g.tiles_k + kt) * g.tiles_o + ot;
-      wg_owners(g, ctas, t, first, last);
+      wg_owners(g, units, t, first, last);
 #pragma unroll 4
       for (int i = first; i <= last; ++i)
 #pragma unroll
-        for (int j = 0; j < 4; ++j) v[j] += g.bias[(size_t)(i + t) * WG_BIAS + j * 256 + threadIdx.x];
+        for (int r = 0; r < CG; ++r)
+#pragma unroll
+          for (int j = 0; j < 4; ++j) v[r][j] += g.bias[((size_t)(i + t) * CG + r) * WG_BIAS + j * 256 + threadIdx.x];
     }
 #pragma unroll
-    for (int j = 0; j < 4; ++j) s_db[j * 256 + threadIdx.x] = v[j];
+    for (int r = 0; r < CG; ++r)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) s_db[r][j * 256 + threadIdx.x] = v[r][j];
     __syncthreads();
     const int col = threadIdx.x;
     if (col >= BN || ot * BN + col >= g.O) return;
     float sum = 0.f;
-    for (int i = 0; i < WG_BIAS / BN; ++i) sum += s_db[i * BN + col];
+    for (int i = 0; i < WG_BIAS / BH; ++i) sum += s_db[col / BH][i * BH + col % BH];
     g.db[ot * BN + col] = sum;
     return;
   }
-  const int t = blockIdx.x / PARTS;
-  wg_owners(g, ctas, t, first, last);
-  if (first == last) return;                                             // one CTA had all of it
-  const int o0 = t % g.tiles_o * BN, tk = t / g.tiles_o, tap = tk / g.tiles_k, k0 = (tk - tap * g.tiles_k) * WG_BM;
-  const int which0 = wg_begin(g.line, first, ctas) / g.stages == t ? 0 : 1;          // of the first; the others begin in this tile
+  const int t = blockIdx.x / PARTS, rank = blockIdx.x / (PARTS / CG) % CG;
+  wg_owners(g, units, t, first, last);
+  if (first == last) return;                                             // one CTA (or pair) had all of it
+  const int o0 = t % g.tiles_o * BN, tk = t / g.tiles_o, tap = tk / g.tiles_k, k0 = ((tk - tap * g.tiles_k) * CG + rank) * WG_BM;
+  const int which0 = wg_begin(g.line, first, units) / g.stages == t ? 0 : 1;         // of the first; the others begin in this tile
 #pragma unroll
   for (int j = 0; j < 2; ++j) {
-    const int e = j * 256 + threadIdx.x, row = (e >> 5) * 8 + (e & 7), c = (blockIdx.x % PARTS) * 16 + ((e >> 3) & 3) * 4, k = k0 + row;
+    const int e = j * 256 + threadIdx.x, row = (e >> 5) * 8 + (e & 7), c = (blockIdx.x % (PARTS / CG)) * 16 + ((e >> 3) & 3) * 4, k = k0 + row;
     if (k >= g.K || o0 + c >= g.O) continue;
     const float* sh = g.share + (c >> 2) * (WG_BM * 4) + row * 4;
-    float4 v = *reinterpret_cast<const float4*>(sh + (2ll * first + which0) * (WG_BM * BN));
+    float4 v = *reinterpret_cast<const float4*>(sh + (2ll * (first * CG + rank) + which0) * (WG_BM * BN));
 #pragma unroll 4
     for (int i = first + 1; i <= last; ++i) {
-      const float4 u = *reinterpret_cast<const float4*>(sh + 2ll * i * (WG_BM * BN));
+      const float4 u = *reinterpret_cast<const float4*>(sh + 2ll * (i * CG + rank) * (WG_BM * BN));
       v.x += u.x; v.y += u.y; v.z += u.z; v.w += u.w;
     }
     float* out = g.dW + ((long long)tap * g.K + k) * g.O + o0 + c;

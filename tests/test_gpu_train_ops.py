@@ -365,6 +365,15 @@ def test_weight_gradient(N, L, K, O, taps, dtype):
     check_weight(saved, dy, taps, L)
 
 
+# Large enough for pairs of CTAs (148 SMs: 2368 steps of 64 rows over 256 x 256 tiles), with ragged rows, channels and columns; many
+# tiles a unit; several roundings of one accumulator.
+@pytest.mark.parametrize("N,L,K,O,taps", [(240, 64, 256, 264, 5), (600, 32, 1008, 300, 1), (26, 501, 880, 520, 1), (1, 38011, 512, 512, 1),
+                                          (100, 10, 1024, 2048, 5)])
+def test_weight_gradient_by_pairs(N, L, K, O, taps):
+    saved, dy = weight_case(N, L, K, O, taps, "bf16", N * L + K)
+    check_weight(saved, dy, taps, L)
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
 @pytest.mark.parametrize("O,ldy", [(128, 136), (128, 131), (100, 104), (256, 1024)])
 def test_weight_gradient_of_strided_rows(O, ldy, dtype):

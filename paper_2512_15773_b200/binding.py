@@ -2,6 +2,7 @@
 runs in the library's CUDA kernels.  There is no CPU fallback: loading fails loudly when the shared
 library is missing, and tsdp_init fails when no CUDA device is present."""
 import ctypes as C
+import functools
 import os
 
 import numpy as np
@@ -192,37 +193,47 @@ def verify_commit_static(d_xt, d_muhat, d_eps, h_t, B, K, D, accept, seed, d_act
 # Module-level functions on torch tensors (see tsdp.h): they check types, shapes and devices, which the C side cannot see, and
 # only enqueue work on `stream` (a cudaStream_t; 0 is the default stream).  The tensors have to live until that work is done.
 
+@functools.lru_cache(maxsize=None)
+def _torch():
+    import torch
+    return torch
+
+
 def _dtype_code(t, name):
-    s = str(t.dtype)
-    if s == "torch.bfloat16":
+    torch = _torch()
+    if t.dtype is torch.bfloat16:
         return 1
-    if s == "torch.float32":
+    if t.dtype is torch.float32:
         return 0
-    raise ValueError(f"{name}: bfloat16 or float32 expected, got {s}")
+    raise ValueError(f"{name}: bfloat16 or float32 expected, got {t.dtype}")
 
 
 def _rows(t, name, like=None):
     """(address, stride of a sequence, stride of a position, N, L, C) of a tensor [N, L, C] or [rows, C]."""
-    if t.device.type != "cuda":
+    if not t.is_cuda:
         raise ValueError(f"{name}: a CUDA tensor expected")
     shape, stride = t.shape, t.stride()
-    if len(shape) == 2:
-        shape, stride = (1, *shape), (0, *stride)
-    if len(shape) != 3:
-        raise ValueError(f"{name}: [N, L, C] or [rows, C] expected, got {tuple(t.shape)}")
-    if stride[2] != 1 and shape[2] != 1:
+    if len(shape) == 3:
+        sn, sl, sc = stride
+        N, L, ch = shape
+    elif len(shape) == 2:
+        sn, (sl, sc) = 0, stride
+        N, (L, ch) = 1, shape
+    else:
+        raise ValueError(f"{name}: [N, L, C] or [rows, C] expected, got {tuple(shape)}")
+    if sc != 1 and ch != 1:
         raise ValueError(f"{name}: channels have to be innermost, without a gap")
-    if like is not None and (t.shape != like.shape or t.dtype != like.dtype or t.device != like.device):
-        raise ValueError(f"{name}: {tuple(like.shape)} of {like.dtype} on {like.device} expected, got {tuple(t.shape)} of {t.dtype} on {t.device}")
-    return t.data_ptr(), stride[0], stride[1], *shape
+    if like is not None and (shape != like.shape or t.dtype is not like.dtype or t.get_device() != like.get_device()):
+        raise ValueError(f"{name}: {tuple(like.shape)} of {like.dtype} on {like.device} expected, got {tuple(shape)} of {t.dtype} on {t.device}")
+    return t.data_ptr(), sn, sl, N, L, ch
 
 
-def _dense(t, name, shape, dtype, device):
-    """Address of a dense tensor of this shape and type on this device; None stays None."""
+def _dense(t, name, values, dtype, device):
+    """Address of a dense tensor of so many values of this type on this device (an ordinal); None stays None."""
     if t is None:
         return None
-    if t.shape != shape or str(t.dtype) != dtype or t.device != device or not t.is_contiguous():
-        raise ValueError(f"{name}: contiguous {tuple(shape)} of {dtype} on {device} expected, got {tuple(t.shape)} of {t.dtype} on {t.device}")
+    if t.numel() != values or t.dtype is not dtype or t.get_device() != device or not t.is_contiguous():
+        raise ValueError(f"{name}: {values} values of {dtype} without gaps on device {device} expected, got {tuple(t.shape)} of {t.dtype} on {t.device}")
     return t.data_ptr()
 
 
@@ -231,17 +242,28 @@ def _saved(pair, name, rows, channels, device):
     if pair is None:
         return None
     q, scale = pair
-    if q.numel() != rows * channels or q.shape[-1] != channels:
+    if q.shape[-1] != channels:
         raise ValueError(f"{name}: q of {rows} rows of {channels} channels expected, got {tuple(q.shape)}")
-    if scale.numel() != rows * (-(-channels // 32)):
-        raise ValueError(f"{name}: {-(-channels // 32)} scales for each of {rows} rows expected, got {tuple(scale.shape)}")
-    return SavedT(_dense(q, name + " q", q.shape, "torch.int8", device), _dense(scale, name + " scale", scale.shape, "torch.uint8", device))
+    torch = _torch()
+    return SavedT(_dense(q, name + " q", rows * channels, torch.int8, device),
+                  _dense(scale, name + " scale", rows * ((channels + 31) // 32), torch.uint8, device))
+
+
+@functools.lru_cache(maxsize=1024)
+def _norm_t(*sizes):
+    return NormT(*sizes)
 
 
 def _act(act):
     if act not in ACT:
         raise ValueError(f"act: one of {sorted(ACT)} expected, got {act!r}")
     return ACT[act]
+
+
+def _workspace(t, device):
+    if t.get_device() != device or not t.is_contiguous():
+        raise ValueError(f"workspace: a contiguous tensor on device {device} expected")
+    return t.data_ptr(), t.numel() * t.element_size()
 
 
 def _status(st, what):
@@ -251,7 +273,7 @@ def _status(st, what):
 
 def saved_like(x):
     """An empty 8-bit copy (q, scale) for a tensor [N, L, C] or [rows, C]."""
-    import torch
+    torch = _torch()
     return (torch.empty(x.shape, dtype=torch.int8, device=x.device),
             torch.empty((*x.shape[:-1], -(-x.shape[-1] // 32)), dtype=torch.uint8, device=x.device))
 
@@ -259,34 +281,35 @@ def saved_like(x):
 def checkpoint_pack(x, saved, stream=0):
     """Write the 8-bit copy of x into saved = (q, scale)."""
     p, sn, sl, N, L, ch = _rows(x, "x")
-    _status(load_library().tsdp_checkpoint_pack(x.device.index, _dtype_code(x, "x"), p, sn, sl, N, L, ch,
-                                                _saved(saved, "saved", N * L, ch, x.device), stream), "tsdp_checkpoint_pack")
+    dev = x.get_device()
+    _status(load_library().tsdp_checkpoint_pack(dev, _dtype_code(x, "x"), p, sn, sl, N, L, ch, _saved(saved, "saved", N * L, ch, dev), stream),
+            "tsdp_checkpoint_pack")
 
 
 def checkpoint_unpack(saved, x, stream=0):
     """Write the values that saved = (q, scale) stands for into x."""
     p, sn, sl, N, L, ch = _rows(x, "x")
-    _status(load_library().tsdp_checkpoint_unpack(x.device.index, _dtype_code(x, "x"), _saved(saved, "saved", N * L, ch, x.device), p, sn,
-                                                  sl, N, L, ch, stream), "tsdp_checkpoint_unpack")
+    dev = x.get_device()
+    _status(load_library().tsdp_checkpoint_unpack(dev, _dtype_code(x, "x"), _saved(saved, "saved", N * L, ch, dev), p, sn, sl, N, L, ch, stream),
+            "tsdp_checkpoint_unpack")
 
 
 def group_norm(x, gamma, beta, groups, y, act="mish", film=None, eps=1e-5, mean=None, rstd=None, saved_x=None, saved_y=None, stream=0):
     """y = film scale * act(GroupNorm(x)) + film bias; mean, rstd [N, groups] and the 8-bit copies of x and y where given."""
     p, sn, sl, N, L, ch = _rows(x, "x")
-    yp, yn, yl, *_ = _rows(y, "y", x)
-    dev, f32 = x.device, "torch.float32"
-    shape = NormT(_dtype_code(x, "x"), N, L, ch, groups, _act(act), eps)
+    yp, yn, yl = _rows(y, "y", x)[:3]
+    dev, f32 = x.get_device(), _torch().float32
     _status(load_library().tsdp_group_norm(
-        dev.index, shape, p, sn, sl, _dense(gamma, "gamma", (ch,), f32, dev), _dense(beta, "beta", (ch,), f32, dev),
-        _dense(film, "film", (N, 2 * ch), f32, dev), yp, yn, yl, _dense(mean, "mean", (N, groups), f32, dev),
-        _dense(rstd, "rstd", (N, groups), f32, dev), _saved(saved_x, "saved_x", N * L, ch, dev), _saved(saved_y, "saved_y", N * L, ch, dev),
-        stream), "tsdp_group_norm")
+        dev, _norm_t(_dtype_code(x, "x"), N, L, ch, groups, _act(act), eps), p, sn, sl, _dense(gamma, "gamma", ch, f32, dev),
+        _dense(beta, "beta", ch, f32, dev), _dense(film, "film", 2 * N * ch, f32, dev), yp, yn, yl,
+        _dense(mean, "mean", N * groups, f32, dev), _dense(rstd, "rstd", N * groups, f32, dev), _saved(saved_x, "saved_x", N * L, ch, dev),
+        _saved(saved_y, "saved_y", N * L, ch, dev), stream), "tsdp_group_norm")
 
 
 def group_norm_grad_workspace(dy, groups):
     """Bytes of workspace that group_norm_grad takes for gradients like dy."""
     _, _, _, N, L, ch = _rows(dy, "dy")
-    n = load_library().tsdp_group_norm_grad_workspace(dy.device.index, NormT(_dtype_code(dy, "dy"), N, L, ch, groups, 0, 1e-5))
+    n = load_library().tsdp_group_norm_grad_workspace(dy.get_device(), NormT(_dtype_code(dy, "dy"), N, L, ch, groups, 0, 1e-5))
     if n == 0:
         raise TsdpError(1, "tsdp_group_norm_grad_workspace", "sizes")
     return n
@@ -299,24 +322,17 @@ def group_norm_grad(dy, x, gamma, beta, groups, mean, rstd, dx, dgamma, dbeta, w
     if (x is None) == (saved_x is None):
         raise ValueError("x, saved_x: one of the two expected")
     xp, xn, xl = (None, 0, 0) if x is None else _rows(x, "x", dy)[:3]
-    dp, dn, dl, *_ = _rows(dx, "dx", dy)
-    dev, f32 = dy.device, "torch.float32"
-    shape = NormT(_dtype_code(dy, "dy"), N, L, ch, groups, _act(act), 1.0)
+    dp, dn, dl = _rows(dx, "dx", dy)[:3]
+    dev, f32 = dy.get_device(), _torch().float32
     _status(load_library().tsdp_group_norm_grad(
-        dev.index, shape, p, sn, sl, xp, xn, xl, _saved(saved_x, "saved_x", N * L, ch, dev), _dense(gamma, "gamma", (ch,), f32, dev),
-        _dense(beta, "beta", (ch,), f32, dev), _dense(film, "film", (N, 2 * ch), f32, dev), _dense(mean, "mean", (N, groups), f32, dev),
-        _dense(rstd, "rstd", (N, groups), f32, dev), dp, dn, dl, _dense(dgamma, "dgamma", (ch,), f32, dev),
-        _dense(dbeta, "dbeta", (ch,), f32, dev), _dense(dfilm, "dfilm", (N, 2 * ch), f32, dev), *_workspace(workspace, dev), stream),
-        "tsdp_group_norm_grad")
+        dev, _norm_t(_dtype_code(dy, "dy"), N, L, ch, groups, _act(act), 1.0), p, sn, sl, xp, xn, xl, _saved(saved_x, "saved_x", N * L, ch, dev),
+        _dense(gamma, "gamma", ch, f32, dev), _dense(beta, "beta", ch, f32, dev), _dense(film, "film", 2 * N * ch, f32, dev),
+        _dense(mean, "mean", N * groups, f32, dev), _dense(rstd, "rstd", N * groups, f32, dev), dp, dn, dl,
+        _dense(dgamma, "dgamma", ch, f32, dev), _dense(dbeta, "dbeta", ch, f32, dev), _dense(dfilm, "dfilm", 2 * N * ch, f32, dev),
+        *_workspace(workspace, dev), stream), "tsdp_group_norm_grad")
 
 
-def _workspace(t, device):
-    if t.device != device or not t.is_contiguous():
-        raise ValueError(f"workspace: a contiguous tensor on {device} expected")
-    return t.data_ptr(), t.numel() * t.element_size()
-
-
-def _weight_sizes(dy, taps, length):
+def _weight_sizes(dy, length):
     p, _, sl, _, rows, out = _rows(dy, "dy")
     if dy.dim() != 2:
         raise ValueError(f"dy: [rows, out] expected, got {tuple(dy.shape)}")
@@ -328,8 +344,8 @@ def _weight_sizes(dy, taps, length):
 
 def weight_grad_workspace(dy, channels, taps=1, length=None):
     """Bytes of workspace that weight_grad takes for gradients like dy and `channels` input channels."""
-    _, _, N, L, out = _weight_sizes(dy, taps, length)
-    n = load_library().tsdp_weight_grad_workspace(dy.device.index, _dtype_code(dy, "dy"), N, L, channels, out, taps)
+    _, _, N, L, out = _weight_sizes(dy, length)
+    n = load_library().tsdp_weight_grad_workspace(dy.get_device(), _dtype_code(dy, "dy"), N, L, channels, out, taps)
     if n == 0:
         raise TsdpError(1, "tsdp_weight_grad_workspace", "sizes")
     return n
@@ -338,13 +354,15 @@ def weight_grad_workspace(dy, channels, taps=1, length=None):
 def weight_grad(saved_x, dy, dW, workspace, db=None, length=None, stream=0):
     """dW [taps, in, out] (or [in, out]) and db [out] from dy [rows, out] and the 8-bit copy of the layer's input [rows, in];
     length: rows of a sequence, beyond whose ends a convolution sees zeros (default: all rows are one sequence)."""
-    taps, channels = (1, dW.shape[0]) if dW.dim() == 2 else dW.shape[:2]
-    p, sl, N, L, out = _weight_sizes(dy, taps, length)
-    dev, f32 = dy.device, "torch.float32"
-    shape = (channels, out) if dW.dim() == 2 else (taps, channels, out)
+    shape = dW.shape
+    taps, channels = (1, shape[0]) if len(shape) == 2 else shape[:2]
+    p, sl, N, L, out = _weight_sizes(dy, length)
+    if shape[-1] != out or not 2 <= len(shape) <= 3:
+        raise ValueError(f"dW: [taps, in, {out}] or [in, {out}] expected, got {tuple(shape)}")
+    dev, f32 = dy.get_device(), _torch().float32
     _status(load_library().tsdp_weight_grad(
-        dev.index, _dtype_code(dy, "dy"), _saved(saved_x, "saved_x", N * L, channels, dev), p, sl, N, L, channels, out, taps,
-        _dense(dW, "dW", shape, f32, dev), _dense(db, "db", (out,), f32, dev), *_workspace(workspace, dev), stream), "tsdp_weight_grad")
+        dev, _dtype_code(dy, "dy"), _saved(saved_x, "saved_x", N * L, channels, dev), p, sl, N, L, channels, out, taps,
+        _dense(dW, "dW", taps * channels * out, f32, dev), _dense(db, "db", out, f32, dev), *_workspace(workspace, dev), stream), "tsdp_weight_grad")
 
 
 class Sampler:

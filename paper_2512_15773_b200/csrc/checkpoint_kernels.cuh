@@ -81,38 +81,61 @@ template <typename T, int V> __device__ __forceinline__ void store_values(T* p, 
   }
 }
 
+// Row r = n L + l of a tensor [N, L, C].
+__device__ __forceinline__ long long row_offset(const Rows& x, long long r, int N, int L) {
+  if (N == 1) return r * x.sl;
+  const long long n = r < (1ll << 32) ? (long long)((uint32_t)r / (uint32_t)L) : r / L;      // (a 64-bit division costs as much as the row)
+  return n * x.sn + (r - n * L) * x.sl;
+}
+
 // Eight channels a thread, four neighbouring lanes a block of 32; a row's threads are counted in whole blocks, so that the four lanes of
-// a block sit side by side whatever C is.  A thread keeps its channels and walks the rows.  C % 8 = 0, 16-byte aligned rows.
-constexpr int COPY_THREADS = 256;
+// a block sit side by side whatever C is.  A thread keeps its channels and walks the rows, COPY_ROWS of them asked for before the first is used.
+// C % 8 = 0, 16-byte aligned rows.  Bound by bytes.
+constexpr int COPY_THREADS = 256, COPY_ROWS = 4;
 template <typename T>
 __global__ void __launch_bounds__(COPY_THREADS)
 checkpoint_pack_kernel(Rows x, Copy8 out, int N, int L, int C) {
   pdl_wait();
-  const int units = 4 * copy_blocks(C), per = min(units, COPY_THREADS);      // threads on a row
+  constexpr int W = sizeof(T) / 2;                                           // 16-byte pieces of eight values
+  const int nb = copy_blocks(C), units = 4 * nb, per = min(units, COPY_THREADS);      // threads on a row
   const int lanes = COPY_THREADS / per, lane = threadIdx.x / per;
-  const long long rows = (long long)N * L;
-  for (long long r0 = (long long)blockIdx.x * lanes; r0 < rows; r0 += (long long)gridDim.x * lanes) {
-    const long long r = r0 + lane;
-    const bool row_in = lane < lanes && r < rows;
-    const long long n = L == 1 ? r : r / L;
-    const T* row = reinterpret_cast<const T*>(x.p) + n * x.sn + (r - n * L) * x.sl;
+  const long long rows = (long long)N * L, step = (long long)gridDim.x * lanes;
+  for (long long r0 = (long long)blockIdx.x * lanes; r0 < rows; r0 += COPY_ROWS * step) {
     for (int u0 = 0; u0 < units; u0 += per) {
       const int u = u0 + threadIdx.x - lane * per, c = 8 * u;
-      const bool in = row_in && c < C;
-      float v[8] = {};
-      if (in) {
-        load_values<T, 16 / sizeof(T)>(row + c, v);
-        if constexpr (sizeof(T) == 4) load_values<T, 4>(row + c + 4, v + 4);
-      }
-      uint32_t top = 0;
+      uint4 v[COPY_ROWS][W];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) top = max(top, __float_as_uint(v[i]) & 0x7fffffffu);
-      top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
-      top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
-      const uint32_t b = copy_byte(top);
-      const float inv = copy_inv_step(b);
-      if (in) *reinterpret_cast<uint2*>(out.q + r * C + c) = make_uint2(copy_q4(v, inv, b), copy_q4(v + 4, inv, b));
-      if (in && (u & 3) == 0) out.b[r * copy_blocks(C) + (u >> 2)] = (unsigned char)b;
+      for (int k = 0; k < COPY_ROWS; ++k) {
+        const long long r = r0 + k * step + lane;
+        const bool in = lane < lanes && r < rows && c < C;
+        const uint4* p = reinterpret_cast<const uint4*>(reinterpret_cast<const T*>(x.p) + (in ? row_offset(x, r, N, L) : 0) + c);
+#pragma unroll
+        for (int w = 0; w < W; ++w) v[k][w] = in ? p[w] : make_uint4(0u, 0u, 0u, 0u);
+      }
+#pragma unroll
+      for (int k = 0; k < COPY_ROWS; ++k) {
+        const long long r = r0 + k * step + lane;
+        uint32_t top;
+        float2 f[4];
+        if constexpr (sizeof(T) == 2) {
+          top = copy_top_bf16(v[k][0]);
+          const uint32_t w[4] = {v[k][0].x, v[k][0].y, v[k][0].z, v[k][0].w};
+#pragma unroll
+          for (int i = 0; i < 4; ++i) f[i] = make_float2(__uint_as_float(w[i] << 16), __uint_as_float(w[i] & 0xffff0000u));
+        } else {
+          top = max(copy_top_fp32(v[k][0]), copy_top_fp32(v[k][W - 1]));
+          f[0] = make_float2(__uint_as_float(v[k][0].x), __uint_as_float(v[k][0].y)); f[1] = make_float2(__uint_as_float(v[k][0].z), __uint_as_float(v[k][0].w));
+          f[2] = make_float2(__uint_as_float(v[k][W - 1].x), __uint_as_float(v[k][W - 1].y)); f[3] = make_float2(__uint_as_float(v[k][W - 1].z), __uint_as_float(v[k][W - 1].w));
+        }
+        top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
+        top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
+        const uint32_t b = copy_byte(top);
+        const float inv = copy_inv_step(b);
+        if (lane < lanes && r < rows && c < C) {
+          *reinterpret_cast<uint2*>(out.q + r * C + c) = make_uint2(copy_q4(f[0], f[1], inv, b), copy_q4(f[2], f[3], inv, b));
+          if ((u & 3) == 0) out.b[r * nb + (u >> 2)] = (unsigned char)b;
+        }
+      }
     }
   }
 }
@@ -125,10 +148,10 @@ checkpoint_pack_any_kernel(Rows x, Copy8 out, int N, int L, int C) {
   const int nb = copy_blocks(C), lane = threadIdx.x & 31;
   const long long blocks = (long long)N * L * nb;
   for (long long i = (long long)blockIdx.x * (COPY_THREADS / 32) + (threadIdx.x >> 5); i < blocks; i += (long long)gridDim.x * (COPY_THREADS / 32)) {
-    const long long r = i / nb, n = r / L;
+    const long long r = i / nb;
     const int c = (int)(i - r * nb) * 32 + lane;
     float v = 0.f;
-    if (c < C) v = to_f(reinterpret_cast<const T*>(x.p)[n * x.sn + (r - n * L) * x.sl + c]);
+    if (c < C) v = to_f(reinterpret_cast<const T*>(x.p)[row_offset(x, r, N, L) + c]);
     const uint32_t b = copy_byte(__reduce_max_sync(0xffffffffu, __float_as_uint(v) & 0x7fffffffu));
     if (c < C) out.q[r * C + c] = (signed char)copy_q(v, copy_inv_step(b), b);
     if (lane == 0) out.b[i] = (unsigned char)b;
@@ -139,21 +162,33 @@ template <typename T>
 __global__ void __launch_bounds__(COPY_THREADS)
 checkpoint_unpack_kernel(Copy8 in, Rows x, int N, int L, int C) {
   pdl_wait();
-  const int units = C >> 3, per = min(units, COPY_THREADS);
+  const int nb = copy_blocks(C), units = C >> 3, per = min(units, COPY_THREADS);
   const int lanes = COPY_THREADS / per, lane = threadIdx.x / per;
-  const long long rows = (long long)N * L;
+  const long long rows = (long long)N * L, step = (long long)gridDim.x * lanes;
   if (lane >= lanes) return;
-  for (long long r = (long long)blockIdx.x * lanes + lane; r < rows; r += (long long)gridDim.x * lanes) {
-    const long long n = L == 1 ? r : r / L;
-    T* row = reinterpret_cast<T*>(x.p) + n * x.sn + (r - n * L) * x.sl;
+  for (long long r0 = (long long)blockIdx.x * lanes + lane; r0 < rows; r0 += COPY_ROWS * step) {
     for (int u = threadIdx.x - lane * per; u < units; u += per) {
-      const uint2 w = *reinterpret_cast<const uint2*>(in.q + r * C + 8 * u);
-      const float step = copy_step(in.b[r * copy_blocks(C) + (u >> 2)]);
-      float v[8];
+      uint2 w[COPY_ROWS];
+      uint32_t b[COPY_ROWS];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) { v[i] = copy_value(w.x, i, step); v[4 + i] = copy_value(w.y, i, step); }
-      store_values<T, 16 / sizeof(T)>(row + 8 * u, v);
-      if constexpr (sizeof(T) == 4) store_values<T, 4>(row + 8 * u + 4, v + 4);
+      for (int k = 0; k < COPY_ROWS; ++k) {
+        const long long r = r0 + k * step;
+        w[k] = make_uint2(0u, 0u);
+        b[k] = 0u;
+        if (r < rows) { w[k] = *reinterpret_cast<const uint2*>(in.q + r * C + 8 * u); b[k] = in.b[r * nb + (u >> 2)]; }
+      }
+#pragma unroll
+      for (int k = 0; k < COPY_ROWS; ++k) {
+        const long long r = r0 + k * step;
+        if (r >= rows) break;
+        const float st = copy_step(b[k]);
+        float v[8];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) { v[i] = copy_value(w[k].x, i, st); v[4 + i] = copy_value(w[k].y, i, st); }
+        T* p = reinterpret_cast<T*>(x.p) + row_offset(x, r, N, L) + 8 * u;
+        store_values<T, 16 / sizeof(T)>(p, v);
+        if constexpr (sizeof(T) == 4) store_values<T, 4>(p + 4, v + 4);
+      }
     }
   }
 }
@@ -165,9 +200,9 @@ checkpoint_unpack_any_kernel(Copy8 in, Rows x, int N, int L, int C) {
   const int nb = copy_blocks(C), lane = threadIdx.x & 31;
   const long long blocks = (long long)N * L * nb;
   for (long long i = (long long)blockIdx.x * (COPY_THREADS / 32) + (threadIdx.x >> 5); i < blocks; i += (long long)gridDim.x * (COPY_THREADS / 32)) {
-    const long long r = i / nb, n = r / L;
+    const long long r = i / nb;
     const int c = (int)(i - r * nb) * 32 + lane;
-    if (c < C) reinterpret_cast<T*>(x.p)[n * x.sn + (r - n * L) * x.sl + c] = from_f<T>((float)in.q[r * C + c] * copy_step(in.b[i]));
+    if (c < C) reinterpret_cast<T*>(x.p)[row_offset(x, r, N, L) + c] = from_f<T>((float)in.q[r * C + c] * copy_step(in.b[i]));
   }
 }
 

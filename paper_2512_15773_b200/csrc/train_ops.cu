@@ -107,10 +107,8 @@ cudaError_t pack(const Rows& x, Copy8 out, int N, int L, int C, int sms, cudaStr
     const long long blocks = min((rows + lanes - 1) / lanes, (long long)sms * 32);
     return launch(checkpoint_pack_kernel<T>, (unsigned)blocks, COPY_THREADS, 1, 0, s, x, out, N, L, C);
   }
-  {
-    const long long blocks = min((rows * copy_blocks(C) + 7) / 8, (long long)sms * 64);
-    return launch(checkpoint_pack_any_kernel<T>, (unsigned)blocks, COPY_THREADS, 1, 0, s, x, out, N, L, C);
-  }
+  const long long blocks = min((rows * copy_blocks(C) + 7) / 8, (long long)sms * 64);
+  return launch(checkpoint_pack_any_kernel<T>, (unsigned)blocks, COPY_THREADS, 1, 0, s, x, out, N, L, C);
 }
 
 template <typename T>
@@ -122,10 +120,8 @@ cudaError_t unpack(Copy8 in, const Rows& x, int N, int L, int C, int sms, cudaSt
     const long long blocks = min((rows + lanes - 1) / lanes, (long long)sms * 32);
     return launch(checkpoint_unpack_kernel<T>, (unsigned)blocks, COPY_THREADS, 1, 0, s, in, x, N, L, C);
   }
-  {
-    const long long blocks = min((rows * copy_blocks(C) + 7) / 8, (long long)sms * 64);
-    return launch(checkpoint_unpack_any_kernel<T>, (unsigned)blocks, COPY_THREADS, 1, 0, s, in, x, N, L, C);
-  }
+  const long long blocks = min((rows * copy_blocks(C) + 7) / 8, (long long)sms * 64);
+  return launch(checkpoint_unpack_any_kernel<T>, (unsigned)blocks, COPY_THREADS, 1, 0, s, in, x, N, L, C);
 }
 
 // ---------------------------------------------------------------------------------------------------------- GroupNorm

@@ -83,7 +83,12 @@ def test_binding_refuses_what_the_library_cannot_see():
     assert q.shape == (3, 70) and s.shape == (3, 3) and q.dtype == torch.int8 and s.dtype == torch.uint8
     with pytest.raises(ValueError, match="act"):
         binding._act("relu")
-    with pytest.raises(ValueError, match="scales"):
-        binding._saved((q, s[:, :2].contiguous()), "saved", 3, 70, q.device)
-    with pytest.raises(ValueError, match="contiguous"):
-        binding._dense(x.transpose(0, 1), "x", (4, 2, 64), "torch.float32", x.device)
+    cpu = x.get_device()
+    with pytest.raises(ValueError, match="scale"):
+        binding._saved((q, s[:, :2].contiguous()), "saved", 3, 70, cpu)
+    with pytest.raises(ValueError, match="channels"):
+        binding._saved((q, s), "saved", 7, 30, cpu)
+    with pytest.raises(ValueError, match="without gaps"):
+        binding._dense(x.transpose(0, 1), "x", x.numel(), torch.float32, cpu)
+    with pytest.raises(ValueError, match="x: 512 values"):
+        binding._dense(x, "x", 512, torch.bfloat16, cpu)

@@ -30,31 +30,60 @@ __device__ __forceinline__ uint32_t copy_q(float x, float inv, uint32_t b) {
   if (b == 248u) s = fminf(fmaxf(s, -127.f), 127.f);
   return b == 255u ? 0u : __float_as_uint(s + 12582912.f) & 0xffu;
 }
-// Four of them in a word, two products and two sums at a time.
-__device__ __forceinline__ uint32_t copy_q4(float2 x0, float2 x1, float inv, uint32_t b) {
-  const float2 k = make_float2(inv, inv), magic = make_float2(12582912.f, 12582912.f);
-  x0 = __fmul2_rn(x0, k); x1 = __fmul2_rn(x1, k);
-  if (b >= 248u) {                             // (rare: the largest magnitudes of fp32, and what is not finite)
-    if (b == 255u) return 0u;
-    x0.x = fminf(fmaxf(x0.x, -127.f), 127.f); x0.y = fminf(fmaxf(x0.y, -127.f), 127.f);
-    x1.x = fminf(fmaxf(x1.x, -127.f), 127.f); x1.y = fminf(fmaxf(x1.y, -127.f), 127.f);
-  }
-  x0 = __fadd2_rn(x0, magic); x1 = __fadd2_rn(x1, magic);
+// Four of them in a word.  (b >= 248 is rare: the largest magnitudes of fp32, and what is not finite.)
+__device__ __forceinline__ uint32_t copy_bytes(float2 x0, float2 x1) {
   return __byte_perm(__byte_perm(__float_as_uint(x0.x), __float_as_uint(x0.y), 0x0040), __byte_perm(__float_as_uint(x1.x), __float_as_uint(x1.y), 0x0040), 0x5410);
+}
+__device__ __forceinline__ uint32_t copy_q4_top(float2 x0, float2 x1, float inv, uint32_t b) {
+  const uint32_t q[4] = {copy_q(x0.x, inv, b), copy_q(x0.y, inv, b), copy_q(x1.x, inv, b), copy_q(x1.y, inv, b)};
+  return q[0] | q[1] << 8 | q[2] << 16 | q[3] << 24;
+}
+__device__ __forceinline__ uint32_t copy_q4(float2 x0, float2 x1, float inv, uint32_t b) {
+  if (b >= 248u) return copy_q4_top(x0, x1, inv, b);
+  const float2 k = make_float2(inv, inv), magic = make_float2(12582912.f, 12582912.f);
+  return copy_bytes(__ffma2_rn(x0, k, magic), __ffma2_rn(x1, k, magic));
+}
+__device__ __forceinline__ uint2 copy_q8(const float2* x, float inv, uint32_t b) {
+  if (b >= 248u) return make_uint2(copy_q4_top(x[0], x[1], inv, b), copy_q4_top(x[2], x[3], inv, b));
+  const float2 k = make_float2(inv, inv), magic = make_float2(12582912.f, 12582912.f);
+  return make_uint2(copy_bytes(__ffma2_rn(x[0], k, magic), __ffma2_rn(x[1], k, magic)), copy_bytes(__ffma2_rn(x[2], k, magic), __ffma2_rn(x[3], k, magic)));
 }
 __device__ __forceinline__ uint32_t copy_q4(const float* x, float inv, uint32_t b) {
   return copy_q4(make_float2(x[0], x[1]), make_float2(x[2], x[3]), inv, b);
 }
-// Largest magnitude (as bits) of eight bf16 values, of four fp32 ones.
-__device__ __forceinline__ uint32_t copy_top_bf16(uint4 u) {
-  const uint32_t m = __vmaxu2(__vmaxu2(u.x & 0x7fff7fffu, u.y & 0x7fff7fffu), __vmaxu2(u.z & 0x7fff7fffu, u.w & 0x7fff7fffu));
+// Largest magnitude (as bits) of eight bf16 values over `lanes` neighbouring lanes, two at a time and a NaN above all; of four fp32 ones.
+template <int LANES> __device__ __forceinline__ uint32_t copy_top_bf16(uint4 u) {
+  auto larger = [](uint32_t a, uint32_t b) {
+    const __nv_bfloat162 m = __hmax2_nan(*reinterpret_cast<const __nv_bfloat162*>(&a), *reinterpret_cast<const __nv_bfloat162*>(&b));
+    return *reinterpret_cast<const uint32_t*>(&m);
+  };
+  uint32_t m = larger(larger(u.x & 0x7fff7fffu, u.y & 0x7fff7fffu), larger(u.z & 0x7fff7fffu, u.w & 0x7fff7fffu));
+#pragma unroll
+  for (int i = 1; i < LANES; i *= 2) m = larger(m, __shfl_xor_sync(0xffffffffu, m, i));
+  m &= 0x7fff7fffu;
   return max(m << 16, m & 0xffff0000u);
 }
 __device__ __forceinline__ uint32_t copy_top_fp32(uint4 u) {
   return max(max(u.x & 0x7fffffffu, u.y & 0x7fffffffu), max(u.z & 0x7fffffffu, u.w & 0x7fffffffu));
 }
-__device__ __forceinline__ float copy_value(uint32_t word, int i, float step) {
-  return (float)(signed char)(word >> (8 * i)) * step;
+// Values 2 i and 2 i + 1 of four in a word, without their step.  The byte with its sign bit turned over is q + 128, put behind the exponent
+// of 2^23 it counts there by ones: a permutation and a subtraction, where the conversion instruction runs at an eighth of the rate.
+__device__ __forceinline__ float2 copy_ints(uint32_t word, int i) {
+  word ^= 0x80808080u;
+  return __fadd2_rn(make_float2(__uint_as_float(__byte_perm(word, 0x4b000000u, i ? 0x7542 : 0x7540)), __uint_as_float(__byte_perm(word, 0x4b000000u, i ? 0x7543 : 0x7541))),
+                    make_float2(-8388736.f, -8388736.f));
+}
+// The same with their step as two bf16 values: the magnitude's seven bits on 128 (bf16 counts by ones there), 128 or 256 taken off by the
+// sign bit; both exact, and so is the product with a power of two.
+__device__ __forceinline__ uint32_t copy_pair(uint32_t word, int i, __nv_bfloat162 step) {
+  const uint32_t p = __byte_perm(word, 0u, i ? 0x4342 : 0x4140);
+  const uint32_t hi = (p & 0x007f007fu) | 0x43004300u, lo = (p & 0x00800080u) | 0xc300c300u;
+  const __nv_bfloat162 v = __hmul2(__hadd2(*reinterpret_cast<const __nv_bfloat162*>(&hi), *reinterpret_cast<const __nv_bfloat162*>(&lo)), step);
+  return *reinterpret_cast<const uint32_t*>(&v);
+}
+__device__ __forceinline__ __nv_bfloat162 copy_step2(uint32_t b) {           // the byte as the exponent of two bf16 values
+  const uint32_t s = b == 255u ? 0x7fc07fc0u : b * 0x00800080u;
+  return *reinterpret_cast<const __nv_bfloat162*>(&s);
 }
 
 // V consecutive values as fp32; V * sizeof(T) = 16 bytes, or one value.
@@ -100,25 +129,32 @@ checkpoint_pack_kernel(Rows x, Copy8 out, int N, int L, int C) {
   const int nb = copy_blocks(C), units = 4 * nb, per = min(units, COPY_THREADS);      // threads on a row
   const int lanes = COPY_THREADS / per, lane = threadIdx.x / per;
   const long long rows = (long long)N * L, step = (long long)gridDim.x * lanes;
+  const long long q_step = step * C, b_step = step * nb, x_step = step * x.sl;      // (x: of one sequence)
   for (long long r0 = (long long)blockIdx.x * lanes; r0 < rows; r0 += COPY_ROWS * step) {
     for (int u0 = 0; u0 < units; u0 += per) {
       const int u = u0 + threadIdx.x - lane * per, c = 8 * u;
+      const bool mine = lane < lanes && c < C;
+      const long long r = r0 + lane;
+      const T* p0 = reinterpret_cast<const T*>(x.p) + (N == 1 ? r * x.sl : 0) + c;
       uint4 v[COPY_ROWS][W];
 #pragma unroll
       for (int k = 0; k < COPY_ROWS; ++k) {
-        const long long r = r0 + k * step + lane;
-        const bool in = lane < lanes && r < rows && c < C;
-        const uint4* p = reinterpret_cast<const uint4*>(reinterpret_cast<const T*>(x.p) + (in ? row_offset(x, r, N, L) : 0) + c);
 #pragma unroll
-        for (int w = 0; w < W; ++w) v[k][w] = in ? p[w] : make_uint4(0u, 0u, 0u, 0u);
+        for (int w = 0; w < W; ++w) v[k][w] = make_uint4(0u, 0u, 0u, 0u);
+        if (mine && r + k * step < rows) {
+          const uint4* p = reinterpret_cast<const uint4*>(N == 1 ? p0 + k * x_step : p0 + row_offset(x, r + k * step, N, L));
+#pragma unroll
+          for (int w = 0; w < W; ++w) v[k][w] = p[w];
+        }
       }
+      signed char* q0 = out.q + r * C + c;
+      unsigned char* b0 = out.b + r * nb + (u >> 2);
 #pragma unroll
       for (int k = 0; k < COPY_ROWS; ++k) {
-        const long long r = r0 + k * step + lane;
         uint32_t top;
         float2 f[4];
         if constexpr (sizeof(T) == 2) {
-          top = copy_top_bf16(v[k][0]);
+          top = copy_top_bf16<4>(v[k][0]);
           const uint32_t w[4] = {v[k][0].x, v[k][0].y, v[k][0].z, v[k][0].w};
 #pragma unroll
           for (int i = 0; i < 4; ++i) f[i] = make_float2(__uint_as_float(w[i] << 16), __uint_as_float(w[i] & 0xffff0000u));
@@ -126,14 +162,14 @@ checkpoint_pack_kernel(Rows x, Copy8 out, int N, int L, int C) {
           top = max(copy_top_fp32(v[k][0]), copy_top_fp32(v[k][W - 1]));
           f[0] = make_float2(__uint_as_float(v[k][0].x), __uint_as_float(v[k][0].y)); f[1] = make_float2(__uint_as_float(v[k][0].z), __uint_as_float(v[k][0].w));
           f[2] = make_float2(__uint_as_float(v[k][W - 1].x), __uint_as_float(v[k][W - 1].y)); f[3] = make_float2(__uint_as_float(v[k][W - 1].z), __uint_as_float(v[k][W - 1].w));
+          top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
+          top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
         }
-        top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
-        top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
         const uint32_t b = copy_byte(top);
         const float inv = copy_inv_step(b);
-        if (lane < lanes && r < rows && c < C) {
-          *reinterpret_cast<uint2*>(out.q + r * C + c) = make_uint2(copy_q4(f[0], f[1], inv, b), copy_q4(f[2], f[3], inv, b));
-          if ((u & 3) == 0) out.b[r * nb + (u >> 2)] = (unsigned char)b;
+        if (mine && r + k * step < rows) {
+          *reinterpret_cast<uint2*>(q0 + k * q_step) = copy_q8(f, inv, b);
+          if ((u & 3) == 0) b0[k * b_step] = (unsigned char)b;
         }
       }
     }
@@ -166,28 +202,40 @@ checkpoint_unpack_kernel(Copy8 in, Rows x, int N, int L, int C) {
   const int lanes = COPY_THREADS / per, lane = threadIdx.x / per;
   const long long rows = (long long)N * L, step = (long long)gridDim.x * lanes;
   if (lane >= lanes) return;
-  for (long long r0 = (long long)blockIdx.x * lanes + lane; r0 < rows; r0 += COPY_ROWS * step) {
+  const long long q_step = step * C, b_step = step * nb, x_step = step * x.sl;      // (x: of one sequence)
+  for (long long r = (long long)blockIdx.x * lanes + lane; r < rows; r += COPY_ROWS * step) {
     for (int u = threadIdx.x - lane * per; u < units; u += per) {
+      const signed char* q0 = in.q + r * C + 8 * u;
+      const unsigned char* b0 = in.b + r * nb + (u >> 2);
       uint2 w[COPY_ROWS];
       uint32_t b[COPY_ROWS];
 #pragma unroll
       for (int k = 0; k < COPY_ROWS; ++k) {
-        const long long r = r0 + k * step;
         w[k] = make_uint2(0u, 0u);
         b[k] = 0u;
-        if (r < rows) { w[k] = *reinterpret_cast<const uint2*>(in.q + r * C + 8 * u); b[k] = in.b[r * nb + (u >> 2)]; }
+        if (r + k * step < rows) { w[k] = *reinterpret_cast<const uint2*>(q0 + k * q_step); b[k] = b0[k * b_step]; }
       }
+      T* p0 = reinterpret_cast<T*>(x.p) + (N == 1 ? r * x.sl : 0) + 8 * u;
 #pragma unroll
       for (int k = 0; k < COPY_ROWS; ++k) {
-        const long long r = r0 + k * step;
-        if (r >= rows) break;
-        const float st = copy_step(b[k]);
-        float v[8];
+        uint4 v[sizeof(T) / 2];
+        if constexpr (sizeof(T) == 2) {
+          const __nv_bfloat162 st = copy_step2(b[k]);
+          v[0] = make_uint4(copy_pair(w[k].x, 0, st), copy_pair(w[k].x, 1, st), copy_pair(w[k].y, 0, st), copy_pair(w[k].y, 1, st));
+        } else {
+          const float2 st = make_float2(copy_step(b[k]), copy_step(b[k]));
 #pragma unroll
-        for (int i = 0; i < 4; ++i) { v[i] = copy_value(w[k].x, i, st); v[4 + i] = copy_value(w[k].y, i, st); }
-        T* p = reinterpret_cast<T*>(x.p) + row_offset(x, r, N, L) + 8 * u;
-        store_values<T, 16 / sizeof(T)>(p, v);
-        if constexpr (sizeof(T) == 4) store_values<T, 4>(p + 4, v + 4);
+          for (int h = 0; h < 2; ++h) {
+            const uint32_t word = h ? w[k].y : w[k].x;
+            const float2 f0 = __fmul2_rn(copy_ints(word, 0), st), f1 = __fmul2_rn(copy_ints(word, 1), st);
+            v[h] = make_uint4(__float_as_uint(f0.x), __float_as_uint(f0.y), __float_as_uint(f1.x), __float_as_uint(f1.y));
+          }
+        }
+        if (r + k * step < rows) {
+          uint4* p = reinterpret_cast<uint4*>(N == 1 ? p0 + k * x_step : p0 + row_offset(x, r + k * step, N, L));
+#pragma unroll
+          for (int h = 0; h < (int)sizeof(T) / 2; ++h) p[h] = v[h];
+        }
       }
     }
   }

@@ -38,9 +38,10 @@ template <bool GRAD> __device__ __forceinline__ void act_pair(int act, float2 z,
   if (act == ACT_MISH) {
     const float2 zc = make_float2(act_min(z.x, 20.f), act_min(z.y, 20.f)), u = exp2_of(zc, ACT_LOG2E), w = __fadd2_rn(u, two(1.f));
     const float2 r = rcp_of(__ffma2_rn(w, w, two(1.f)));
-    const float2 t = __fmul2_rn(__ffma2_rn(u, u, __fadd2_rn(u, u)), r);
+    // (the values themselves to their last digits; with the derivative, which is of the order of 1, to those of 1)
+    const float2 t = GRAD ? __ffma2_rn(r, two(-2.f), two(1.f)) : __fmul2_rn(__ffma2_rn(u, u, __fadd2_rn(u, u)), r);
     a = __fmul2_rn(z, t);
-    if (GRAD) d = __ffma2_rn(__fmul2_rn(__fmul2_rn(zc, two(4.f)), r), __fmul2_rn(__fmul2_rn(u, w), r), t);
+    if (GRAD) d = __ffma2_rn(__fmul2_rn(zc, __fmul2_rn(__fmul2_rn(r, r), __fmul2_rn(u, w))), two(4.f), t);
   } else if (act == ACT_SILU) {
     const float2 s = rcp_of(__fadd2_rn(exp2_of(z, -ACT_LOG2E), two(1.f)));
     a = __fmul2_rn(z, s);
@@ -279,7 +280,10 @@ __device__ __forceinline__ void load_x(const NormArgs& g, int n, int l, int c, f
       if constexpr (V == 8) { const uint2 u = *reinterpret_cast<const uint2*>(q); w[0] = u.x; w[1] = u.y; }
       else w[0] = *reinterpret_cast<const uint32_t*>(q);
 #pragma unroll
-      for (int i = 0; i < V; ++i) v[i] = copy_value(w[i >> 2], i & 3, step);
+      for (int i = 0; i < V; i += 2) {
+        const float2 f = copy_ints(w[i >> 2], (i >> 1) & 1);
+        v[i] = f.x * step; v[i + 1] = f.y * step;
+      }
     }
   }
 }

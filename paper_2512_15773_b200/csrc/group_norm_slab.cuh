@@ -49,28 +49,31 @@ template <typename T, int V> __device__ __forceinline__ void piece_values(const 
   for (int i = 0; i < V / 2; ++i) {
     if constexpr (sizeof(T) == 2) v[i] = make_float2(__uint_as_float(r.w[i] << 16), __uint_as_float(r.w[i] & 0xffff0000u));
     else if constexpr (sizeof(T) == 4) v[i] = make_float2(__uint_as_float(r.w[2 * i]), __uint_as_float(r.w[2 * i + 1]));
-    else {
+    else {                                     // (by the conversion instruction: its pipe has room here, that of the permutations has none: 70 us, not 78)
       const uint32_t u = r.w[i >> 1] >> (16 * (i & 1));
       v[i] = make_float2((float)(signed char)u, (float)(signed char)(u >> 8));
     }
   }
 }
-// The 8-bit copy of 16 bytes of a row; the lanes of a block of 32 sit side by side in a warp.  top = 0 where there is no row.
-template <typename T> __device__ __forceinline__ void write_copy(const Copy8& o, uint4 u, bool row, long long r, int C, int c) {
+// The 8-bit copy of 16 bytes of a row; the lanes of a block of 32 sit side by side in a warp, all of them with the row or none.
+// q: where its bytes go, b: where the block's byte goes (by its first lane).
+template <typename T> __device__ __forceinline__ void write_copy(signed char* q, unsigned char* b, uint4 u, bool row, bool first) {
   constexpr int V = 16 / sizeof(T);
-  uint32_t top = sizeof(T) == 2 ? copy_top_bf16(u) : copy_top_fp32(u);
-  if (!row) top = 0;
+  uint32_t top;
+  if constexpr (V == 8) top = copy_top_bf16<4>(u);
+  else {
+    top = copy_top_fp32(u);
 #pragma unroll
-  for (int i = 1; i < 32 / V; i *= 2) top = max(top, __shfl_xor_sync(0xffffffffu, top, i));
-  const uint32_t b = copy_byte(top);
-  const float is = copy_inv_step(b);
+    for (int i = 1; i < 8; i *= 2) top = max(top, __shfl_xor_sync(0xffffffffu, top, i));
+  }
+  const uint32_t byte = copy_byte(top);
+  const float is = copy_inv_step(byte);
   float2 w[V / 2];
   unpack16<T, V>(u, w);
   if (row) {
-    signed char* q = o.q + r * C + c;
-    if constexpr (V == 8) *reinterpret_cast<uint2*>(q) = make_uint2(copy_q4(w[0], w[1], is, b), copy_q4(w[2], w[3], is, b));
-    else *reinterpret_cast<uint32_t*>(q) = copy_q4(w[0], w[1], is, b);
-    if ((c & 31) == 0) o.b[r * copy_blocks(C) + (c >> 5)] = (unsigned char)b;
+    if constexpr (V == 8) *reinterpret_cast<uint2*>(q) = copy_q8(w, is, byte);
+    else *reinterpret_cast<uint32_t*>(q) = copy_q4(w[0], w[1], is, byte);
+    if (first) *b = (unsigned char)byte;
   }
 }
 // f(the activation as a constant): the choice is made once, not for every value.
@@ -222,8 +225,9 @@ group_norm_slab_kernel(NormArgs g) {
         const uint4 out = pack16<T, V>(y);
         if (row) *reinterpret_cast<uint4*>(reinterpret_cast<T*>(g.y.p) + n * g.y.sn + l * g.y.sl + c) = out;
         const long long r = (long long)n * g.L + l;
-        if (g.cx.q) write_copy<T>(g.cx, raw[j], row, r, g.C, c);
-        if (g.cy.q) write_copy<T>(g.cy, out, row, r, g.C, c);
+        const long long qo = r * g.C + c, bo = r * copy_blocks(g.C) + (c >> 5);
+        if (g.cx.q) write_copy<T>(g.cx.q + qo, g.cx.b + bo, raw[j], row, (c & 31) == 0);
+        if (g.cy.q) write_copy<T>(g.cy.q + qo, g.cy.b + bo, row ? out : make_uint4(0u, 0u, 0u, 0u), row, (c & 31) == 0);
       }
     });
   }

@@ -9,100 +9,6 @@ namespace tsdp {
 
 constexpr int GN_WARP_THREADS = 256;
 
-template <typename T, int ITEMS>
-__global__ void __launch_bounds__(GN_WARP_THREADS, 2)
-group_norm_warp_kernel(NormArgs g) {
-  constexpr int V = 16 / sizeof(T), P = V / 2;
-  const int gw = blockIdx.x * (GN_WARP_THREADS / 32) + (threadIdx.x >> 5), wl = threadIdx.x & 31;
-  const int grp = gw % g.groups, split = gw / g.groups;
-  pdl_wait();
-  if (split >= g.splits) return;
-  const int cg = g.C / g.groups, gcols = cg / V, R = 32 / gcols;             // lanes on a position, positions at a time
-  const int lr = wl / gcols, c = grp * cg + (wl - lr * gcols) * V;
-  float2 ga[P], be[P];
-#pragma unroll
-  for (int i = 0; i < P; ++i) {
-    ga[i] = *reinterpret_cast<const float2*>(g.gamma + c + 2 * i);
-    be[i] = *reinterpret_cast<const float2*>(g.beta + c + 2 * i);
-  }
-  const float inv = 1.f / ((float)g.L * cg);
-  uint4 next[ITEMS];
-  auto fetch = [&](int n) {
-    const T* x = reinterpret_cast<const T*>(g.x.p) + n * g.x.sn + c;
-#pragma unroll
-    for (int j = 0; j < ITEMS; ++j) {
-      const int l = lr + j * R;
-      next[j] = make_uint4(0u, 0u, 0u, 0u);
-      if (n < g.N && l < g.L) next[j] = *reinterpret_cast<const uint4*>(x + l * g.x.sl);
-    }
-  };
-  fetch(split);
-  for (int n = split; n < g.N; n += g.splits) {
-    uint4 raw[ITEMS];
-#pragma unroll
-    for (int j = 0; j < ITEMS; ++j) raw[j] = next[j];
-    float2 fs[P], fb[P];
-#pragma unroll
-    for (int i = 0; i < P; ++i) {
-      fs[i] = two(1.f); fb[i] = two(0.f);
-      if (g.film) {
-        fs[i] = *reinterpret_cast<const float2*>(g.film + (long long)n * 2 * g.C + c + 2 * i);
-        fb[i] = *reinterpret_cast<const float2*>(g.film + ((long long)n * 2 + 1) * g.C + c + 2 * i);
-      }
-    }
-    fetch(n + g.splits);
-    float2 t2 = two(0.f);
-#pragma unroll
-    for (int j = 0; j < ITEMS; ++j) {
-      float2 v[P];
-      unpack16<T, V>(raw[j], v);
-#pragma unroll
-      for (int i = 0; i < P; ++i) t2 = __fadd2_rn(t2, v[i]);       // (zeros where there is no row)
-    }
-    const float mean = warp_sum(t2.x + t2.y) * inv;
-    t2 = two(0.f);
-#pragma unroll
-    for (int j = 0; j < ITEMS; ++j) {
-      if (lr + j * R < g.L) {
-        float2 v[P];
-        unpack16<T, V>(raw[j], v);
-#pragma unroll
-        for (int i = 0; i < P; ++i) { v[i] = __fadd2_rn(v[i], two(-mean)); t2 = __ffma2_rn(v[i], v[i], t2); }
-      }
-    }
-    const float rstd = rsqrtf(warp_sum(t2.x + t2.y) * inv + g.eps);
-    if (wl == 0) {
-      if (g.mean) g.mean[(long long)n * g.groups + grp] = mean;
-      if (g.rstd) g.rstd[(long long)n * g.groups + grp] = rstd;
-    }
-    T* y0 = reinterpret_cast<T*>(g.y.p) + n * g.y.sn + c;
-    with_act(g.act, [&](auto act) {
-#pragma unroll
-      for (int j = 0; j < ITEMS; ++j) {
-        const int l = lr + j * R;
-        const bool row = l < g.L;
-        float2 v[P], y[P];
-        unpack16<T, V>(raw[j], v);
-#pragma unroll
-        for (int i = 0; i < P; ++i) {
-          const float2 z = __ffma2_rn(__fmul2_rn(__fadd2_rn(v[i], two(-mean)), two(rstd)), ga[i], be[i]);
-          float2 a, d;
-          act_pair<false>(decltype(act)::value, z, a, d);
-          y[i] = __ffma2_rn(a, fs[i], fb[i]);
-        }
-        const uint4 out = pack16<T, V>(y);
-        if (row) *reinterpret_cast<uint4*>(y0 + l * g.y.sl) = out;
-        const long long r = (long long)n * g.L + l;
-        if (g.cx.q) write_copy<T>(g.cx, raw[j], row, r, g.C, c);
-        if (g.cy.q) write_copy<T>(g.cy, out, row, r, g.C, c);
-      }
-    });
-  }
-}
-
-// Backward.  dz stays in registers between the sums and dx; dy and x (or its copy) come by cp.async into memory of the warp's own, one
-// sequence ahead, and are read from there as often as they are needed: with them in registers too the kernel spills.  The steps of an
-// 8-bit copy (L cg / 32 bytes) come one to a lane.
 __device__ __forceinline__ void cp_async16(uint32_t dst, const void* src) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
 }
@@ -111,7 +17,121 @@ __device__ __forceinline__ void warp_rows(uint32_t dst, const char* src, long lo
   const int shift = 31 - __clz(bytes);
   for (int o = wl * 16; o < rows * bytes; o += 512) cp_async16(dst + o, src + (o >> shift) * pitch + (o & (bytes - 1)));
 }
+// Rows that a stage has room for and a sequence does not have stay zero: they are worked on like the others and count nothing.
+__device__ __forceinline__ void zero_stages(uint32_t dst, int bytes, int wl) {
+  for (int o = wl * 16; o < bytes; o += 512) asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(dst + o), "r"(0u) : "memory");
+}
 constexpr int GN_WARP_STAGES = 2;
+__host__ __device__ constexpr int gn_warp_stage(int items, int cg) { return 512 * items + 8 * cg; }      // rows, FiLM vectors
+
+template <typename T, int ITEMS>
+__global__ void __launch_bounds__(GN_WARP_THREADS, 3)
+group_norm_warp_kernel(NormArgs g) {
+  constexpr int V = 16 / sizeof(T), P = V / 2;
+  extern __shared__ __align__(16) uint8_t gw_raw[];
+  const int gw = blockIdx.x * (GN_WARP_THREADS / 32) + (threadIdx.x >> 5), wl = threadIdx.x & 31;
+  const int grp = gw % g.groups, split = gw / g.groups;
+  pdl_wait();
+  if (split >= g.splits) return;
+  const int cg = g.C / g.groups, gcols = cg / V, R = 32 / gcols;             // lanes on a position, positions at a time
+  const int lr = wl / gcols, cc = (wl - lr * gcols) * V, c = grp * cg + cc, stage = gn_warp_stage(ITEMS, cg);
+  const uint8_t* mine = gw_raw + (threadIdx.x >> 5) * (GN_WARP_STAGES * stage);
+  const uint32_t mine_a = ptx::smem_u32(mine);
+  float2 ga[P], be[P];
+#pragma unroll
+  for (int i = 0; i < P; ++i) {
+    ga[i] = *reinterpret_cast<const float2*>(g.gamma + c + 2 * i);
+    be[i] = *reinterpret_cast<const float2*>(g.beta + c + 2 * i);
+  }
+  const float inv = 1.f / ((float)g.L * cg);
+  auto fetch = [&](int n, int s) {
+    if (n < g.N) {
+      warp_rows(mine_a + s * stage, reinterpret_cast<const char*>(reinterpret_cast<const T*>(g.x.p) + n * g.x.sn + grp * cg), g.x.sl * (long long)sizeof(T),
+                cg * (int)sizeof(T), g.L, wl);
+      if (g.film) warp_rows(mine_a + s * stage + 512 * ITEMS, reinterpret_cast<const char*>(g.film + (long long)n * 2 * g.C + grp * cg), 4ll * g.C, 4 * cg, 2, wl);
+    }
+    asm volatile("cp.async.commit_group;" ::: "memory");
+  };
+  zero_stages(mine_a, GN_WARP_STAGES * stage, wl);
+  __syncwarp();
+  fetch(split, 0);
+  const bool full = g.L == ITEMS * R;
+  const long long y_step = R * g.y.sl, q_step = (long long)R * g.C, b_step = (long long)R * copy_blocks(g.C);
+  int s = 0;
+  for (int n = split; n < g.N; n += g.splits) {
+    __syncwarp();                              // every lane is done with the stage that is filled next
+    fetch(n + g.splits, s ^ 1);
+    asm volatile("cp.async.wait_group 1;" ::: "memory");
+    __syncwarp();
+    const uint8_t* xs = mine + s * stage + (lr * cg + cc) * sizeof(T);
+    const float* film = reinterpret_cast<const float*>(mine + s * stage + 512 * ITEMS) + cc;
+    s ^= 1;
+    const int x_step = R * cg * (int)sizeof(T);
+    auto piece = [&](int j) { return *reinterpret_cast<const uint4*>(xs + j * x_step); };
+    float2 t2 = two(0.f);
+#pragma unroll
+    for (int j = 0; j < ITEMS; ++j) {
+      float2 v[P];
+      unpack16<T, V>(piece(j), v);
+#pragma unroll
+      for (int i = 0; i < P; ++i) t2 = __fadd2_rn(t2, v[i]);
+    }
+    const float mean = warp_sum(t2.x + t2.y) * inv;
+    t2 = two(0.f);
+    auto squares = [&](int j) {
+      float2 v[P];
+      unpack16<T, V>(piece(j), v);
+#pragma unroll
+      for (int i = 0; i < P; ++i) { v[i] = __fadd2_rn(v[i], two(-mean)); t2 = __ffma2_rn(v[i], v[i], t2); }
+    };
+    if (full) {
+#pragma unroll
+      for (int j = 0; j < ITEMS; ++j) squares(j);
+    } else {
+#pragma unroll
+      for (int j = 0; j < ITEMS; ++j)
+        if (lr + j * R < g.L) squares(j);
+    }
+    const float rstd = rsqrtf(warp_sum(t2.x + t2.y) * inv + g.eps);
+    if (wl == 0) {
+      if (g.mean) g.mean[(long long)n * g.groups + grp] = mean;
+      if (g.rstd) g.rstd[(long long)n * g.groups + grp] = rstd;
+    }
+    T* y = reinterpret_cast<T*>(g.y.p) + n * g.y.sn + lr * g.y.sl + c;
+    const long long r0 = (long long)n * g.L + lr;
+    long long qo = r0 * g.C + c, bo = r0 * copy_blocks(g.C) + (c >> 5);
+    float2 ka[P], kb[P];                       // z = x ka + kb
+#pragma unroll
+    for (int i = 0; i < P; ++i) { ka[i] = __fmul2_rn(ga[i], two(rstd)); kb[i] = __ffma2_rn(ka[i], two(-mean), be[i]); }
+    with_act(g.act, [&](auto act) {
+#pragma unroll 1                               // (one piece at a time: several do not fit the registers of three CTAs)
+      for (int j = 0; j < ITEMS; ++j) {
+        const bool row = lr + j * R < g.L;
+        const uint4 raw = piece(j);
+        float2 v[P];
+        unpack16<T, V>(raw, v);
+#pragma unroll
+        for (int i = 0; i < P; ++i) {
+          float2 d;
+          act_pair<false>(decltype(act)::value, __ffma2_rn(v[i], ka[i], kb[i]), v[i], d);
+        }
+        if (g.film)
+#pragma unroll
+          for (int i = 0; i < P; ++i)
+            v[i] = __ffma2_rn(v[i], *reinterpret_cast<const float2*>(film + 2 * i), *reinterpret_cast<const float2*>(film + cg + 2 * i));
+        const uint4 out = pack16<T, V>(v);
+        if (row) *reinterpret_cast<uint4*>(y) = out;
+        if (g.cx.q) write_copy<T>(g.cx.q + qo, g.cx.b + bo, raw, row, (cc & 31) == 0);
+        if (g.cy.q) write_copy<T>(g.cy.q + qo, g.cy.b + bo, out, row, (cc & 31) == 0);
+        y += y_step; qo += q_step; bo += b_step;
+      }
+    });
+  }
+}
+
+// Backward.  dz stays in registers between the sums and dx; dy and x (or its copy) come by cp.async into memory of the warp's own, one
+// sequence ahead, and are read from there as often as they are needed: with them in registers too the kernel spills.  The steps of an
+// 8-bit copy (L cg / 32 bytes) come one to a lane.
 template <typename T, bool COPY> __host__ __device__ constexpr int gn_warp_grad_smem(int items) {
   return GN_WARP_THREADS * GN_GRAD_V * items * (int)(sizeof(T) + (COPY ? 1 : sizeof(T))) * GN_WARP_STAGES;
 }
@@ -162,7 +182,10 @@ group_norm_warp_grad_kernel(NormArgs g) {
     }
     asm volatile("cp.async.commit_group;" ::: "memory");
   };
+  zero_stages(mine_a, GN_WARP_STAGES * STAGE, wl);
+  __syncwarp();
   fetch(split, 0);
+  const long long dx_step = R * g.dx.sl;
   int s = 0;
   for (int n = split; n < g.N; n += g.splits) {
     const float mean = nmean, rstd = nrstd, steps = COPY ? copy_step(nstep) : 1.f;
@@ -179,32 +202,32 @@ group_norm_warp_grad_kernel(NormArgs g) {
     float2 dz[ITEMS][P], s_z[P], s_h[P], s_a[P], s_y[P];
 #pragma unroll
     for (int i = 0; i < P; ++i) s_z[i] = s_h[i] = s_a[i] = s_y[i] = two(0.f);
-    auto h_values = [&](int j, float2* h) {              // (rows past the last: whatever the stage holds, not used)
+    // h = x rstd - mean rstd (an 8-bit copy's steps times rstd)
+    const float shift = -mean * rstd;
+    float scale[COPY ? ITEMS : 1];
+    scale[0] = rstd;
+    if constexpr (COPY)
+#pragma unroll
+      for (int j = 0; j < ITEMS; ++j) scale[j] = __shfl_sync(0xffffffffu, steps, min((lr + j * R) * gb + (cc >> 5), 31)) * rstd;
+    auto h_values = [&](int j, float2* h) {
       piece_values<X, V>(load_piece<X, V>(xs + j * R * cg * sizeof(X)), h);
-      if constexpr (COPY) {
-        const float st = __shfl_sync(0xffffffffu, steps, min((lr + j * R) * gb + (cc >> 5), 31));
 #pragma unroll
-        for (int i = 0; i < P; ++i) h[i] = __fmul2_rn(h[i], two(st));
-      }
-#pragma unroll
-      for (int i = 0; i < P; ++i) h[i] = __fmul2_rn(__fadd2_rn(h[i], two(-mean)), two(rstd));
+      for (int i = 0; i < P; ++i) h[i] = __ffma2_rn(h[i], two(scale[COPY ? j : 0]), two(shift));
     };
     with_act(g.act, [&](auto act) {
 #pragma unroll
       for (int j = 0; j < ITEMS; ++j) {
         float2 h[P], dy[P];
         h_values(j, h);
-        if (lr + j * R < g.L) {
-          piece_values<T, V>(load_piece<T, V>(dys + j * R * cg * sizeof(T)), dy);
+        piece_values<T, V>(load_piece<T, V>(dys + j * R * cg * sizeof(T)), dy);
 #pragma unroll
-          for (int i = 0; i < P; ++i) {
-            float2 a, d;
-            act_pair<true>(decltype(act)::value, __ffma2_rn(h[i], ga[i], be[i]), a, d);
-            if (dfilm) { s_a[i] = __ffma2_rn(dy[i], a, s_a[i]); s_y[i] = __fadd2_rn(s_y[i], dy[i]); }
-            dz[j][i] = __fmul2_rn(__fmul2_rn(dy[i], fs[i]), d);
-            s_z[i] = __fadd2_rn(s_z[i], dz[j][i]);
-            s_h[i] = __ffma2_rn(dz[j][i], h[i], s_h[i]);
-          }
+        for (int i = 0; i < P; ++i) {
+          float2 a, d;
+          act_pair<true>(decltype(act)::value, __ffma2_rn(h[i], ga[i], be[i]), a, d);
+          if (dfilm) { s_a[i] = __ffma2_rn(dy[i], a, s_a[i]); s_y[i] = __fadd2_rn(s_y[i], dy[i]); }
+          dz[j][i] = __fmul2_rn(__fmul2_rn(dy[i], fs[i]), d);
+          s_z[i] = __fadd2_rn(s_z[i], dz[j][i]);
+          s_h[i] = __ffma2_rn(dz[j][i], h[i], s_h[i]);
         }
       }
     });
@@ -216,21 +239,24 @@ group_norm_warp_grad_kernel(NormArgs g) {
       const float2 p = __fmul2_rn(s_z[i], ga[i]), q = __fmul2_rn(s_h[i], ga[i]);
       m1 += p.x + p.y; m2 += q.x + q.y;
     }
-    m1 = warp_sum(m1) * inv;
-    m2 = warp_sum(m2) * inv;
-    T* dx0 = reinterpret_cast<T*>(g.dx.p) + n * g.dx.sn + c;
+    // dx = dz (gamma rstd) - m1 rstd - h (m2 rstd)
+    m1 = -rstd * (warp_sum(m1) * inv);
+    m2 = -rstd * (warp_sum(m2) * inv);
+    T* dx = reinterpret_cast<T*>(g.dx.p) + n * g.dx.sn + lr * g.dx.sl + c;
+    float2 ka[P];
+#pragma unroll
+    for (int i = 0; i < P; ++i) ka[i] = __fmul2_rn(ga[i], two(rstd));
 #pragma unroll
     for (int j = 0; j < ITEMS; ++j) {
-      const int l = lr + j * R;
       float2 h[P];
       h_values(j, h);
-      if (l >= g.L) continue;
 #pragma unroll
-      for (int i = 0; i < P; ++i)
-        dz[j][i] = __fmul2_rn(two(rstd), __ffma2_rn(h[i], two(-m2), __fadd2_rn(__fmul2_rn(dz[j][i], ga[i]), two(-m1))));
-      T* dx = dx0 + l * g.dx.sl;
-      if constexpr (sizeof(T) == 2) *reinterpret_cast<uint2*>(dx) = make_uint2(pack_bf16(dz[j][0].x, dz[j][0].y), pack_bf16(dz[j][1].x, dz[j][1].y));
-      else *reinterpret_cast<float4*>(dx) = make_float4(dz[j][0].x, dz[j][0].y, dz[j][1].x, dz[j][1].y);
+      for (int i = 0; i < P; ++i) dz[j][i] = __ffma2_rn(dz[j][i], ka[i], __ffma2_rn(h[i], two(m2), two(m1)));
+      if (lr + j * R < g.L) {
+        if constexpr (sizeof(T) == 2) *reinterpret_cast<uint2*>(dx) = make_uint2(pack_bf16(dz[j][0].x, dz[j][0].y), pack_bf16(dz[j][1].x, dz[j][1].y));
+        else *reinterpret_cast<float4*>(dx) = make_float4(dz[j][0].x, dz[j][0].y, dz[j][1].x, dz[j][1].y);
+      }
+      dx += dx_step;
     }
     if (dfilm) {
       for (int o = gcols; o < 32; o *= 2)

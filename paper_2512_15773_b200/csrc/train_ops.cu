@@ -229,13 +229,20 @@ cudaError_t launch_warps(F kern, const NormArgs& g, int smem, cudaStream_t s) {
   const long long warps = (long long)g.splits * g.groups;
   return launch(kern, (unsigned)((warps + GN_WARP_THREADS / 32 - 1) / (GN_WARP_THREADS / 32)), GN_WARP_THREADS, 1, smem, s, g);
 }
+template <typename T, int ITEMS>
+cudaError_t norm_warp_items(const NormArgs& g, int device, cudaStream_t s) {
+  static std::atomic<unsigned long long> done{0};
+  constexpr int per = GN_WARP_THREADS / 32 * GN_WARP_STAGES;
+  const cudaError_t e = allow_smem(group_norm_warp_kernel<T, ITEMS>, per * gn_warp_stage(ITEMS, 256), device, done);
+  return e != cudaSuccess ? e : launch_warps(group_norm_warp_kernel<T, ITEMS>, g, per * gn_warp_stage(ITEMS, g.C / g.groups), s);
+}
 template <typename T>
-cudaError_t norm_warp(const NormArgs& g, int items, cudaStream_t s) {
-  if (items <= 1) return launch_warps(group_norm_warp_kernel<T, 1>, g, 0, s);
-  if (items <= 2) return launch_warps(group_norm_warp_kernel<T, 2>, g, 0, s);
+cudaError_t norm_warp(const NormArgs& g, int items, int device, cudaStream_t s) {
+  if (items <= 1) return norm_warp_items<T, 1>(g, device, s);
+  if (items <= 2) return norm_warp_items<T, 2>(g, device, s);
   if constexpr (sizeof(T) == 4)
-    if (items > 4) return launch_warps(group_norm_warp_kernel<T, 8>, g, 0, s);
-  return launch_warps(group_norm_warp_kernel<T, 4>, g, 0, s);
+    if (items > 4) return norm_warp_items<T, 8>(g, device, s);
+  return norm_warp_items<T, 4>(g, device, s);
 }
 template <typename T, int ITEMS, bool COPY>
 cudaError_t norm_warp_grad_items(const NormArgs& g, int device, cudaStream_t s) {
@@ -261,7 +268,7 @@ cudaError_t norm_forward(NormArgs& g, int sms, int device, cudaStream_t s) {
   const int unit = V > 1 && set_fits(g.C, g.groups, 32) ? 32 : V;      // (with or without copies: the same plan, the same bits)
   int items, bytes;
   if constexpr (V > 1) {
-    if (vectors_wide(g) && warp_plan(g, V, 32 / V, 2, sms, items)) return norm_warp<T>(g, items, s);
+    if (vectors_wide(g) && warp_plan(g, V, 32 / V, 3, sms, items)) return norm_warp<T>(g, items, device, s);
     if (vectors_wide(g) && slab_plan(g, V, unit, sizeof(T), sms, false, false, items, bytes))
       return items <= 1 ? norm_slab<T, 1>(g, bytes, device, s) : (items <= 2 ? norm_slab<T, 2>(g, bytes, device, s) : norm_slab<T, 4>(g, bytes, device, s));
   }

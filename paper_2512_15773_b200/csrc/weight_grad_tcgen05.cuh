@@ -76,14 +76,6 @@ __device__ __forceinline__ uint64_t umma_desc_mn_sw128(uint32_t smem_addr, uint3
   return d;
 }
 
-// Two bf16 values of a word pair's bytes j, j + 1: the magnitude's seven bits on 128 (bf16 counts by ones there), 128 or 256 taken off by
-// the sign bit; both exact, and so is the product with a power of two.
-__device__ __forceinline__ uint32_t wg_pair(uint32_t word, uint32_t sel, __nv_bfloat162 step) {
-  const uint32_t p = __byte_perm(word, 0u, sel);
-  const uint32_t hi = (p & 0x007f007fu) | 0x43004300u, lo = (p & 0x00800080u) | 0xc300c300u;
-  const __nv_bfloat162 v = __hmul2(__hadd2(*reinterpret_cast<const __nv_bfloat162*>(&hi), *reinterpret_cast<const __nv_bfloat162*>(&lo)), step);
-  return *reinterpret_cast<const uint32_t*>(&v);
-}
 __device__ __forceinline__ void st_shared16(uint32_t addr, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
   asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
 }
@@ -302,11 +294,10 @@ weight_grad_kernel(const __grid_constant__ CUtensorMap tmDy, const __grid_consta
       const uint32_t a0 = base + sa * WG_TILE_A + row_off;
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
-        const uint32_t step = cur[h] == 255u ? 0x7fc07fc0u : cur[h] * 0x00800080u;      // the byte as the exponent of two bf16 values
-        const __nv_bfloat162 k = *reinterpret_cast<const __nv_bfloat162*>(&step);
+        const __nv_bfloat162 k = copy_step2(cur[h]);
         const uint32_t x0 = half ? w[h].z : w[h].x, x1 = half ? w[h].w : w[h].y, y0 = half ? w[h].x : w[h].z, y1 = half ? w[h].y : w[h].w;
-        st_shared16(a0 + h * (32 * 128) + u0, wg_pair(x0, 0x4140, k), wg_pair(x0, 0x4342, k), wg_pair(x1, 0x4140, k), wg_pair(x1, 0x4342, k));
-        st_shared16(a0 + h * (32 * 128) + u1, wg_pair(y0, 0x4140, k), wg_pair(y0, 0x4342, k), wg_pair(y1, 0x4140, k), wg_pair(y1, 0x4342, k));
+        st_shared16(a0 + h * (32 * 128) + u0, copy_pair(x0, 0, k), copy_pair(x0, 1, k), copy_pair(x1, 0, k), copy_pair(x1, 1, k));
+        st_shared16(a0 + h * (32 * 128) + u1, copy_pair(y0, 0, k), copy_pair(y0, 1, k), copy_pair(y1, 0, k), copy_pair(y1, 1, k));
       }
       if constexpr (DYK != WG_DY_TMA) {
         // eight output channels at a time

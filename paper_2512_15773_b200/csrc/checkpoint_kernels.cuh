@@ -122,7 +122,7 @@ __device__ __forceinline__ long long row_offset(const Rows& x, long long r, int 
 // C % 8 = 0, 16-byte aligned rows.  Bound by bytes.
 constexpr int COPY_THREADS = 256, COPY_ROWS = 4;
 template <typename T>
-__global__ void __launch_bounds__(COPY_THREADS)
+__global__ void __launch_bounds__(COPY_THREADS, 4)
 checkpoint_pack_kernel(Rows x, Copy8 out, int N, int L, int C) {
   pdl_wait();
   constexpr int W = sizeof(T) / 2;                                           // 16-byte pieces of eight values
@@ -195,7 +195,7 @@ checkpoint_pack_any_kernel(Rows x, Copy8 out, int N, int L, int C) {
 }
 
 template <typename T>
-__global__ void __launch_bounds__(COPY_THREADS)
+__global__ void __launch_bounds__(COPY_THREADS, 4)
 checkpoint_unpack_kernel(Copy8 in, Rows x, int N, int L, int C) {
   pdl_wait();
   const int nb = copy_blocks(C), units = C >> 3, per = min(units, COPY_THREADS);

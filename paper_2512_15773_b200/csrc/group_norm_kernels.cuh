@@ -222,40 +222,17 @@ group_norm_kernel(NormArgs g) {
           if (g.film) { fs[i] = g.film[(long long)n * 2 * g.C + c_set + c + i]; fb[i] = g.film[((long long)n * 2 + 1) * g.C + c_set + c + i]; }
         }
       }
-      for (int l0 = lo; l0 < hi; l0 += g.lanes) {             // (a whole CTA's trip: the copies' blocks span lanes)
-        const int l = l0 + lane;
-        const bool row = in && l < hi;
+      if (!in) continue;
+#pragma unroll 4
+      for (int l = lo + lane; l < hi; l += g.lanes) {
         float v[V], z[V], a[V], d[V];
-#pragma unroll
-        for (int i = 0; i < V; ++i) v[i] = 0.f;
-        if (row) load_values<T, V>(x + l * g.x.sl + c, v);
+        load_values<T, V>(x + l * g.x.sl + c, v);
 #pragma unroll
         for (int i = 0; i < V; ++i) z[i] = fmaf((v[i] - mu[i]) * rs[i], ga[i], be[i]);
         act_values<false, V>(g.act, z, a, d);
 #pragma unroll
-        for (int i = 0; i < V; ++i) a[i] = to_f(from_f<T>(fmaf(a[i], fs[i], fb[i])));
-        if (row) store_values<T, V>(y + l * g.y.sl + c, a);
-        if constexpr (V > 1) {
-          const long long r = (long long)n * g.L + l;
-#pragma unroll
-          for (int which = 0; which < 2; ++which) {
-            const Copy8& o = which ? g.cy : g.cx;
-            if (o.q == nullptr) continue;
-            const float* w = which ? a : v;
-            uint32_t top = 0;
-#pragma unroll
-            for (int i = 0; i < V; ++i) top = max(top, row ? __float_as_uint(w[i]) & 0x7fffffffu : 0u);
-#pragma unroll
-            for (int o2 = 1; o2 < 32 / V; o2 *= 2) top = max(top, __shfl_xor_sync(0xffffffffu, top, o2));
-            const uint32_t b = copy_byte(top);
-            const float inv = copy_inv_step(b);
-            if (row) {
-              if constexpr (V == 8) *reinterpret_cast<uint2*>(o.q + r * g.C + c_set + c) = make_uint2(copy_q4(w, inv, b), copy_q4(w + 4, inv, b));
-              else *reinterpret_cast<uint32_t*>(o.q + r * g.C + c_set + c) = copy_q4(w, inv, b);
-              if ((c & 31) == 0) o.b[r * copy_blocks(g.C) + ((c_set + c) >> 5)] = (unsigned char)b;
-            }
-          }
-        }
+        for (int i = 0; i < V; ++i) a[i] = fmaf(a[i], fs[i], fb[i]);
+        store_values<T, V>(y + l * g.y.sl + c, a);
       }
     }
     if (g.ranks > 1) ptx::cluster_sync_all();               // s_grp may be written again once every CTA has read it

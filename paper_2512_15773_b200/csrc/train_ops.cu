@@ -104,7 +104,7 @@ cudaError_t pack(const Rows& x, Copy8 out, int N, int L, int C, int sms, cudaStr
   const bool wide = rows_wide(x, sizeof(T) == 2 ? TSDP_TYPE_BF16 : TSDP_TYPE_FP32, C) && C % 8 == 0 && ((uintptr_t)out.q & 7) == 0;
   if (wide) {
     const int lanes = COPY_THREADS / min(4 * copy_blocks(C), COPY_THREADS);
-    const long long blocks = min((rows + lanes - 1) / lanes, (long long)sms * 32);
+    const long long blocks = min((rows + lanes - 1) / lanes, (long long)sms * 4);
     return launch(checkpoint_pack_kernel<T>, (unsigned)blocks, COPY_THREADS, 1, 0, s, x, out, N, L, C);
   }
   const long long blocks = min((rows * copy_blocks(C) + 7) / 8, (long long)sms * 64);
@@ -117,7 +117,7 @@ cudaError_t unpack(Copy8 in, const Rows& x, int N, int L, int C, int sms, cudaSt
   const bool wide = rows_wide(x, sizeof(T) == 2 ? TSDP_TYPE_BF16 : TSDP_TYPE_FP32, C) && C % 8 == 0 && ((uintptr_t)in.q & 7) == 0;
   if (wide) {
     const int lanes = COPY_THREADS / min(C / 8, COPY_THREADS);
-    const long long blocks = min((rows + lanes - 1) / lanes, (long long)sms * 32);
+    const long long blocks = min((rows + lanes - 1) / lanes, (long long)sms * 4);
     return launch(checkpoint_unpack_kernel<T>, (unsigned)blocks, COPY_THREADS, 1, 0, s, in, x, N, L, C);
   }
   const long long blocks = min((rows * copy_blocks(C) + 7) / 8, (long long)sms * 64);
@@ -136,25 +136,19 @@ int gcd(int a, int b) { while (b) { const int t = a % b; a = b; b = t; } return 
 bool set_fits(int C, int groups, int unit) { const int cg = C / groups; return (long long)min(unit / gcd(cg, unit), groups) * cg <= GN_MAX_WIDTH; }
 
 // Which groups a CTA takes, how its threads lie over them, how many CTAs share the positions.
-// unit: channels that a set has to be a multiple of (16-byte pieces, 32 for 8-bit copies).
-void norm_plan(NormArgs& g, int V, int unit, int elem, int sms, bool grad) {
+void norm_plan(NormArgs& g, int V, int elem, int sms, bool grad) {
   const int cg = g.C / g.groups;
-  g.per_set = unit / gcd(cg, unit);
-  if (g.per_set > g.groups) g.per_set = g.groups;
+  g.per_set = min(V / gcd(cg, V), g.groups);
   const int step = g.per_set;
-  // rows of 128 bytes at least, where that leaves enough sets for the SMs and a row does not outgrow the threads
+  // rows of 128 bytes at least, where a row does not outgrow the threads
   while (g.per_set + step <= g.groups && (g.per_set + step) * cg <= GN_THREADS * V && g.per_set * cg * elem < 128) g.per_set += step;
   g.width = g.per_set * cg;
   g.sets = (g.groups + g.per_set - 1) / g.per_set;
   g.cols = min((g.width + V - 1) / V, GN_THREADS);
-  if (unit == 32 && g.cols < GN_THREADS) {                          // whole blocks of 32 channels side by side in a warp
-    const int per = 32 / V;
-    g.cols = (g.cols + per - 1) / per * per;
-  }
   g.lanes = GN_THREADS / g.cols;
   g.ranks = 1;
   while (g.ranks < 8 && (long long)g.N * g.sets * g.ranks < 2 * sms && g.L >= 8ll * g.lanes * g.ranks) g.ranks *= 2;
-  const long long fill = (long long)sms * (grad ? 4 : 8) / ((long long)g.sets * g.ranks);
+  const long long fill = (long long)sms * 4 / ((long long)g.sets * g.ranks);
   g.splits = (int)min((long long)g.N, max(1ll, grad ? fill : (1ll << 24) / ((long long)g.sets * g.ranks)));
 }
 
@@ -263,16 +257,16 @@ cudaError_t norm_warp_grad(const NormArgs& g, int items, int device, cudaStream_
 // The vectors that slab kernels read in pairs or by bulk copies.
 bool vectors_wide(const NormArgs& g) { return ((uintptr_t)g.gamma & 7) == 0 && ((uintptr_t)g.beta & 7) == 0 && (!g.film || aligned16(g.film)); }
 
+// The three forms of the forward pass; the first two write the copies on their way.
+enum { NORM_STREAM = 0, NORM_WARPS = 1, NORM_SLABS = 2 };
 template <typename T, int V>
-cudaError_t norm_forward(NormArgs& g, int sms, int device, cudaStream_t s) {
-  const int unit = V > 1 && set_fits(g.C, g.groups, 32) ? 32 : V;      // (with or without copies: the same plan, the same bits)
-  int items, bytes;
+cudaError_t norm_forward(NormArgs& g, int form, int items, int bytes, int sms, int device, cudaStream_t s) {
   if constexpr (V > 1) {
-    if (vectors_wide(g) && warp_plan(g, V, 32 / V, 3, sms, items)) return norm_warp<T>(g, items, device, s);
-    if (vectors_wide(g) && slab_plan(g, V, unit, sizeof(T), sms, false, false, items, bytes))
+    if (form == NORM_WARPS) return norm_warp<T>(g, items, device, s);
+    if (form == NORM_SLABS)
       return items <= 1 ? norm_slab<T, 1>(g, bytes, device, s) : (items <= 2 ? norm_slab<T, 2>(g, bytes, device, s) : norm_slab<T, 4>(g, bytes, device, s));
   }
-  norm_plan(g, V, unit, sizeof(T), sms, false);
+  norm_plan(g, V, sizeof(T), sms, false);
   static std::atomic<unsigned long long> done{0};
   const int smem = (2 * GN_THREADS * V + 4 * g.per_set) * 4;
   const cudaError_t e = allow_smem(group_norm_kernel<T, V>, (2 * GN_THREADS * V + 4 * GN_MAX_WIDTH) * 4, device, done);
@@ -395,16 +389,21 @@ int tsdp_group_norm(int device, const tsdp_norm_t* shape, const void* d_x, int64
   g.gamma = d_gamma; g.beta = d_beta; g.film = d_film; g.mean = d_mean; g.rstd = d_rstd;
   const Copy8 cx = copy_of(saved_x), cy = copy_of(saved_y);
   const bool wide = rows_wide(g.x, dtype, C) && rows_wide(g.y, dtype, C) && set_fits(C, g.groups, 16 / (int)esize(dtype));
-  // copies are written on the way where rows come in 16-byte pieces, by a pass of their own elsewhere
-  const bool fused = wide && ((uintptr_t)cx.q & 7) == 0 && ((uintptr_t)cy.q & 7) == 0 && set_fits(C, g.groups, 32);
+  int form = NORM_STREAM, items = 0, bytes = 0;
+  if (wide && vectors_wide(g) && ((uintptr_t)cx.q & 7) == 0 && ((uintptr_t)cy.q & 7) == 0) {
+    const int V = 16 / (int)esize(dtype), unit = set_fits(C, g.groups, 32) ? 32 : V;      // (with or without copies: the same plan, the same bits)
+    if (warp_plan(g, V, 32 / V, 3, sms, items)) form = NORM_WARPS;
+    else if ((unit == 32 || (!cx.q && !cy.q)) && slab_plan(g, V, unit, (int)esize(dtype), sms, false, false, items, bytes)) form = NORM_SLABS;
+  }
+  // copies are written on the way by the forms that hold a group, by a pass of their own otherwise
   cudaError_t e = cudaSuccess;
-  if (fused) { g.cx = cx; g.cy = cy; }
+  if (form != NORM_STREAM) { g.cx = cx; g.cy = cy; }
   else if (cx.q) e = dtype == TSDP_TYPE_BF16 ? pack<__nv_bfloat16>(g.x, cx, N, L, C, sms, s) : pack<float>(g.x, cx, N, L, C, sms, s);
   if (e == cudaSuccess) {
-    if (dtype == TSDP_TYPE_BF16) e = wide ? norm_forward<__nv_bfloat16, 8>(g, sms, device, s) : norm_forward<__nv_bfloat16, 1>(g, sms, device, s);
-    else e = wide ? norm_forward<float, 4>(g, sms, device, s) : norm_forward<float, 1>(g, sms, device, s);
+    if (dtype == TSDP_TYPE_BF16) e = wide ? norm_forward<__nv_bfloat16, 8>(g, form, items, bytes, sms, device, s) : norm_forward<__nv_bfloat16, 1>(g, form, items, bytes, sms, device, s);
+    else e = wide ? norm_forward<float, 4>(g, form, items, bytes, sms, device, s) : norm_forward<float, 1>(g, form, items, bytes, sms, device, s);
   }
-  if (e == cudaSuccess && !fused && cy.q)
+  if (e == cudaSuccess && form == NORM_STREAM && cy.q)
     e = dtype == TSDP_TYPE_BF16 ? pack<__nv_bfloat16>(g.y, cy, N, L, C, sms, s) : pack<float>(g.y, cy, N, L, C, sms, s);
   return e == cudaSuccess ? TSDP_OK : fail_cuda("tsdp_group_norm", e);
 }
@@ -422,7 +421,7 @@ size_t tsdp_group_norm_grad_workspace(int device, const tsdp_norm_t* shape) {
     int items, bytes;
     g.N = shape->N < 1 ? 1 : shape->N; g.L = shape->L; g.C = shape->C; g.groups = shape->groups;
     g.dfilm = form & 1 ? &some : nullptr;
-    if (form < 2) norm_plan(g, V, V, elem, sms, true);
+    if (form < 2) norm_plan(g, V, elem, sms, true);
     else if (form == 6 ? !warp_plan(g, GN_GRAD_V, elem == 2 ? 8 : 4, 2, sms, items) : !slab_plan(g, GN_GRAD_V, V, elem, sms, true, form >= 4, items, bytes)) continue;
     if (norm_grad_bytes(g) > most) most = norm_grad_bytes(g);
   }
@@ -467,7 +466,7 @@ int tsdp_group_norm_grad(int device, const tsdp_norm_t* shape, const void* d_dy,
     if ((!copy || aligned16(g.cx.q)) && warp_plan(g, GN_GRAD_V, dtype == TSDP_TYPE_BF16 ? 8 : 4, 2, sms, items)) form = GRAD_WARPS;
     else if ((!copy || aligned16(g.cx.q)) && slab_plan(g, GN_GRAD_V, V, (int)esize(dtype), sms, true, copy, items, bytes)) form = GRAD_SLABS;
   }
-  if (form == GRAD_STREAM) norm_plan(g, V, V, (int)esize(dtype), sms, true);
+  if (form == GRAD_STREAM) norm_plan(g, V, (int)esize(dtype), sms, true);
   if (workspace_bytes < norm_grad_bytes(g)) return TSDP_ERR_ARG;
   if (dtype == TSDP_TYPE_BF16) {
     if (wide) e = copy ? norm_backward<__nv_bfloat16, 8, true>(g, form, items, bytes, device, s) : norm_backward<__nv_bfloat16, 8, false>(g, form, items, bytes, device, s);

@@ -58,7 +58,7 @@ template <bool GRAD> __device__ __forceinline__ void act_pair(int act, float2 z,
     if (GRAD) d = two(1.f);
   }
 }
-template <bool GRAD, int V> __device__ __forceinline__ void act_values(int act, const float* z, float* a, float* d) {
+template <bool GRAD, int V> __device__ __forceinline__ void act_values(int act, const float* z, float* a, float* d) {      // act: a constant at the call
   if constexpr (V == 1) {
     float2 av, dv;
     act_pair<GRAD>(act, two(z[0]), av, dv);
@@ -75,6 +75,47 @@ template <bool GRAD, int V> __device__ __forceinline__ void act_values(int act, 
   }
 }
 
+// V values (4, 8 or 16 bytes, or one value) of memory as they are.
+template <typename T, int V> struct Piece { uint32_t w[V == 1 ? 1 : V * sizeof(T) / 4]; };
+template <typename T, int V> __device__ __forceinline__ Piece<T, V> load_piece(const uint8_t* p) {
+  Piece<T, V> r;
+  if constexpr (V == 1) r.w[0] = sizeof(T) == 4 ? *reinterpret_cast<const uint32_t*>(p) : sizeof(T) == 2 ? *reinterpret_cast<const unsigned short*>(p) : *p;
+  else if constexpr (sizeof(r) == 16) { const uint4 u = *reinterpret_cast<const uint4*>(p); r.w[0] = u.x; r.w[1] = u.y; r.w[2] = u.z; r.w[3] = u.w; }
+  else if constexpr (sizeof(r) == 8) { const uint2 u = *reinterpret_cast<const uint2*>(p); r.w[0] = u.x; r.w[1] = u.y; }
+  else r.w[0] = *reinterpret_cast<const uint32_t*>(p);
+  return r;
+}
+template <typename T, int V> __device__ __forceinline__ void piece_values(const Piece<T, V>& r, float2* v) {
+#pragma unroll
+  for (int i = 0; i < V / 2; ++i) {
+    if constexpr (sizeof(T) == 2) v[i] = make_float2(__uint_as_float(r.w[i] << 16), __uint_as_float(r.w[i] & 0xffff0000u));
+    else if constexpr (sizeof(T) == 4) v[i] = make_float2(__uint_as_float(r.w[2 * i]), __uint_as_float(r.w[2 * i + 1]));
+    else {                                     // (by the conversion instruction: its pipe has room here, that of the permutations has none: 70 us, not 78)
+      const uint32_t u = r.w[i >> 1] >> (16 * (i & 1));
+      v[i] = make_float2((float)(signed char)u, (float)(signed char)(u >> 8));
+    }
+  }
+}
+template <typename T, int V> __device__ __forceinline__ void piece_floats(const Piece<T, V>& r, float* v) {
+  if constexpr (V == 1) {
+    v[0] = sizeof(T) == 4 ? __uint_as_float(r.w[0]) : sizeof(T) == 2 ? __uint_as_float(r.w[0] << 16) : (float)(signed char)r.w[0];
+  } else {
+    float2 f[V / 2];
+    piece_values<T, V>(r, f);
+#pragma unroll
+    for (int i = 0; i < V / 2; ++i) { v[2 * i] = f[i].x; v[2 * i + 1] = f[i].y; }
+  }
+}
+
+// f(the activation as a constant): the choice is made once, not for every value.
+template <int A> struct ActIs { static constexpr int value = A; };
+template <typename F> __device__ __forceinline__ void with_act(int act, F&& f) {
+  if (act == ACT_MISH) f(ActIs<ACT_MISH>{});
+  else if (act == ACT_SILU) f(ActIs<ACT_SILU>{});
+  else if (act == ACT_GELU) f(ActIs<ACT_GELU>{});
+  else f(ActIs<ACT_NONE>{});
+}
+
 struct NormArgs {
   int N, L, C, groups, act;
   float eps;
@@ -89,7 +130,8 @@ struct NormArgs {
   int fold, red_rows, stage_bytes;
 };
 
-constexpr int GN_THREADS = 256;
+constexpr int GN_GRAD_V = 4;                   // channels of a thread in the backward pass: with eight its sums do not fit the registers
+constexpr int GN_THREADS = 256, GN_STREAM_THREADS = 512;      // of the kernels; of the backward one over long sequences (few CTAs with much to fetch)
 constexpr int GN_MAX_WIDTH = 2048;             // channels of a set: their sums stay in shared memory
 
 __device__ __forceinline__ float ld_rank_f32(const float* p, uint32_t rank) {       // the same shared-memory word of another CTA of the cluster
@@ -105,7 +147,7 @@ __device__ __forceinline__ int lane_rows(int lo, int hi, int r, int lanes) { ret
 // First walk: each thread keeps, per channel, the sums about its own first value (so that a large mean costs no digits); mean and centred
 // sum of squares of its share are then merged, thread by thread and CTA by CTA, with their counts: M2 = sum M2_i + n_i (mean_i - mean)^2.
 template <typename T, int V>
-__global__ void __launch_bounds__(GN_THREADS)
+__global__ void __launch_bounds__(GN_THREADS, 2)
 group_norm_kernel(NormArgs g) {
   extern __shared__ __align__(16) float gn_smem[];
   pdl_wait();
@@ -131,20 +173,23 @@ group_norm_kernel(NormArgs g) {
 #pragma unroll
         for (int i = 0; i < V; ++i) k[i] = s[i] = q[i] = 0.f;
         int l = lo + lane;
-        if (l < hi) load_values<T, V>(x + l * g.x.sl + c, k);
-        constexpr int U = 4;
+        Piece<T, V> pivot{};
+        if (l < hi) { pivot = load_piece<T, V>(reinterpret_cast<const uint8_t*>(x + l * g.x.sl + c)); piece_floats<T, V>(pivot, k); }
+        constexpr int U = 8;
         for (; l < hi; l += U * g.lanes) {
-          float v[U][V];
+          Piece<T, V> raw[U];
 #pragma unroll
           for (int j = 0; j < U; ++j) {
-#pragma unroll
-            for (int i = 0; i < V; ++i) v[j][i] = k[i];
-            if (l + j * g.lanes < hi) load_values<T, V>(x + (l + j * g.lanes) * g.x.sl + c, v[j]);
+            raw[j] = pivot;                                    // (counts nothing)
+            if (l + j * g.lanes < hi) raw[j] = load_piece<T, V>(reinterpret_cast<const uint8_t*>(x + (l + j * g.lanes) * g.x.sl + c));
           }
 #pragma unroll
-          for (int j = 0; j < U; ++j)
+          for (int j = 0; j < U; ++j) {
+            float v[V];
+            piece_floats<T, V>(raw[j], v);
 #pragma unroll
-            for (int i = 0; i < V; ++i) { const float d = v[j][i] - k[i]; s[i] += d; q[i] = fmaf(d, d, q[i]); }
+            for (int i = 0; i < V; ++i) { const float d = v[i] - k[i]; s[i] += d; q[i] = fmaf(d, d, q[i]); }
+          }
         }
         const int cnt = lane_rows(lo, hi, lane, g.lanes);
         const float inv = cnt ? 1.f / cnt : 0.f;
@@ -223,17 +268,27 @@ group_norm_kernel(NormArgs g) {
         }
       }
       if (!in) continue;
-#pragma unroll 4
-      for (int l = lo + lane; l < hi; l += g.lanes) {
-        float v[V], z[V], a[V], d[V];
-        load_values<T, V>(x + l * g.x.sl + c, v);
+      with_act(g.act, [&](auto act) {
+        constexpr int U = 4;                                   // positions asked for together
+        for (int l = lo + lane; l < hi; l += U * g.lanes) {
+          Piece<T, V> raw[U];
 #pragma unroll
-        for (int i = 0; i < V; ++i) z[i] = fmaf((v[i] - mu[i]) * rs[i], ga[i], be[i]);
-        act_values<false, V>(g.act, z, a, d);
+          for (int j = 0; j < U; ++j)
+            if (l + j * g.lanes < hi) raw[j] = load_piece<T, V>(reinterpret_cast<const uint8_t*>(x + (l + j * g.lanes) * g.x.sl + c));
 #pragma unroll
-        for (int i = 0; i < V; ++i) a[i] = fmaf(a[i], fs[i], fb[i]);
-        store_values<T, V>(y + l * g.y.sl + c, a);
-      }
+          for (int j = 0; j < U; ++j) {
+            if (l + j * g.lanes >= hi) break;
+            float v[V], z[V], a[V], d[V];
+            piece_floats<T, V>(raw[j], v);
+#pragma unroll
+            for (int i = 0; i < V; ++i) z[i] = fmaf((v[i] - mu[i]) * rs[i], ga[i], be[i]);
+            act_values<false, V>(decltype(act)::value, z, a, d);
+#pragma unroll
+            for (int i = 0; i < V; ++i) a[i] = fmaf(a[i], fs[i], fb[i]);
+            store_values<T, V>(y + (l + j * g.lanes) * g.y.sl + c, a);
+          }
+        }
+      });
     }
     if (g.ranks > 1) ptx::cluster_sync_all();               // s_grp may be written again once every CTA has read it
     else __syncthreads();
@@ -242,29 +297,6 @@ group_norm_kernel(NormArgs g) {
 }
 
 // ------------------------------------------------------------------------------------------------------------------ backward
-// V values of x as the forward pass saw it (COPY: as its 8-bit copy has it).
-template <typename T, int V, bool COPY>
-__device__ __forceinline__ void load_x(const NormArgs& g, int n, int l, int c, float* v) {
-  if constexpr (!COPY) {
-    load_values<T, V>(reinterpret_cast<const T*>(g.x.p) + n * g.x.sn + l * g.x.sl + c, v);
-  } else {
-    const long long r = (long long)n * g.L + l;
-    const float step = copy_step(g.cx.b[r * copy_blocks(g.C) + (c >> 5)]);
-    const signed char* q = g.cx.q + r * g.C + c;
-    if constexpr (V == 1) v[0] = (float)*q * step;
-    else {
-      uint32_t w[2];
-      if constexpr (V == 8) { const uint2 u = *reinterpret_cast<const uint2*>(q); w[0] = u.x; w[1] = u.y; }
-      else w[0] = *reinterpret_cast<const uint32_t*>(q);
-#pragma unroll
-      for (int i = 0; i < V; i += 2) {
-        const float2 f = copy_ints(w[i >> 2], (i >> 1) & 1);
-        v[i] = f.x * step; v[i + 1] = f.y * step;
-      }
-    }
-  }
-}
-
 template <int V> struct NormVectors { float ga[V], be[V], mu[V], rs[V], fs[V]; };
 template <int V>
 __device__ __forceinline__ void norm_vectors(const NormArgs& g, int n, int c, bool in, NormVectors<V>& p) {
@@ -281,28 +313,67 @@ __device__ __forceinline__ void norm_vectors(const NormArgs& g, int n, int c, bo
   }
 }
 
-// dz, h and dy a of V values
-template <typename T, int V, bool COPY>
-__device__ __forceinline__ void norm_dz(const NormArgs& g, int n, int l, int c, const NormVectors<V>& p, float* dz, float* h, float* dy, float* dya) {
-  float x[V], z[V], a[V], d[V];
-  load_x<T, V, COPY>(g, n, l, c, x);
-  load_values<T, V>(reinterpret_cast<const T*>(g.dy.p) + n * g.dy.sn + l * g.dy.sl + c, dy);
+// f(position, dz, h, dy, dy a) for this lane's positions, GN_WALK of them asked for together.
+constexpr int GN_WALK = 2;
+template <typename T, int V, bool COPY, typename F>
+__device__ __forceinline__ void norm_walk(const NormArgs& g, int n, int l0, int hi, int c, const NormVectors<V>& p, F&& f) {
+  using X = std::conditional_t<COPY, signed char, T>;
+  const X* x0 = COPY ? reinterpret_cast<const X*>(g.cx.q) + (long long)n * g.L * g.C + c : reinterpret_cast<const X*>(g.x.p) + n * g.x.sn + c;
+  const T* dy0 = reinterpret_cast<const T*>(g.dy.p) + n * g.dy.sn + c;
+  const long long xl = COPY ? g.C : g.x.sl, nb = copy_blocks(g.C);
+  const unsigned char* b0 = COPY ? g.cx.b + (long long)n * g.L * nb + (c >> 5) : nullptr;
+  with_act(g.act, [&](auto act) {
+    for (int l = l0; l < hi; l += GN_WALK * g.lanes) {
+      Piece<X, V> x[GN_WALK];
+      Piece<T, V> dy[GN_WALK];
+      uint32_t b[GN_WALK];
 #pragma unroll
-  for (int i = 0; i < V; ++i) { h[i] = (x[i] - p.mu[i]) * p.rs[i]; z[i] = fmaf(h[i], p.ga[i], p.be[i]); }
-  act_values<true, V>(g.act, z, a, d);
+      for (int j = 0; j < GN_WALK; ++j) {
+        const int lj = l + j * g.lanes;
+        x[j] = Piece<X, V>{};                                  // (a position that is not there counts nothing: its dy is zero)
+        dy[j] = Piece<T, V>{};
+        b[j] = 0u;
+        if (lj < hi) {
+          x[j] = load_piece<X, V>(reinterpret_cast<const uint8_t*>(x0 + lj * xl));
+          dy[j] = load_piece<T, V>(reinterpret_cast<const uint8_t*>(dy0 + lj * g.dy.sl));
+          if (COPY) b[j] = b0[lj * nb];
+        }
+      }
 #pragma unroll
-  for (int i = 0; i < V; ++i) { dz[i] = dy[i] * p.fs[i] * d[i]; dya[i] = dy[i] * a[i]; }
+      for (int j = 0; j < GN_WALK; ++j) {
+        float h[V], z[V], a[V], d[V], dz[V], dya[V], dyf[V];
+        piece_floats<X, V>(x[j], h);
+        piece_floats<T, V>(dy[j], dyf);
+        const float step = COPY ? copy_step(b[j]) : 1.f;
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+          h[i] = ((COPY ? h[i] * step : h[i]) - p.mu[i]) * p.rs[i];
+          z[i] = fmaf(h[i], p.ga[i], p.be[i]);
+        }
+        act_values<true, V>(decltype(act)::value, z, a, d);
+#pragma unroll
+        for (int i = 0; i < V; ++i) { dz[i] = dyf[i] * p.fs[i] * d[i]; dya[i] = dyf[i] * a[i]; }
+        f(l + j * g.lanes, dz, h, dyf, dya);
+      }
+    }
+  });
+}
+
+// V values in 4, 8 or 16 bytes.
+template <typename T, int V> __device__ __forceinline__ void store_few(T* p, const float* v) {
+  if constexpr (V == 4 && sizeof(T) == 2) *reinterpret_cast<uint2*>(p) = make_uint2(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]));
+  else store_values<T, V>(p, v);
 }
 
 // A cluster walks the sequences split, split + splits, ... and keeps its channels' share of dgamma and dbeta in shared memory.
 template <typename T, int V, bool COPY>
-__global__ void __launch_bounds__(GN_THREADS)
+__global__ void __launch_bounds__(GN_STREAM_THREADS, 1)
 group_norm_grad_kernel(NormArgs g) {
   extern __shared__ __align__(16) float gn_smem[];
   pdl_wait();
   const int cg = g.C / g.groups;
   float* s_lane = gn_smem;                                  // [4][lanes][tile channels]: sums of a lane
-  float* s_sum = s_lane + 4 * GN_THREADS * V;               // [4][width]: of the CTA
+  float* s_sum = s_lane + 4 * GN_STREAM_THREADS * V;               // [4][width]: of the CTA
   float* s_tot = s_sum + 4 * g.width;                       // [2][width]: of the cluster (dz, dz h)
   float* s_acc = s_tot + 2 * g.width;                       // [2][width]: over the sequences so far
   float* s_grp = s_acc + 2 * g.width;                       // [2][per_set]: m1, m2
@@ -314,7 +385,7 @@ group_norm_grad_kernel(NormArgs g) {
   const int warp = threadIdx.x >> 5, wl = threadIdx.x & 31;
   const bool film = g.film != nullptr && g.dfilm != nullptr;
   const int sums = film ? 4 : 2;
-  for (int i = threadIdx.x; i < 2 * g.width; i += GN_THREADS) s_acc[i] = 0.f;
+  for (int i = threadIdx.x; i < 2 * g.width; i += GN_STREAM_THREADS) s_acc[i] = 0.f;
   for (int n = split; n < g.N; n += g.splits) {
     for (int t0 = 0; t0 < width; t0 += tile) {
       const int c = t0 + col * V;
@@ -325,32 +396,29 @@ group_norm_grad_kernel(NormArgs g) {
         float s0[V], s1[V], s2[V], s3[V];
 #pragma unroll
         for (int i = 0; i < V; ++i) s0[i] = s1[i] = s2[i] = s3[i] = 0.f;
-#pragma unroll 2
-        for (int l = lo + lane; l < hi; l += g.lanes) {
-          float dz[V], h[V], dy[V], dya[V];
-          norm_dz<T, V, COPY>(g, n, l, c_set + c, p, dz, h, dy, dya);
+        norm_walk<T, V, COPY>(g, n, lo + lane, hi, c_set + c, p, [&](int, const float* dz, const float* h, const float* dy, const float* dya) {
 #pragma unroll
           for (int i = 0; i < V; ++i) { s0[i] += dz[i]; s1[i] = fmaf(dz[i], h[i], s1[i]); s2[i] += dya[i]; s3[i] += dy[i]; }
-        }
+        });
 #pragma unroll
         for (int i = 0; i < V; ++i) {
           float* o = s_lane + lane * tile + col * V + i;
-          o[0] = s0[i]; o[GN_THREADS * V] = s1[i];
-          if (film) { o[2 * GN_THREADS * V] = s2[i]; o[3 * GN_THREADS * V] = s3[i]; }
+          o[0] = s0[i]; o[GN_STREAM_THREADS * V] = s1[i];
+          if (film) { o[2 * GN_STREAM_THREADS * V] = s2[i]; o[3 * GN_STREAM_THREADS * V] = s3[i]; }
         }
       }
       __syncthreads();
       const int w = min(width - t0, tile);
-      for (int i = threadIdx.x; i < sums * w; i += GN_THREADS) {
+      for (int i = threadIdx.x; i < sums * w; i += GN_STREAM_THREADS) {
         const int k = i / w, cc = i - k * w;
         float s = 0.f;
-        for (int r = 0; r < g.lanes; ++r) s += s_lane[k * GN_THREADS * V + r * tile + cc];
+        for (int r = 0; r < g.lanes; ++r) s += s_lane[k * GN_STREAM_THREADS * V + r * tile + cc];
         s_sum[k * g.width + t0 + cc] = s;
       }
       __syncthreads();
     }
     if (g.ranks > 1) ptx::cluster_sync_all();
-    for (int i = threadIdx.x; i < sums * width; i += GN_THREADS) {
+    for (int i = threadIdx.x; i < sums * width; i += GN_STREAM_THREADS) {
       const int k = i / width, c = i - k * width;
       float s = s_sum[k * g.width + c];
       if (g.ranks > 1) {
@@ -362,7 +430,7 @@ group_norm_grad_kernel(NormArgs g) {
     }
     __syncthreads();
     const float inv = 1.f / ((float)g.L * cg);
-    for (int gr = warp; gr < n_grp; gr += GN_THREADS / 32) {
+    for (int gr = warp; gr < n_grp; gr += GN_STREAM_THREADS / 32) {
       float a = 0.f, b = 0.f;
       for (int i = wl; i < cg; i += 32) {
         const float ga = g.gamma[c_set + gr * cg + i];
@@ -381,21 +449,18 @@ group_norm_grad_kernel(NormArgs g) {
       float m1[V], m2[V];
 #pragma unroll
       for (int i = 0; i < V; ++i) { m1[i] = s_grp[(c + i) / cg]; m2[i] = s_grp[g.per_set + (c + i) / cg]; }
-#pragma unroll 2
-      for (int l = lo + lane; l < hi; l += g.lanes) {
-        float dz[V], h[V], dy[V], dya[V];
-        norm_dz<T, V, COPY>(g, n, l, c_set + c, p, dz, h, dy, dya);
+      norm_walk<T, V, COPY>(g, n, lo + lane, hi, c_set + c, p, [&](int l, float* dz, const float* h, const float*, const float*) {
 #pragma unroll
         for (int i = 0; i < V; ++i) dz[i] = p.rs[i] * fmaf(-h[i], m2[i], __fadd_rn(__fmul_rn(dz[i], p.ga[i]), -m1[i]));
-        store_values<T, V>(dx + l * g.dx.sl + c, dz);
-      }
+        if (l < hi) store_few<T, V>(dx + l * g.dx.sl + c, dz);
+      });
     }
     if (g.ranks > 1) ptx::cluster_sync_all();
     else __syncthreads();
   }
   __syncthreads();
   if (rank == 0)
-    for (int i = threadIdx.x; i < 2 * width; i += GN_THREADS) {
+    for (int i = threadIdx.x; i < 2 * width; i += GN_STREAM_THREADS) {
       const int k = i / width, c = i - k * width;
       g.part[((long long)split * 2 + k) * g.C + c_set + c] = s_acc[k * g.width + c];
     }

@@ -35,26 +35,6 @@ template <typename T, int V> __device__ __forceinline__ void unpack16(uint4 u, f
     v[1] = make_float2(__uint_as_float(u.z), __uint_as_float(u.w));
   }
 }
-// V values (8 or 16 bytes) of shared memory as they are.
-template <typename T, int V> struct Piece { uint32_t w[V * sizeof(T) / 4]; };
-template <typename T, int V> __device__ __forceinline__ Piece<T, V> load_piece(const uint8_t* p) {
-  Piece<T, V> r;
-  if constexpr (sizeof(r) == 16) { const uint4 u = *reinterpret_cast<const uint4*>(p); r.w[0] = u.x; r.w[1] = u.y; r.w[2] = u.z; r.w[3] = u.w; }
-  else if constexpr (sizeof(r) == 8) { const uint2 u = *reinterpret_cast<const uint2*>(p); r.w[0] = u.x; r.w[1] = u.y; }
-  else r.w[0] = *reinterpret_cast<const uint32_t*>(p);
-  return r;
-}
-template <typename T, int V> __device__ __forceinline__ void piece_values(const Piece<T, V>& r, float2* v) {
-#pragma unroll
-  for (int i = 0; i < V / 2; ++i) {
-    if constexpr (sizeof(T) == 2) v[i] = make_float2(__uint_as_float(r.w[i] << 16), __uint_as_float(r.w[i] & 0xffff0000u));
-    else if constexpr (sizeof(T) == 4) v[i] = make_float2(__uint_as_float(r.w[2 * i]), __uint_as_float(r.w[2 * i + 1]));
-    else {                                     // (by the conversion instruction: its pipe has room here, that of the permutations has none: 70 us, not 78)
-      const uint32_t u = r.w[i >> 1] >> (16 * (i & 1));
-      v[i] = make_float2((float)(signed char)u, (float)(signed char)(u >> 8));
-    }
-  }
-}
 // The 8-bit copy of 16 bytes of a row; the lanes of a block of 32 sit side by side in a warp, all of them with the row or none.
 // q: where its bytes go, b: where the block's byte goes (by its first lane).
 template <typename T> __device__ __forceinline__ void write_copy(signed char* q, unsigned char* b, uint4 u, bool row, bool first) {
@@ -75,14 +55,6 @@ template <typename T> __device__ __forceinline__ void write_copy(signed char* q,
     else *reinterpret_cast<uint32_t*>(q) = copy_q4(w[0], w[1], is, byte);
     if (first) *b = (unsigned char)byte;
   }
-}
-// f(the activation as a constant): the choice is made once, not for every value.
-template <int A> struct ActIs { static constexpr int value = A; };
-template <typename F> __device__ __forceinline__ void with_act(int act, F&& f) {
-  if (act == ACT_MISH) f(ActIs<ACT_MISH>{});
-  else if (act == ACT_SILU) f(ActIs<ACT_SILU>{});
-  else if (act == ACT_GELU) f(ActIs<ACT_GELU>{});
-  else f(ActIs<ACT_NONE>{});
 }
 template <typename T, int V> __device__ __forceinline__ uint4 pack16(const float2* y) {
   if constexpr (sizeof(T) == 2) return make_uint4(pack_bf16(y[0].x, y[0].y), pack_bf16(y[1].x, y[1].y), pack_bf16(y[2].x, y[2].y), pack_bf16(y[3].x, y[3].y));
@@ -235,7 +207,6 @@ group_norm_slab_kernel(NormArgs g) {
 
 // Backward.  dz stays in registers between the sums and dx; h is taken from x again.  A thread owns four channels: with eight, the sums of
 // dz, dz h, dy a and dy and the shares of dgamma and dbeta do not fit the registers of three CTAs.
-constexpr int GN_GRAD_V = 4;
 template <typename T, int ITEMS, bool COPY>
 __global__ void __launch_bounds__(GN_THREADS, GN_SLAB_CTAS)
 group_norm_slab_grad_kernel(NormArgs g) {

@@ -136,18 +136,18 @@ int gcd(int a, int b) { while (b) { const int t = a % b; a = b; b = t; } return 
 bool set_fits(int C, int groups, int unit) { const int cg = C / groups; return (long long)min(unit / gcd(cg, unit), groups) * cg <= GN_MAX_WIDTH; }
 
 // Which groups a CTA takes, how its threads lie over them, how many CTAs share the positions.
-void norm_plan(NormArgs& g, int V, int elem, int sms, bool grad) {
-  const int cg = g.C / g.groups;
+void norm_plan(NormArgs& g, int V, int elem, int sms, bool grad, int most_ranks = 8) {
+  const int cg = g.C / g.groups, threads = grad ? GN_STREAM_THREADS : GN_THREADS;
   g.per_set = min(V / gcd(cg, V), g.groups);
   const int step = g.per_set;
   // rows of 128 bytes at least, where a row does not outgrow the threads
-  while (g.per_set + step <= g.groups && (g.per_set + step) * cg <= GN_THREADS * V && g.per_set * cg * elem < 128) g.per_set += step;
+  while (g.per_set + step <= g.groups && (g.per_set + step) * cg <= threads * V && g.per_set * cg * elem < 128) g.per_set += step;
   g.width = g.per_set * cg;
   g.sets = (g.groups + g.per_set - 1) / g.per_set;
-  g.cols = min((g.width + V - 1) / V, GN_THREADS);
-  g.lanes = GN_THREADS / g.cols;
+  g.cols = min((g.width + V - 1) / V, threads);
+  g.lanes = threads / g.cols;
   g.ranks = 1;
-  while (g.ranks < 8 && (long long)g.N * g.sets * g.ranks < 2 * sms && g.L >= 8ll * g.lanes * g.ranks) g.ranks *= 2;
+  while (g.ranks < most_ranks && (long long)g.N * g.sets * g.ranks < 2 * sms && g.L >= 8ll * g.lanes * g.ranks) g.ranks *= 2;
   const long long fill = (long long)sms * 4 / ((long long)g.sets * g.ranks);
   g.splits = (int)min((long long)g.N, max(1ll, grad ? fill : (1ll << 24) / ((long long)g.sets * g.ranks)));
 }
@@ -283,9 +283,9 @@ cudaError_t norm_backward(NormArgs& g, int form, int items, int bytes, int devic
                         : (items <= 2 ? norm_slab_grad<T, 2, COPY>(g, bytes, device, s) : norm_slab_grad<T, 4, COPY>(g, bytes, device, s));
   }
   static std::atomic<unsigned long long> done{0};
-  const int smem = (4 * GN_THREADS * V + 8 * g.width + 2 * g.per_set) * 4;
-  const cudaError_t e = allow_smem(group_norm_grad_kernel<T, V, COPY>, (4 * GN_THREADS * V + 10 * GN_MAX_WIDTH) * 4, device, done);
-  return e != cudaSuccess ? e : launch(group_norm_grad_kernel<T, V, COPY>, (unsigned)((long long)g.splits * g.sets * g.ranks), GN_THREADS, g.ranks, smem, s, g);
+  const int smem = (4 * GN_STREAM_THREADS * V + 8 * g.width + 2 * g.per_set) * 4;
+  const cudaError_t e = allow_smem(group_norm_grad_kernel<T, V, COPY>, (4 * GN_STREAM_THREADS * V + 10 * GN_MAX_WIDTH) * 4, device, done);
+  return e != cudaSuccess ? e : launch(group_norm_grad_kernel<T, V, COPY>, (unsigned)((long long)g.splits * g.sets * g.ranks), GN_STREAM_THREADS, g.ranks, smem, s, g);
 }
 
 size_t norm_grad_bytes(const NormArgs& g) { return (size_t)g.splits * 2 * g.C * 4; }
@@ -414,14 +414,14 @@ size_t tsdp_group_norm_grad_workspace(int device, const tsdp_norm_t* shape) {
   size_t most = 16;
   const int elem = (int)esize(shape->dtype), sms = device_sms(device);
   for (int form = 0; form < 7; ++form) {                 // one value at a time, 16 bytes, four forms of slabs, warps
-    const int V = form == 0 ? 1 : 16 / elem;
+    const int V = form == 0 ? 1 : 16 / elem;                 // (form 1: 16 bytes, form 0: one value at a time)
     if (!set_fits(shape->C, shape->groups, V)) continue;
     NormArgs g{};
     float some;
     int items, bytes;
     g.N = shape->N < 1 ? 1 : shape->N; g.L = shape->L; g.C = shape->C; g.groups = shape->groups;
     g.dfilm = form & 1 ? &some : nullptr;
-    if (form < 2) norm_plan(g, V, elem, sms, true);
+    if (form < 2) norm_plan(g, form == 0 ? 1 : GN_GRAD_V, elem, sms, true);
     else if (form == 6 ? !warp_plan(g, GN_GRAD_V, elem == 2 ? 8 : 4, 2, sms, items) : !slab_plan(g, GN_GRAD_V, V, elem, sms, true, form >= 4, items, bytes)) continue;
     if (norm_grad_bytes(g) > most) most = norm_grad_bytes(g);
   }
@@ -466,10 +466,10 @@ int tsdp_group_norm_grad(int device, const tsdp_norm_t* shape, const void* d_dy,
     if ((!copy || aligned16(g.cx.q)) && warp_plan(g, GN_GRAD_V, dtype == TSDP_TYPE_BF16 ? 8 : 4, 2, sms, items)) form = GRAD_WARPS;
     else if ((!copy || aligned16(g.cx.q)) && slab_plan(g, GN_GRAD_V, V, (int)esize(dtype), sms, true, copy, items, bytes)) form = GRAD_SLABS;
   }
-  if (form == GRAD_STREAM) norm_plan(g, V, (int)esize(dtype), sms, true);
+  if (form == GRAD_STREAM) norm_plan(g, wide ? GN_GRAD_V : 1, (int)esize(dtype), sms, true);
   if (workspace_bytes < norm_grad_bytes(g)) return TSDP_ERR_ARG;
   if (dtype == TSDP_TYPE_BF16) {
-    if (wide) e = copy ? norm_backward<__nv_bfloat16, 8, true>(g, form, items, bytes, device, s) : norm_backward<__nv_bfloat16, 8, false>(g, form, items, bytes, device, s);
+    if (wide) e = copy ? norm_backward<__nv_bfloat16, 4, true>(g, form, items, bytes, device, s) : norm_backward<__nv_bfloat16, 4, false>(g, form, items, bytes, device, s);
     else e = copy ? norm_backward<__nv_bfloat16, 1, true>(g, form, items, bytes, device, s) : norm_backward<__nv_bfloat16, 1, false>(g, form, items, bytes, device, s);
   } else {
     if (wide) e = copy ? norm_backward<float, 4, true>(g, form, items, bytes, device, s) : norm_backward<float, 4, false>(g, form, items, bytes, device, s);

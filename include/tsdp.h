@@ -421,7 +421,7 @@ int tsdp_verify_commit_static(int device, int T, float beta0, float beta1, float
  * Tensors are [N, L, C] (sequences, positions, channels), channels innermost without a gap, strides x_n of a sequence and x_l of a
  * position in ELEMENTS (so the zero-padded layout and channel slices of wider rows can be given as they are); what lies between
  * rows is neither read nor written.  Rows in 16-byte pieces (strides, C and address) take the fast kernels, all others
- * are served too.  N = 0 is a call with nothing to do (gradients of parameters become zero).
+ * are served too.  N, L <= 2^30, C <= 2^24.  N = 0 is a call with nothing to do (gradients of parameters become zero).
  * Errors: ARG (null pointers, sizes, strides under which written rows overlap, workspace too small), CUDA (text on stderr). */
 enum { TSDP_TYPE_FP32 = 0, TSDP_TYPE_BF16 = 1 };
 enum { TSDP_ACT_NONE = 0, TSDP_ACT_MISH = 1, TSDP_ACT_SILU = 2, TSDP_ACT_GELU = 3 /* tanh form */ };

@@ -48,10 +48,7 @@ __device__ __forceinline__ uint2 copy_q8(const float2* x, float inv, uint32_t b)
   const float2 k = make_float2(inv, inv), magic = make_float2(12582912.f, 12582912.f);
   return make_uint2(copy_bytes(__ffma2_rn(x[0], k, magic), __ffma2_rn(x[1], k, magic)), copy_bytes(__ffma2_rn(x[2], k, magic), __ffma2_rn(x[3], k, magic)));
 }
-__device__ __forceinline__ uint32_t copy_q4(const float* x, float inv, uint32_t b) {
-  return copy_q4(make_float2(x[0], x[1]), make_float2(x[2], x[3]), inv, b);
-}
-// Largest magnitude (as bits) of eight bf16 values over `lanes` neighbouring lanes, two at a time and a NaN above all; of four fp32 ones.
+// Largest magnitude (as bits) of eight bf16 values in each of LANES neighbouring lanes, two at a time and a NaN above all; of four fp32 ones.
 template <int LANES> __device__ __forceinline__ uint32_t copy_top_bf16(uint4 u) {
   auto larger = [](uint32_t a, uint32_t b) {
     const __nv_bfloat162 m = __hmax2_nan(*reinterpret_cast<const __nv_bfloat162*>(&a), *reinterpret_cast<const __nv_bfloat162*>(&b));
@@ -86,20 +83,7 @@ __device__ __forceinline__ __nv_bfloat162 copy_step2(uint32_t b) {           // 
   return *reinterpret_cast<const __nv_bfloat162*>(&s);
 }
 
-// V consecutive values as fp32; V * sizeof(T) = 16 bytes, or one value.
-template <typename T, int V> __device__ __forceinline__ void load_values(const T* p, float* v) {
-  if constexpr (V == 1) {
-    v[0] = to_f(*p);
-  } else if constexpr (sizeof(T) == 2) {
-    const uint4 u = *reinterpret_cast<const uint4*>(p);
-    const uint32_t w[4] = {u.x, u.y, u.z, u.w};
-#pragma unroll
-    for (int i = 0; i < 4; ++i) { v[2 * i] = __uint_as_float(w[i] << 16); v[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u); }
-  } else {
-    const float4 u = *reinterpret_cast<const float4*>(p);
-    v[0] = u.x; v[1] = u.y; v[2] = u.z; v[3] = u.w;
-  }
-}
+// V fp32 values rounded to their type; V * sizeof(T) = 16 bytes, or one value.
 template <typename T, int V> __device__ __forceinline__ void store_values(T* p, const float* v) {
   if constexpr (V == 1) {
     *p = from_f<T>(v[0]);

@@ -18,6 +18,7 @@ using namespace tsdp;
 namespace {
 
 constexpr int MAX_DEVICES = 64;
+constexpr int MOST_ROWS = 1 << 30, MOST_CHANNELS = 1 << 24;      // of N and L, of C: counters step past them without leaving 32 bits
 
 // The caller's device for the time of a call, the one that was current afterwards.
 struct DeviceScope {
@@ -126,7 +127,7 @@ cudaError_t unpack(Copy8 in, const Rows& x, int N, int L, int C, int sms, cudaSt
 
 // ---------------------------------------------------------------------------------------------------------- GroupNorm
 bool norm_ok(const tsdp_norm_t* n) {
-  return n && dtype_ok(n->dtype) && n->N >= 0 && n->L >= 1 && n->C >= 1 && n->groups >= 1 && n->C % n->groups == 0 &&
+  return n && dtype_ok(n->dtype) && n->N >= 0 && n->N <= MOST_ROWS && n->L >= 1 && n->L <= MOST_ROWS && n->C >= 1 && n->C <= MOST_CHANNELS && n->groups >= 1 && n->C % n->groups == 0 &&
          n->C / n->groups <= GN_MAX_WIDTH && n->act >= TSDP_ACT_NONE && n->act <= TSDP_ACT_GELU && n->eps > 0.f && n->eps < 1e30f;
 }
 
@@ -136,7 +137,7 @@ int gcd(int a, int b) { while (b) { const int t = a % b; a = b; b = t; } return 
 bool set_fits(int C, int groups, int unit) { const int cg = C / groups; return (long long)min(unit / gcd(cg, unit), groups) * cg <= GN_MAX_WIDTH; }
 
 // Which groups a CTA takes, how its threads lie over them, how many CTAs share the positions.
-void norm_plan(NormArgs& g, int V, int elem, int sms, bool grad, int most_ranks = 8) {
+void norm_plan(NormArgs& g, int V, int elem, int sms, bool grad) {
   const int cg = g.C / g.groups, threads = grad ? GN_STREAM_THREADS : GN_THREADS;
   g.per_set = min(V / gcd(cg, V), g.groups);
   const int step = g.per_set;
@@ -147,7 +148,7 @@ void norm_plan(NormArgs& g, int V, int elem, int sms, bool grad, int most_ranks 
   g.cols = min((g.width + V - 1) / V, threads);
   g.lanes = threads / g.cols;
   g.ranks = 1;
-  while (g.ranks < most_ranks && (long long)g.N * g.sets * g.ranks < 2 * sms && g.L >= 8ll * g.lanes * g.ranks) g.ranks *= 2;
+  while (g.ranks < 8 && (long long)g.N * g.sets * g.ranks < 2 * sms && g.L >= 8ll * g.lanes * g.ranks) g.ranks *= 2;
   const long long fill = (long long)sms * 4 / ((long long)g.sets * g.ranks);
   g.splits = (int)min((long long)g.N, max(1ll, grad ? fill : (1ll << 24) / ((long long)g.sets * g.ranks)));
 }
@@ -346,7 +347,7 @@ bool wgrad_ok(int dtype, long long N, int L, int K, int O, int taps) {
 extern "C" {
 
 int tsdp_checkpoint_pack(int device, int dtype, const void* d_x, int64_t x_n, int64_t x_l, int N, int L, int C, const tsdp_saved_t* out, void* stream) {
-  if (device < 0 || device >= MAX_DEVICES || !dtype_ok(dtype) || N < 0 || L < 0 || C < 1 || !strides_ok(x_n, x_l)) return TSDP_ERR_ARG;
+  if (device < 0 || device >= MAX_DEVICES || !dtype_ok(dtype) || N < 0 || N > MOST_ROWS || L < 0 || L > MOST_ROWS || C < 1 || C > MOST_CHANNELS || !strides_ok(x_n, x_l)) return TSDP_ERR_ARG;
   if (N == 0 || L == 0) return TSDP_OK;
   if (!d_x || !copy_ok(out)) return TSDP_ERR_ARG;
   DeviceScope scope(device);
@@ -359,7 +360,7 @@ int tsdp_checkpoint_pack(int device, int dtype, const void* d_x, int64_t x_n, in
 }
 
 int tsdp_checkpoint_unpack(int device, int dtype, const tsdp_saved_t* in, void* d_x, int64_t x_n, int64_t x_l, int N, int L, int C, void* stream) {
-  if (device < 0 || device >= MAX_DEVICES || !dtype_ok(dtype) || N < 0 || L < 0 || C < 1 || !strides_ok(x_n, x_l)) return TSDP_ERR_ARG;
+  if (device < 0 || device >= MAX_DEVICES || !dtype_ok(dtype) || N < 0 || N > MOST_ROWS || L < 0 || L > MOST_ROWS || C < 1 || C > MOST_CHANNELS || !strides_ok(x_n, x_l)) return TSDP_ERR_ARG;
   if (N == 0 || L == 0) return TSDP_OK;
   if (!d_x || !copy_ok(in) || !rows_apart(N, L, C, x_n, x_l)) return TSDP_ERR_ARG;
   DeviceScope scope(device);

@@ -189,6 +189,7 @@ def check_gradient(dy, x, saved, ga, be, G, mean, rstd, act, fi, dtype, dx=None)
     N, L, C = dy.shape
     w = C // G
     dx = torch.full_like(dy, float("nan")) if dx is None else dx
+    assert L <= 4096 and N <= 4096                    # (what DEPTH stands for)
     dga, dbe = torch.full((C,), float("nan"), device="cuda"), torch.full((C,), float("nan"), device="cuda")
     dfi = None if fi is None else torch.full((N, 2 * C), float("nan"), device="cuda")
     ws = torch.empty(binding.group_norm_grad_workspace(dy, G), dtype=torch.uint8, device="cuda")
@@ -239,6 +240,104 @@ def test_norm_gradient(N, L, C, G, act, film, saved, dtype):
         s = binding.saved_like(x)
         binding.checkpoint_pack(x, s)
     check_gradient(dy, None if saved else x, s, ga, be, G, mean, rstd, act, fi, dtype)
+
+
+# More sequences than a CTA, a warp or a cluster takes at once: each walks over several (a warp per group; a CTA per set of groups; clusters over
+# long sequences), an uneven number of them.
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("N,L,C,G", [(3001, 4, 256, 8), (2001, 16, 96, 4), (701, 600, 16, 2)])
+def test_walks_over_many_sequences(N, L, C, G, dtype):
+    rng, x, ga, be, fi = norm_inputs(N, L, C, G, dtype, True, N)
+    y, mean, rstd = torch.full_like(x, float("nan")), torch.empty(N, G, device="cuda"), torch.empty(N, G, device="cuda")
+    sx, sy = binding.saved_like(x), binding.saved_like(x)
+    binding.group_norm(x, ga, be, G, y, film=fi, mean=mean, rstd=rstd, saved_x=sx, saved_y=sy)
+    ry, rm, rr = train.group_norm(host(x), host(ga), host(be), G, "mish", host(fi))
+    assert (np.abs(host(y) - ry) <= norm_bound(dtype, x, ry, rm, rr, ga, fi, N, C, G)).all()
+    for t, s in ((x, sx), (y, sy)):
+        want = binding.saved_like(t)
+        binding.checkpoint_pack(t, want)
+        assert torch.equal(s[0], want[0]) and torch.equal(s[1], want[1])
+    dy = rng_tensor(rng, (N, L, C), dtype, 0.1)
+    check_gradient(dy, x, None, ga, be, G, mean, rstd, "mish", fi, dtype)
+    check_gradient(dy, None, sx, ga, be, G, mean, rstd, "mish", fi, dtype)
+
+
+def test_offsets_past_32_bits():
+    """Sequences and rows more than 2^32 bytes apart, in one buffer of 11 GB."""
+    far, N, L, C, G = (1 << 31) + 24, 3, 16, 64, 2
+    buf = torch.empty(2 * far + L * C + 64, dtype=torch.bfloat16, device="cuda")
+    x = torch.as_strided(buf, (N, L, C), (far, C, 1))
+    rng = np.random.default_rng(2)
+    x.copy_(rng_tensor(rng, (N, L, C), "bf16"))
+    near = x.contiguous()
+    ga, be = rng_tensor(rng, (C,), "fp32", 1, 0.2), rng_tensor(rng, (C,), "fp32", 0, 0.2)
+    mean, rstd = torch.empty(N, G, device="cuda"), torch.empty(N, G, device="cuda")
+    sx, want = binding.saved_like(near), torch.empty_like(near)
+    binding.group_norm(near, ga, be, G, want, mean=mean, rstd=rstd)
+    y = torch.empty_like(near)
+    binding.group_norm(x, ga, be, G, y, saved_x=sx)
+    assert torch.equal(y, want)
+    dx = [torch.empty_like(near) for _ in range(2)]
+    dga, dbe = torch.empty(C, device="cuda"), torch.empty(C, device="cuda")
+    ws = torch.empty(binding.group_norm_grad_workspace(near, G), dtype=torch.uint8, device="cuda")
+    for t, o in ((near, dx[0]), (x, dx[1])):
+        binding.group_norm_grad(t, t, ga, be, G, mean, rstd, o, dga, dbe, ws)
+    assert torch.equal(*dx)
+    x.zero_()
+    binding.checkpoint_unpack(sx, x)
+    back = torch.empty_like(near)
+    binding.checkpoint_unpack(sx, back)
+    assert torch.equal(x, back)
+    rows = torch.as_strided(buf, (3, C), (far, 1))                  # rows of a weight gradient's dy
+    rows.copy_(near[0, :3])
+    saved = (sx[0].view(-1, C)[:3].contiguous(), sx[1].view(-1, 2)[:3].contiguous())
+    check_weight(saved, rows, 1, 3)
+    # long sequences (clusters), one value at a time
+    wide = torch.as_strided(buf, (2, 300, 7), (far, 11, 1))
+    wide.copy_(rng_tensor(rng, (2, 300, 7), "bf16"))
+    tight = wide.contiguous()
+    m, r = torch.empty(2, 7, device="cuda"), torch.empty(2, 7, device="cuda")
+    a, b = torch.empty_like(tight), torch.empty_like(tight)
+    binding.group_norm(tight, ga[:7], be[:7], 7, a, mean=m, rstd=r)
+    binding.group_norm(wide, ga[:7], be[:7], 7, b)
+    assert torch.equal(a, b)
+    d1, d2, d3 = torch.empty(7, device="cuda"), torch.empty(7, device="cuda"), torch.empty_like(tight)
+    ws = torch.empty(binding.group_norm_grad_workspace(tight, 7), dtype=torch.uint8, device="cuda")
+    binding.group_norm_grad(tight, tight, ga[:7], be[:7], 7, m, r, a, d1, d2, ws)
+    binding.group_norm_grad(wide, wide, ga[:7], be[:7], 7, m, r, d3, d1, d2, ws)
+    assert torch.equal(a, d3)
+
+
+def test_broadcast_inputs():
+    """A dy of one position for all, an x of one sequence for all: strides of zero."""
+    N, L, C, G = 4, 16, 64, 2
+    rng, x, ga, be, _ = norm_inputs(N, L, C, G, "bf16", False, 6)
+    one, dy = x[:1].expand(N, L, C), rng_tensor(rng, (1, 1, C), "bf16", 0).expand(N, L, C)
+    mean, rstd = torch.empty(N, G, device="cuda"), torch.empty(N, G, device="cuda")
+    y, want = torch.empty(N, L, C, dtype=x.dtype, device="cuda"), torch.empty(N, L, C, dtype=x.dtype, device="cuda")
+    binding.group_norm(one, ga, be, G, y, mean=mean, rstd=rstd)
+    binding.group_norm(one.contiguous(), ga, be, G, want)
+    assert torch.equal(y, want)
+    check_gradient(dy, one, None, ga, be, G, mean, rstd, "mish", None, "bf16", torch.empty_like(y))
+    saved = binding.saved_like(x.view(N * L, C))
+    binding.checkpoint_pack(x.view(N * L, C), saved)
+    check_weight(saved, dy[0, :1].expand(N * L, C), 3, L)
+
+
+def test_gradients_in_place():
+    for L, C, G in ((16, 256, 8), (16, 96, 4), (700, 20, 2)):        # a warp per group, a CTA per set, clusters
+        rng, x, ga, be, fi = norm_inputs(3, L, C, G, "bf16", True, L)
+        mean, rstd = torch.empty(3, G, device="cuda"), torch.empty(3, G, device="cuda")
+        y = torch.empty_like(x)
+        binding.group_norm(x, ga, be, G, y, film=fi, mean=mean, rstd=rstd)
+        dy, dga, dbe = rng_tensor(rng, (3, L, C), "bf16", 0), torch.empty(C, device="cuda"), torch.empty(C, device="cuda")
+        ws = torch.empty(binding.group_norm_grad_workspace(dy, G), dtype=torch.uint8, device="cuda")
+        dx = torch.empty_like(dy)
+        binding.group_norm_grad(dy, x, ga, be, G, mean, rstd, dx, dga, dbe, ws, film=fi)
+        binding.group_norm_grad(dy, x, ga, be, G, mean, rstd, dy, dga, dbe, ws, film=fi)
+        assert torch.equal(dx, dy)
+        binding.group_norm(x, ga, be, G, x, film=fi)
+        assert torch.equal(x, y)
 
 
 def test_gradient_against_differences_of_the_kernel_itself():

@@ -21,7 +21,7 @@ def norm(N=2, L=4, C=64, groups=8, dtype=1, act=1, eps=1e-5):
 
 
 BAD_SHAPES = [dict(C=60), dict(groups=0), dict(L=0), dict(N=-1), dict(dtype=2), dict(act=4), dict(act=-1), dict(eps=0.0), dict(eps=float("nan")),
-              dict(C=4096, groups=1), dict(C=0)]
+              dict(C=4096, groups=1), dict(C=0), dict(N=(1 << 30) + 1), dict(L=(1 << 30) + 1), dict(C=1 << 25, groups=1 << 22)]
 
 
 @pytest.mark.parametrize("bad", BAD_SHAPES)

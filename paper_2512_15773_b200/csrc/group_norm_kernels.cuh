@@ -125,7 +125,7 @@ struct NormArgs {
   Copy8 cx, cy;                                // forward: 8-bit copies to write (q null: none); backward: cx is x
   float *dfilm, *part;                         // [N, 2C] or null; [splits, 2, C]
   // the plan: a set is `per_set` groups, `width` channels; cols threads on a position; `ranks` CTAs of a cluster share the positions
-  int per_set, sets, width, cols, lanes, ranks, splits;
+  int per_set, sets, width, cols, lanes, ranks, splits, threads;
   // slab kernels: threads of a group that a shuffle adds up; rows of partial sums left (of warps or lanes); bytes of a stage
   int fold, red_rows, stage_bytes;
 };
@@ -151,10 +151,10 @@ __global__ void __launch_bounds__(GN_THREADS, 2)
 group_norm_kernel(NormArgs g) {
   extern __shared__ __align__(16) float gn_smem[];
   pdl_wait();
-  const int cg = g.C / g.groups;
+  const int cg = g.C / g.groups, threads = blockDim.x;
   float* s_mean = gn_smem;                                  // [lanes][tile channels]
-  float* s_m2 = s_mean + GN_THREADS * V;                    // the same
-  float* s_grp = s_m2 + GN_THREADS * V;                     // [2][per_set]: this CTA's mean and M2
+  float* s_m2 = s_mean + threads * V;                    // the same
+  float* s_grp = s_m2 + threads * V;                     // [2][per_set]: this CTA's mean and M2
   float* s_stat = s_grp + 2 * g.per_set;                    // [2][per_set]: mean and rstd
   const uint32_t rank = g.ranks > 1 ? ptx::cluster_rank() : 0u;
   const int set = (blockIdx.x / g.ranks) % g.sets, split = blockIdx.x / g.ranks / g.sets;
@@ -202,7 +202,7 @@ group_norm_kernel(NormArgs g) {
       __syncthreads();
       // groups that this tile holds (a part of): a warp each
       const int t1 = min(width, t0 + tile);
-      for (int gr = t0 / cg + warp; gr * cg < t1; gr += GN_THREADS / 32) {
+      for (int gr = t0 / cg + warp; gr * cg < t1; gr += threads / 32) {
         const int a = max(gr * cg, t0) - t0, b = min(gr * cg + cg, t1) - t0, w = b - a, items = w * g.lanes;
         float sum = 0.f;
         for (int i = wl; i < items; i += 32) {
@@ -230,7 +230,7 @@ group_norm_kernel(NormArgs g) {
       __syncthreads();
     }
     if (g.ranks > 1) ptx::cluster_sync_all();
-    for (int gr = threadIdx.x; gr < n_grp; gr += GN_THREADS) {
+    for (int gr = threadIdx.x; gr < n_grp; gr += threads) {
       float m = s_grp[gr], m2 = s_grp[g.per_set + gr];
       if (g.ranks > 1) {
         m = 0.f; m2 = 0.f;
@@ -371,9 +371,9 @@ __global__ void __launch_bounds__(GN_STREAM_THREADS, 1)
 group_norm_grad_kernel(NormArgs g) {
   extern __shared__ __align__(16) float gn_smem[];
   pdl_wait();
-  const int cg = g.C / g.groups;
+  const int cg = g.C / g.groups, threads = blockDim.x;
   float* s_lane = gn_smem;                                  // [4][lanes][tile channels]: sums of a lane
-  float* s_sum = s_lane + 4 * GN_STREAM_THREADS * V;               // [4][width]: of the CTA
+  float* s_sum = s_lane + 4 * threads * V;               // [4][width]: of the CTA
   float* s_tot = s_sum + 4 * g.width;                       // [2][width]: of the cluster (dz, dz h)
   float* s_acc = s_tot + 2 * g.width;                       // [2][width]: over the sequences so far
   float* s_grp = s_acc + 2 * g.width;                       // [2][per_set]: m1, m2
@@ -385,7 +385,7 @@ group_norm_grad_kernel(NormArgs g) {
   const int warp = threadIdx.x >> 5, wl = threadIdx.x & 31;
   const bool film = g.film != nullptr && g.dfilm != nullptr;
   const int sums = film ? 4 : 2;
-  for (int i = threadIdx.x; i < 2 * g.width; i += GN_STREAM_THREADS) s_acc[i] = 0.f;
+  for (int i = threadIdx.x; i < 2 * g.width; i += threads) s_acc[i] = 0.f;
   for (int n = split; n < g.N; n += g.splits) {
     for (int t0 = 0; t0 < width; t0 += tile) {
       const int c = t0 + col * V;
@@ -403,22 +403,22 @@ group_norm_grad_kernel(NormArgs g) {
 #pragma unroll
         for (int i = 0; i < V; ++i) {
           float* o = s_lane + lane * tile + col * V + i;
-          o[0] = s0[i]; o[GN_STREAM_THREADS * V] = s1[i];
-          if (film) { o[2 * GN_STREAM_THREADS * V] = s2[i]; o[3 * GN_STREAM_THREADS * V] = s3[i]; }
+          o[0] = s0[i]; o[threads * V] = s1[i];
+          if (film) { o[2 * threads * V] = s2[i]; o[3 * threads * V] = s3[i]; }
         }
       }
       __syncthreads();
       const int w = min(width - t0, tile);
-      for (int i = threadIdx.x; i < sums * w; i += GN_STREAM_THREADS) {
+      for (int i = threadIdx.x; i < sums * w; i += threads) {
         const int k = i / w, cc = i - k * w;
         float s = 0.f;
-        for (int r = 0; r < g.lanes; ++r) s += s_lane[k * GN_STREAM_THREADS * V + r * tile + cc];
+        for (int r = 0; r < g.lanes; ++r) s += s_lane[k * threads * V + r * tile + cc];
         s_sum[k * g.width + t0 + cc] = s;
       }
       __syncthreads();
     }
     if (g.ranks > 1) ptx::cluster_sync_all();
-    for (int i = threadIdx.x; i < sums * width; i += GN_STREAM_THREADS) {
+    for (int i = threadIdx.x; i < sums * width; i += threads) {
       const int k = i / width, c = i - k * width;
       float s = s_sum[k * g.width + c];
       if (g.ranks > 1) {
@@ -430,7 +430,7 @@ group_norm_grad_kernel(NormArgs g) {
     }
     __syncthreads();
     const float inv = 1.f / ((float)g.L * cg);
-    for (int gr = warp; gr < n_grp; gr += GN_STREAM_THREADS / 32) {
+    for (int gr = warp; gr < n_grp; gr += threads / 32) {
       float a = 0.f, b = 0.f;
       for (int i = wl; i < cg; i += 32) {
         const float ga = g.gamma[c_set + gr * cg + i];
@@ -460,7 +460,7 @@ group_norm_grad_kernel(NormArgs g) {
   }
   __syncthreads();
   if (rank == 0)
-    for (int i = threadIdx.x; i < 2 * width; i += GN_STREAM_THREADS) {
+    for (int i = threadIdx.x; i < 2 * width; i += threads) {
       const int k = i / width, c = i - k * width;
       g.part[((long long)split * 2 + k) * g.C + c_set + c] = s_acc[k * g.width + c];
     }

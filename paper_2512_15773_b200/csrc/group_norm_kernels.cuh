@@ -128,6 +128,7 @@ struct NormArgs {
   int per_set, sets, width, cols, lanes, ranks, splits, threads;
   // slab kernels: threads of a group that a shuffle adds up; rows of partial sums left (of warps or lanes); bytes of a stage
   int fold, red_rows, stage_bytes;
+  int team;                                    // warp kernels: warps of a group (0 elsewhere)
 };
 
 constexpr int GN_GRAD_V = 4;                   // channels of a thread in the backward pass: with eight its sums do not fit the registers

@@ -197,14 +197,16 @@ bool slab_plan(NormArgs& g, int V, int unit, int elem, int sms, bool grad, bool 
   return true;
 }
 
-// One warp per group: false where a group's channels are not 32, 64, 128 or 256 or a lane would hold more than `most` pieces of V channels.
+// Teams of warps: false where a group's channels are not 32, 64, 128 or 256 or a lane of eight warps would hold more than `most` pieces of V channels.
 bool warp_plan(NormArgs& g, int V, int most, int ctas, int sms, int& items) {
   const int cg = g.C / g.groups;
   if (cg < 32 || cg > 256 || (cg & (cg - 1)) || cg / V > 32) return false;
   const int R = 32 / (cg / V);
-  if (g.L > most * R) return false;
-  items = (g.L + R - 1) / R;
-  const long long places = max(1ll, (long long)sms * ctas * (GN_WARP_THREADS / 32) / g.groups), turns = (g.N + places - 1) / places;
+  g.team = 1;
+  while (g.team < GN_WARP_THREADS / 32 && g.L > most * R * g.team) g.team *= 2;
+  if (g.L > most * R * g.team) { g.team = 0; return false; }
+  items = (g.L + R * g.team - 1) / (R * g.team);
+  const long long places = max(1ll, (long long)sms * ctas * (GN_WARP_THREADS / 32) / ((long long)g.groups * g.team)), turns = (g.N + places - 1) / places;
   g.splits = (int)((g.N + turns - 1) / turns);
   g.sets = g.ranks = 1;
   return true;
@@ -225,33 +227,36 @@ cudaError_t norm_slab_grad(const NormArgs& g, int smem, int device, cudaStream_t
 
 template <typename F>
 cudaError_t launch_warps(F kern, const NormArgs& g, int smem, cudaStream_t s) {
-  const long long warps = (long long)g.splits * g.groups;
+  const long long warps = (long long)g.splits * g.groups * g.team;
   return launch(kern, (unsigned)((warps + GN_WARP_THREADS / 32 - 1) / (GN_WARP_THREADS / 32)), GN_WARP_THREADS, 1, smem, s, g);
 }
-template <typename T, int ITEMS>
+template <typename T, int ITEMS, bool TEAM = false>
 cudaError_t norm_warp_items(const NormArgs& g, int device, cudaStream_t s) {
   static std::atomic<unsigned long long> done{0};
   constexpr int per = GN_WARP_THREADS / 32 * GN_WARP_STAGES;
-  const cudaError_t e = allow_smem(group_norm_warp_kernel<T, ITEMS>, per * gn_warp_stage(ITEMS, 256), device, done);
-  return e != cudaSuccess ? e : launch_warps(group_norm_warp_kernel<T, ITEMS>, g, per * gn_warp_stage(ITEMS, g.C / g.groups), s);
+  const cudaError_t e = allow_smem(group_norm_warp_kernel<T, ITEMS, TEAM>, per * gn_warp_stage(ITEMS, 256), device, done);
+  return e != cudaSuccess ? e : launch_warps(group_norm_warp_kernel<T, ITEMS, TEAM>, g, per * gn_warp_stage(ITEMS, g.C / g.groups), s);
 }
+// (a lane of a team holds more than half of the most it may: one form of it)
 template <typename T>
 cudaError_t norm_warp(const NormArgs& g, int items, int device, cudaStream_t s) {
+  if (g.team > 1) return norm_warp_items<T, sizeof(T) == 2 ? 4 : 8, true>(g, device, s);
   if (items <= 1) return norm_warp_items<T, 1>(g, device, s);
   if (items <= 2) return norm_warp_items<T, 2>(g, device, s);
   if constexpr (sizeof(T) == 4)
     if (items > 4) return norm_warp_items<T, 8>(g, device, s);
   return norm_warp_items<T, 4>(g, device, s);
 }
-template <typename T, int ITEMS, bool COPY>
+template <typename T, int ITEMS, bool COPY, bool TEAM = false>
 cudaError_t norm_warp_grad_items(const NormArgs& g, int device, cudaStream_t s) {
   static std::atomic<unsigned long long> done{0};
-  constexpr int smem = gn_warp_grad_smem<T, COPY>(ITEMS);
-  const cudaError_t e = allow_smem(group_norm_warp_grad_kernel<T, ITEMS, COPY>, smem, device, done);
-  return e != cudaSuccess ? e : launch_warps(group_norm_warp_grad_kernel<T, ITEMS, COPY>, g, smem, s);
+  constexpr int smem = gn_warp_grad_smem<T, COPY>(ITEMS), film = 2 * GN_WARP_THREADS / 32 * 2 * 4;      // (film: a channel of a team)
+  const cudaError_t e = allow_smem(group_norm_warp_grad_kernel<T, ITEMS, COPY, TEAM>, smem + film * 128, device, done);
+  return e != cudaSuccess ? e : launch_warps(group_norm_warp_grad_kernel<T, ITEMS, COPY, TEAM>, g, smem + (TEAM && g.dfilm ? film * (g.C / g.groups) : 0), s);
 }
 template <typename T, bool COPY>
 cudaError_t norm_warp_grad(const NormArgs& g, int items, int device, cudaStream_t s) {
+  if (g.team > 1) return norm_warp_grad_items<T, sizeof(T) == 2 ? 8 : 4, COPY, true>(g, device, s);
   if (items <= 1) return norm_warp_grad_items<T, 1, COPY>(g, device, s);
   if (items <= 2) return norm_warp_grad_items<T, 2, COPY>(g, device, s);
   if constexpr (sizeof(T) == 2)
@@ -293,7 +298,8 @@ cudaError_t norm_backward(NormArgs& g, int form, int items, int bytes, int devic
   return e != cudaSuccess ? e : launch(group_norm_grad_kernel<T, V, COPY>, (unsigned)((long long)g.splits * g.sets * g.ranks), g.threads, g.ranks, smem, s, g);
 }
 
-size_t norm_grad_bytes(const NormArgs& g) { return (size_t)g.splits * 2 * g.C * 4; }
+int norm_shares(const NormArgs& g) { return g.splits * max(1, g.team); }
+size_t norm_grad_bytes(const NormArgs& g) { return (size_t)norm_shares(g) * 2 * g.C * 4; }
 
 // ------------------------------------------------------------------------------------------------------ weight gradient
 typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
@@ -481,7 +487,7 @@ int tsdp_group_norm_grad(int device, const tsdp_norm_t* shape, const void* d_dy,
     else e = copy ? norm_backward<float, 1, true>(g, form, items, bytes, device, s) : norm_backward<float, 1, false>(g, form, items, bytes, device, s);
   }
   if (e == cudaSuccess) {
-    e = launch(group_norm_join_kernel, (unsigned)(2 * ((C + GN_JOIN_CH - 1) / GN_JOIN_CH)), GN_JOIN_CH * GN_JOIN_LANES, 1, 0, s, (const float*)g.part, g.splits, C, d_dgamma, d_dbeta);
+    e = launch(group_norm_join_kernel, (unsigned)(2 * ((C + GN_JOIN_CH - 1) / GN_JOIN_CH)), GN_JOIN_CH * GN_JOIN_LANES, 1, 0, s, (const float*)g.part, norm_shares(g), C, d_dgamma, d_dbeta);
   }
   return e == cudaSuccess ? TSDP_OK : fail_cuda("tsdp_group_norm_grad", e);
 }

@@ -111,7 +111,8 @@ def norm_inputs(N, L, C, G, dtype, film, seed, layout="dense", offset=0.5):
 
 # sizes: single values, one position, UNet levels, odd widths, groups wider than a CTA's threads, long sequences over several CTAs
 NORM_SIZES = [(1, 1, 8, 1), (2, 1, 5, 5), (3, 7, 6, 3), (1, 16, 256, 8), (5, 16, 512, 8), (2, 4, 1024, 8), (3, 33, 40, 4), (2, 50, 1024, 1),
-              (2, 700, 320, 32), (1, 1500, 64, 8), (1, 2500, 77, 7), (2, 9, 2048, 1), (3, 5, 2049, 3), (1, 3, 2000, 2), (40, 8, 96, 32), (700, 16, 64, 8)]
+              (2, 700, 320, 32), (1, 1500, 64, 8), (1, 2500, 77, 7), (2, 9, 2048, 1), (3, 5, 2049, 3), (1, 3, 2000, 2), (40, 8, 96, 32), (700, 16, 64, 8),
+              (3, 50, 256, 2), (2, 100, 64, 2), (2, 33, 128, 2), (1, 17, 1024, 16)]
 
 
 def norm_bound(dtype, x, y, mean, rstd, ga, fi, N, C, G):
@@ -145,7 +146,8 @@ def test_norm(N, L, C, G, act, film, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
-@pytest.mark.parametrize("N,L,C,G", [(2, 16, 256, 8), (3, 5, 40, 4), (2, 7, 77, 7), (1, 900, 96, 3), (2, 3, 2000, 2), (30, 16, 64, 8)])
+@pytest.mark.parametrize("N,L,C,G", [(2, 16, 256, 8), (3, 5, 40, 4), (2, 7, 77, 7), (1, 900, 96, 3), (2, 3, 2000, 2), (30, 16, 64, 8),
+                                     (3, 41, 128, 2)])
 def test_norm_saves_copies_of_its_input_and_output(N, L, C, G, dtype):
     rng, x, ga, be, fi = norm_inputs(N, L, C, G, dtype, True, 11 * C)
     y, plain = torch.empty_like(x), torch.empty_like(x)
@@ -245,7 +247,7 @@ def test_norm_gradient(N, L, C, G, act, film, saved, dtype):
 # More sequences than a CTA, a warp or a cluster takes at once: each walks over several (a warp per group; a CTA per set of groups; clusters over
 # long sequences), an uneven number of them.
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
-@pytest.mark.parametrize("N,L,C,G", [(3001, 4, 256, 8), (2001, 16, 96, 4), (701, 600, 16, 2)])
+@pytest.mark.parametrize("N,L,C,G", [(3001, 4, 256, 8), (901, 50, 128, 2), (2001, 16, 96, 4), (701, 600, 16, 2)])
 def test_walks_over_many_sequences(N, L, C, G, dtype):
     rng, x, ga, be, fi = norm_inputs(N, L, C, G, dtype, True, N)
     y, mean, rstd = torch.full_like(x, float("nan")), torch.empty(N, G, device="cuda"), torch.empty(N, G, device="cuda")

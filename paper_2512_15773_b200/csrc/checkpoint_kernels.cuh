@@ -83,17 +83,6 @@ __device__ __forceinline__ __nv_bfloat162 copy_step2(uint32_t b) {           // 
   return *reinterpret_cast<const __nv_bfloat162*>(&s);
 }
 
-// V fp32 values rounded to their type; V * sizeof(T) = 16 bytes, or one value.
-template <typename T, int V> __device__ __forceinline__ void store_values(T* p, const float* v) {
-  if constexpr (V == 1) {
-    *p = from_f<T>(v[0]);
-  } else if constexpr (sizeof(T) == 2) {
-    *reinterpret_cast<uint4*>(p) = make_uint4(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7]));
-  } else {
-    *reinterpret_cast<float4*>(p) = make_float4(v[0], v[1], v[2], v[3]);
-  }
-}
-
 // Row r = n L + l of a tensor [N, L, C].
 __device__ __forceinline__ long long row_offset(const Rows& x, long long r, int N, int L) {
   if (N == 1) return r * x.sl;

@@ -58,23 +58,6 @@ template <bool GRAD> __device__ __forceinline__ void act_pair(int act, float2 z,
     if (GRAD) d = two(1.f);
   }
 }
-template <bool GRAD, int V> __device__ __forceinline__ void act_values(int act, const float* z, float* a, float* d) {      // act: a constant at the call
-  if constexpr (V == 1) {
-    float2 av, dv;
-    act_pair<GRAD>(act, two(z[0]), av, dv);
-    a[0] = av.x;
-    if (GRAD) d[0] = dv.x;
-  } else {
-#pragma unroll
-    for (int i = 0; i < V; i += 2) {
-      float2 av, dv;
-      act_pair<GRAD>(act, make_float2(z[i], z[i + 1]), av, dv);
-      a[i] = av.x; a[i + 1] = av.y;
-      if (GRAD) { d[i] = dv.x; d[i + 1] = dv.y; }
-    }
-  }
-}
-
 // V values (4, 8 or 16 bytes, or one value) of memory as they are.
 template <typename T, int V> struct Piece { uint32_t w[V == 1 ? 1 : V * sizeof(T) / 4]; };
 template <typename T, int V> __device__ __forceinline__ Piece<T, V> load_piece(const uint8_t* p) {
@@ -96,15 +79,17 @@ template <typename T, int V> __device__ __forceinline__ void piece_values(const 
     }
   }
 }
-template <typename T, int V> __device__ __forceinline__ void piece_floats(const Piece<T, V>& r, float* v) {
-  if constexpr (V == 1) {
-    v[0] = sizeof(T) == 4 ? __uint_as_float(r.w[0]) : sizeof(T) == 2 ? __uint_as_float(r.w[0] << 16) : (float)(signed char)r.w[0];
-  } else {
-    float2 f[V / 2];
-    piece_values<T, V>(r, f);
-#pragma unroll
-    for (int i = 0; i < V / 2; ++i) { v[2 * i] = f[i].x; v[2 * i + 1] = f[i].y; }
-  }
+// The same as pairs; one value stands with a zero.
+template <typename T, int V> __device__ __forceinline__ void piece_pairs(const Piece<T, V>& r, float2* v) {
+  if constexpr (V == 1) v[0] = make_float2(sizeof(T) == 4 ? __uint_as_float(r.w[0]) : sizeof(T) == 2 ? __uint_as_float(r.w[0] << 16) : (float)(signed char)r.w[0], 0.f);
+  else piece_values<T, V>(r, v);
+}
+__host__ __device__ constexpr int pairs_of(int V) { return V > 1 ? V / 2 : 1; }
+template <typename T, int V> __device__ __forceinline__ void store_pairs(T* p, const float2* v) {
+  if constexpr (V == 1) *p = from_f<T>(v[0].x);
+  else if constexpr (sizeof(T) == 2 && V == 8) *reinterpret_cast<uint4*>(p) = make_uint4(pack_bf16(v[0].x, v[0].y), pack_bf16(v[1].x, v[1].y), pack_bf16(v[2].x, v[2].y), pack_bf16(v[3].x, v[3].y));
+  else if constexpr (sizeof(T) == 2) *reinterpret_cast<uint2*>(p) = make_uint2(pack_bf16(v[0].x, v[0].y), pack_bf16(v[1].x, v[1].y));
+  else *reinterpret_cast<float4*>(p) = make_float4(v[0].x, v[0].y, v[1].x, v[1].y);
 }
 
 // f(the activation as a constant): the choice is made once, not for every value.
@@ -131,8 +116,10 @@ struct NormArgs {
   int team;                                    // warp kernels: warps of a group (0 elsewhere)
 };
 
-constexpr int GN_GRAD_V = 4;                   // channels of a thread in the backward pass: with eight its sums do not fit the registers
+constexpr int GN_STREAM_V = 4;                 // channels of a thread over long sequences and in every backward pass: with eight (16 bytes of
+                                               // bf16) its vectors and sums do not fit the registers
 constexpr int GN_THREADS = 256, GN_STREAM_THREADS = 512;      // of the kernels; of the backward one over long sequences (few CTAs with much to fetch)
+constexpr int GN_MAX_RANKS = 8;               // CTAs of a cluster
 constexpr int GN_MAX_WIDTH = 2048;             // channels of a set: their sums stay in shared memory
 
 __device__ __forceinline__ float ld_rank_f32(const float* p, uint32_t rank) {       // the same shared-memory word of another CTA of the cluster
@@ -141,8 +128,12 @@ __device__ __forceinline__ float ld_rank_f32(const float* p, uint32_t rank) {   
   return v;
 }
 
-// Positions of lane r of a share [lo, hi) walked in steps of `lanes`.
-__device__ __forceinline__ int lane_rows(int lo, int hi, int r, int lanes) { return max(0, (hi - lo - r + lanes - 1) / lanes); }
+// Positions of lane r of a share that is walked in steps of `lanes`: `all` each, one more in the first `extra`.
+struct LaneRows {
+  int all, extra;
+  __device__ __forceinline__ LaneRows(int positions, int lanes) : all(positions / lanes), extra(positions % lanes) {}
+  __device__ __forceinline__ int operator()(int r) const { return all + (r < extra ? 1 : 0); }
+};
 
 // ------------------------------------------------------------------------------------------------------------------ forward
 // First walk: each thread keeps, per channel, the sums about its own first value (so that a large mean costs no digits); mean and centred
@@ -150,6 +141,7 @@ __device__ __forceinline__ int lane_rows(int lo, int hi, int r, int lanes) { ret
 template <typename T, int V>
 __global__ void __launch_bounds__(GN_THREADS, 2)
 group_norm_kernel(NormArgs g) {
+  constexpr int P = pairs_of(V);
   extern __shared__ __align__(16) float gn_smem[];
   pdl_wait();
   const int cg = g.C / g.groups, threads = blockDim.x;
@@ -163,6 +155,7 @@ group_norm_kernel(NormArgs g) {
   const int share = (g.L + g.ranks - 1) / g.ranks, lo = min(g.L, (int)rank * share), hi = min(g.L, lo + share);
   const int lane = threadIdx.x / g.cols, col = threadIdx.x - lane * g.cols, tile = g.cols * V;
   const int warp = threadIdx.x >> 5, wl = threadIdx.x & 31;
+  const LaneRows lane_rows(hi - lo, g.lanes);
   for (int n = split; n < g.N; n += g.splits) {
     const T* x = reinterpret_cast<const T*>(g.x.p) + n * g.x.sn + c_set;
     // a group may be wider than a tile of columns: its parts are merged in turn
@@ -170,13 +163,15 @@ group_norm_kernel(NormArgs g) {
       const int c = t0 + col * V;
       const bool in = lane < g.lanes && c < width;
       if (in) {
-        float k[V], s[V], q[V];
+        float2 k[P], s[P], q[P];
 #pragma unroll
-        for (int i = 0; i < V; ++i) k[i] = s[i] = q[i] = 0.f;
+        for (int i = 0; i < P; ++i) k[i] = s[i] = q[i] = two(0.f);
         int l = lo + lane;
         Piece<T, V> pivot{};
-        if (l < hi) { pivot = load_piece<T, V>(reinterpret_cast<const uint8_t*>(x + l * g.x.sl + c)); piece_floats<T, V>(pivot, k); }
-        constexpr int U = 8;
+        if (l < hi) { pivot = load_piece<T, V>(reinterpret_cast<const uint8_t*>(x + l * g.x.sl + c)); piece_pairs<T, V>(pivot, k); }
+#pragma unroll
+        for (int i = 0; i < P; ++i) k[i] = __fmul2_rn(k[i], two(-1.f));
+        constexpr int U = 8;                      // positions asked for together
         for (; l < hi; l += U * g.lanes) {
           Piece<T, V> raw[U];
 #pragma unroll
@@ -186,18 +181,19 @@ group_norm_kernel(NormArgs g) {
           }
 #pragma unroll
           for (int j = 0; j < U; ++j) {
-            float v[V];
-            piece_floats<T, V>(raw[j], v);
+            float2 v[P];
+            piece_pairs<T, V>(raw[j], v);
 #pragma unroll
-            for (int i = 0; i < V; ++i) { const float d = v[i] - k[i]; s[i] += d; q[i] = fmaf(d, d, q[i]); }
+            for (int i = 0; i < P; ++i) { const float2 d = __fadd2_rn(v[i], k[i]); s[i] = __fadd2_rn(s[i], d); q[i] = __ffma2_rn(d, d, q[i]); }
           }
         }
-        const int cnt = lane_rows(lo, hi, lane, g.lanes);
+        const int cnt = lane_rows(lane);
         const float inv = cnt ? 1.f / cnt : 0.f;
 #pragma unroll
         for (int i = 0; i < V; ++i) {
-          s_mean[lane * tile + col * V + i] = fmaf(s[i], inv, k[i]);
-          s_m2[lane * tile + col * V + i] = fmaf(-s[i] * inv, s[i], q[i]);
+          const float si = i & 1 ? s[i / 2].y : s[i / 2].x, qi = i & 1 ? q[i / 2].y : q[i / 2].x, ki = i & 1 ? k[i / 2].y : k[i / 2].x;
+          s_mean[lane * tile + col * V + i] = fmaf(si, inv, -ki);
+          s_m2[lane * tile + col * V + i] = fmaf(-si * inv, si, qi);
         }
       }
       __syncthreads();
@@ -205,16 +201,17 @@ group_norm_kernel(NormArgs g) {
       const int t1 = min(width, t0 + tile);
       for (int gr = t0 / cg + warp; gr * cg < t1; gr += threads / 32) {
         const int a = max(gr * cg, t0) - t0, b = min(gr * cg + cg, t1) - t0, w = b - a, items = w * g.lanes;
+        const float inv_w = 1.f / w;                         // (i / w of a few thousand by a product: off by less than the half it stands away from a whole number)
         float sum = 0.f;
         for (int i = wl; i < items; i += 32) {
-          const int r = i / w;
-          sum += lane_rows(lo, hi, r, g.lanes) * s_mean[r * tile + a + i - r * w];
+          const int r = (int)((i + 0.5f) * inv_w);
+          sum += lane_rows(r) * s_mean[r * tile + a + i - r * w];
         }
         const float cnt = (float)(hi - lo) * w;
         const float m = cnt > 0.f ? warp_sum(sum) / cnt : 0.f;
         float m2 = 0.f;
         for (int i = wl; i < items; i += 32) {
-          const int r = i / w, rows = lane_rows(lo, hi, r, g.lanes);
+          const int r = (int)((i + 0.5f) * inv_w), rows = lane_rows(r);
           const float d = s_mean[r * tile + a + i - r * w] - m;
           if (rows) m2 += s_m2[r * tile + a + i - r * w] + rows * d * d;
         }
@@ -234,13 +231,19 @@ group_norm_kernel(NormArgs g) {
     for (int gr = threadIdx.x; gr < n_grp; gr += threads) {
       float m = s_grp[gr], m2 = s_grp[g.per_set + gr];
       if (g.ranks > 1) {
+        float mr[GN_MAX_RANKS], qr[GN_MAX_RANKS];              // (all asked for before the first is used: each takes a quarter of a microsecond)
+#pragma unroll
+        for (int r = 0; r < GN_MAX_RANKS; ++r)
+          if (r < g.ranks) { mr[r] = ld_rank_f32(s_grp + gr, r); qr[r] = ld_rank_f32(s_grp + g.per_set + gr, r); }
         m = 0.f; m2 = 0.f;
-        for (int r = 0; r < g.ranks; ++r) m += ld_rank_f32(s_grp + gr, r) * (float)max(0, min(g.L, (r + 1) * share) - min(g.L, r * share));
+        auto rows_of = [&](int r) { return (float)max(0, min(g.L, (r + 1) * share) - min(g.L, r * share)); };
+#pragma unroll
+        for (int r = 0; r < GN_MAX_RANKS; ++r)
+          if (r < g.ranks) m += mr[r] * rows_of(r);
         m /= (float)g.L;
-        for (int r = 0; r < g.ranks; ++r) {
-          const float rows = (float)max(0, min(g.L, (r + 1) * share) - min(g.L, r * share)), d = ld_rank_f32(s_grp + gr, r) - m;
-          if (rows > 0.f) m2 += ld_rank_f32(s_grp + g.per_set + gr, r) + d * d * rows * cg;
-        }
+#pragma unroll
+        for (int r = 0; r < GN_MAX_RANKS; ++r)
+          if (r < g.ranks && rows_of(r) > 0.f) { const float d = mr[r] - m; m2 += qr[r] + d * d * rows_of(r) * cg; }
       }
       const float rs = rsqrtf(m2 / ((float)g.L * cg) + g.eps);
       s_stat[gr] = m; s_stat[g.per_set + gr] = rs;
@@ -256,19 +259,18 @@ group_norm_kernel(NormArgs g) {
     for (int t0 = 0; t0 < width; t0 += tile) {
       const int c = t0 + col * V;
       const bool in = lane < g.lanes && c < width;
-      float ga[V], be[V], mu[V], rs[V], fs[V], fb[V];
-#pragma unroll
-      for (int i = 0; i < V; ++i) { ga[i] = be[i] = mu[i] = rs[i] = fb[i] = 0.f; fs[i] = 1.f; }
-      if (in) {
-#pragma unroll
-        for (int i = 0; i < V; ++i) {
-          const int gr = (c + i) / cg;
-          ga[i] = g.gamma[c_set + c + i]; be[i] = g.beta[c_set + c + i];
-          mu[i] = s_stat[gr]; rs[i] = s_stat[g.per_set + gr];
-          if (g.film) { fs[i] = g.film[(long long)n * 2 * g.C + c_set + c + i]; fb[i] = g.film[((long long)n * 2 + 1) * g.C + c_set + c + i]; }
-        }
-      }
       if (!in) continue;
+      float2 ka[P], kb[P], fs[P], fb[P];                       // z = (x + kb) ka + beta, in two steps: x - mean first
+      float2 be[P];
+#pragma unroll
+      for (int i = 0; i < P; ++i) { ka[i] = kb[i] = be[i] = fb[i] = two(0.f); fs[i] = two(1.f); }
+#pragma unroll
+      for (int i = 0; i < V; ++i) {
+        const int ch = c_set + c + i, gr = (c + i) / cg;
+        auto set = [&](float2* a, float v) { if (i & 1) a[i / 2].y = v; else a[i / 2].x = v; };
+        set(ka, g.gamma[ch] * s_stat[g.per_set + gr]); set(kb, -s_stat[gr]); set(be, g.beta[ch]);
+        if (g.film) { set(fs, g.film[(long long)n * 2 * g.C + ch]); set(fb, g.film[((long long)n * 2 + 1) * g.C + ch]); }
+      }
       with_act(g.act, [&](auto act) {
         constexpr int U = 4;                                   // positions asked for together
         for (int l = lo + lane; l < hi; l += U * g.lanes) {
@@ -279,14 +281,15 @@ group_norm_kernel(NormArgs g) {
 #pragma unroll
           for (int j = 0; j < U; ++j) {
             if (l + j * g.lanes >= hi) break;
-            float v[V], z[V], a[V], d[V];
-            piece_floats<T, V>(raw[j], v);
+            float2 v[P];
+            piece_pairs<T, V>(raw[j], v);
 #pragma unroll
-            for (int i = 0; i < V; ++i) z[i] = fmaf((v[i] - mu[i]) * rs[i], ga[i], be[i]);
-            act_values<false, V>(decltype(act)::value, z, a, d);
-#pragma unroll
-            for (int i = 0; i < V; ++i) a[i] = fmaf(a[i], fs[i], fb[i]);
-            store_values<T, V>(y + (l + j * g.lanes) * g.y.sl + c, a);
+            for (int i = 0; i < P; ++i) {
+              float2 d;
+              act_pair<false>(decltype(act)::value, __ffma2_rn(__fadd2_rn(v[i], kb[i]), ka[i], be[i]), v[i], d);
+              v[i] = __ffma2_rn(v[i], fs[i], fb[i]);
+            }
+            store_pairs<T, V>(y + (l + j * g.lanes) * g.y.sl + c, v);
           }
         }
       });
@@ -298,19 +301,19 @@ group_norm_kernel(NormArgs g) {
 }
 
 // ------------------------------------------------------------------------------------------------------------------ backward
-template <int V> struct NormVectors { float ga[V], be[V], mu[V], rs[V], fs[V]; };
+// Of a thread's channels: gamma, beta, -mean, rstd, FiLM scale.
+template <int V> struct NormVectors { float2 ga[pairs_of(V)], be[pairs_of(V)], mu[pairs_of(V)], rs[pairs_of(V)], fs[pairs_of(V)]; };
 template <int V>
-__device__ __forceinline__ void norm_vectors(const NormArgs& g, int n, int c, bool in, NormVectors<V>& p) {
+__device__ __forceinline__ void norm_vectors(const NormArgs& g, int n, int c, NormVectors<V>& p) {
   const int cg = g.C / g.groups;
 #pragma unroll
+  for (int i = 0; i < pairs_of(V); ++i) { p.ga[i] = p.be[i] = p.mu[i] = p.rs[i] = two(0.f); p.fs[i] = two(1.f); }
+#pragma unroll
   for (int i = 0; i < V; ++i) {
-    p.ga[i] = p.be[i] = p.mu[i] = p.rs[i] = 0.f; p.fs[i] = 1.f;
-    if (in) {
-      const int gr = (c + i) / cg;
-      p.ga[i] = g.gamma[c + i]; p.be[i] = g.beta[c + i];
-      p.mu[i] = g.mean[(long long)n * g.groups + gr]; p.rs[i] = g.rstd[(long long)n * g.groups + gr];
-      if (g.film) p.fs[i] = g.film[(long long)n * 2 * g.C + c + i];
-    }
+    const long long gr = (long long)n * g.groups + (c + i) / cg;
+    auto set = [&](float2* a, float v) { if (i & 1) a[i / 2].y = v; else a[i / 2].x = v; };
+    set(p.ga, g.gamma[c + i]); set(p.be, g.beta[c + i]); set(p.mu, -g.mean[gr]); set(p.rs, g.rstd[gr]);
+    if (g.film) set(p.fs, g.film[(long long)n * 2 * g.C + c + i]);
   }
 }
 
@@ -319,6 +322,7 @@ constexpr int GN_WALK = 2;
 template <typename T, int V, bool COPY, typename F>
 __device__ __forceinline__ void norm_walk(const NormArgs& g, int n, int l0, int hi, int c, const NormVectors<V>& p, F&& f) {
   using X = std::conditional_t<COPY, signed char, T>;
+  constexpr int P = pairs_of(V);
   const X* x0 = COPY ? reinterpret_cast<const X*>(g.cx.q) + (long long)n * g.L * g.C + c : reinterpret_cast<const X*>(g.x.p) + n * g.x.sn + c;
   const T* dy0 = reinterpret_cast<const T*>(g.dy.p) + n * g.dy.sn + c;
   const long long xl = COPY ? g.C : g.x.sl, nb = copy_blocks(g.C);
@@ -342,34 +346,29 @@ __device__ __forceinline__ void norm_walk(const NormArgs& g, int n, int l0, int 
       }
 #pragma unroll
       for (int j = 0; j < GN_WALK; ++j) {
-        float h[V], z[V], a[V], d[V], dz[V], dya[V], dyf[V];
-        piece_floats<X, V>(x[j], h);
-        piece_floats<T, V>(dy[j], dyf);
+        float2 h[P], dz[P], dya[P], dyf[P];
+        piece_pairs<X, V>(x[j], h);
+        piece_pairs<T, V>(dy[j], dyf);
         const float step = COPY ? copy_step(b[j]) : 1.f;
 #pragma unroll
-        for (int i = 0; i < V; ++i) {
-          h[i] = ((COPY ? h[i] * step : h[i]) - p.mu[i]) * p.rs[i];
-          z[i] = fmaf(h[i], p.ga[i], p.be[i]);
+        for (int i = 0; i < P; ++i) {
+          h[i] = __fmul2_rn(COPY ? __ffma2_rn(h[i], two(step), p.mu[i]) : __fadd2_rn(h[i], p.mu[i]), p.rs[i]);
+          float2 a, d;
+          act_pair<true>(decltype(act)::value, __ffma2_rn(h[i], p.ga[i], p.be[i]), a, d);
+          dz[i] = __fmul2_rn(__fmul2_rn(dyf[i], p.fs[i]), d);
+          dya[i] = __fmul2_rn(dyf[i], a);
         }
-        act_values<true, V>(decltype(act)::value, z, a, d);
-#pragma unroll
-        for (int i = 0; i < V; ++i) { dz[i] = dyf[i] * p.fs[i] * d[i]; dya[i] = dyf[i] * a[i]; }
         f(l + j * g.lanes, dz, h, dyf, dya);
       }
     }
   });
 }
 
-// V values in 4, 8 or 16 bytes.
-template <typename T, int V> __device__ __forceinline__ void store_few(T* p, const float* v) {
-  if constexpr (V == 4 && sizeof(T) == 2) *reinterpret_cast<uint2*>(p) = make_uint2(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]));
-  else store_values<T, V>(p, v);
-}
-
 // A cluster walks the sequences split, split + splits, ... and keeps its channels' share of dgamma and dbeta in shared memory.
 template <typename T, int V, bool COPY>
 __global__ void __launch_bounds__(GN_STREAM_THREADS, 1)
 group_norm_grad_kernel(NormArgs g) {
+  constexpr int P = pairs_of(V);
   extern __shared__ __align__(16) float gn_smem[];
   pdl_wait();
   const int cg = g.C / g.groups, threads = blockDim.x;
@@ -393,20 +392,24 @@ group_norm_grad_kernel(NormArgs g) {
       const bool in = lane < g.lanes && c < width;
       if (in) {
         NormVectors<V> p;
-        norm_vectors<V>(g, n, c_set + c, true, p);
-        float s0[V], s1[V], s2[V], s3[V];
+        norm_vectors<V>(g, n, c_set + c, p);
+        float2 sum[4][P];
 #pragma unroll
-        for (int i = 0; i < V; ++i) s0[i] = s1[i] = s2[i] = s3[i] = 0.f;
-        norm_walk<T, V, COPY>(g, n, lo + lane, hi, c_set + c, p, [&](int, const float* dz, const float* h, const float* dy, const float* dya) {
+        for (int k = 0; k < 4; ++k)
 #pragma unroll
-          for (int i = 0; i < V; ++i) { s0[i] += dz[i]; s1[i] = fmaf(dz[i], h[i], s1[i]); s2[i] += dya[i]; s3[i] += dy[i]; }
+          for (int i = 0; i < P; ++i) sum[k][i] = two(0.f);
+        norm_walk<T, V, COPY>(g, n, lo + lane, hi, c_set + c, p, [&](int, const float2* dz, const float2* h, const float2* dy, const float2* dya) {
+#pragma unroll
+          for (int i = 0; i < P; ++i) {
+            sum[0][i] = __fadd2_rn(sum[0][i], dz[i]); sum[1][i] = __ffma2_rn(dz[i], h[i], sum[1][i]);
+            sum[2][i] = __fadd2_rn(sum[2][i], dya[i]); sum[3][i] = __fadd2_rn(sum[3][i], dy[i]);
+          }
         });
 #pragma unroll
-        for (int i = 0; i < V; ++i) {
-          float* o = s_lane + lane * tile + col * V + i;
-          o[0] = s0[i]; o[threads * V] = s1[i];
-          if (film) { o[2 * threads * V] = s2[i]; o[3 * threads * V] = s3[i]; }
-        }
+        for (int k = 0; k < 4; ++k)
+          if (k < sums)
+#pragma unroll
+            for (int i = 0; i < V; ++i) s_lane[k * threads * V + lane * tile + col * V + i] = i & 1 ? sum[k][i / 2].y : sum[k][i / 2].x;
       }
       __syncthreads();
       const int w = min(width - t0, tile);
@@ -423,8 +426,12 @@ group_norm_grad_kernel(NormArgs g) {
       const int k = i / width, c = i - k * width;
       float s = s_sum[k * g.width + c];
       if (g.ranks > 1) {
+        float sr[GN_MAX_RANKS];
+#pragma unroll
+        for (int r = 0; r < GN_MAX_RANKS; ++r) sr[r] = r < g.ranks ? ld_rank_f32(s_sum + k * g.width + c, r) : 0.f;
         s = 0.f;
-        for (int r = 0; r < g.ranks; ++r) s += ld_rank_f32(s_sum + k * g.width + c, r);
+#pragma unroll
+        for (int r = 0; r < GN_MAX_RANKS; ++r) s += sr[r];
       }
       if (k < 2) { s_tot[k * g.width + c] = s; s_acc[k * g.width + c] += s; }
       else if (rank == 0) g.dfilm[((long long)n * 2 + k - 2) * g.C + c_set + c] = s;
@@ -446,14 +453,21 @@ group_norm_grad_kernel(NormArgs g) {
       const int c = t0 + col * V;
       if (!(lane < g.lanes && c < width)) continue;
       NormVectors<V> p;
-      norm_vectors<V>(g, n, c_set + c, true, p);
-      float m1[V], m2[V];
+      norm_vectors<V>(g, n, c_set + c, p);
+      float2 m1[P], m2[P];                                     // -m1, -m2
 #pragma unroll
-      for (int i = 0; i < V; ++i) { m1[i] = s_grp[(c + i) / cg]; m2[i] = s_grp[g.per_set + (c + i) / cg]; }
-      norm_walk<T, V, COPY>(g, n, lo + lane, hi, c_set + c, p, [&](int l, float* dz, const float* h, const float*, const float*) {
+      for (int i = 0; i < P; ++i) m1[i] = m2[i] = two(0.f);
 #pragma unroll
-        for (int i = 0; i < V; ++i) dz[i] = p.rs[i] * fmaf(-h[i], m2[i], __fadd_rn(__fmul_rn(dz[i], p.ga[i]), -m1[i]));
-        if (l < hi) store_few<T, V>(dx + l * g.dx.sl + c, dz);
+      for (int i = 0; i < V; ++i) {
+        const int gr = (c + i) / cg;
+        if (i & 1) { m1[i / 2].y = -s_grp[gr]; m2[i / 2].y = -s_grp[g.per_set + gr]; }
+        else { m1[i / 2].x = -s_grp[gr]; m2[i / 2].x = -s_grp[g.per_set + gr]; }
+      }
+      norm_walk<T, V, COPY>(g, n, lo + lane, hi, c_set + c, p, [&](int l, float2* dz, const float2* h, const float2*, const float2*) {
+        // (the product rounded before m1 is taken off: where a group is one value, the two are the same number)
+#pragma unroll
+        for (int i = 0; i < P; ++i) dz[i] = __fmul2_rn(p.rs[i], __ffma2_rn(h[i], m2[i], __fadd2_rn(__fmul2_rn(dz[i], p.ga[i]), m1[i])));
+        if (l < hi) store_pairs<T, V>(dx + l * g.dx.sl + c, dz);
       });
     }
     if (g.ranks > 1) ptx::cluster_sync_all();

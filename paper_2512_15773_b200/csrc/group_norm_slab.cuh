@@ -210,7 +210,7 @@ group_norm_slab_kernel(NormArgs g) {
 template <typename T, int ITEMS, bool COPY>
 __global__ void __launch_bounds__(GN_THREADS, GN_SLAB_CTAS)
 group_norm_slab_grad_kernel(NormArgs g) {
-  constexpr int V = GN_GRAD_V, P = V / 2;
+  constexpr int V = GN_STREAM_V, P = V / 2;
   using X = std::conditional_t<COPY, signed char, T>;
   extern __shared__ __align__(16) uint8_t gs_raw[];
   __shared__ float s_red[2][2 * GN_THREADS];

@@ -154,13 +154,13 @@ group_norm_warp_kernel(NormArgs g) {
 // sequence ahead, and are read from there as often as they are needed: with them in registers too the kernel spills.  The steps of an
 // 8-bit copy (L cg / 32 bytes) come one to a lane.
 template <typename T, bool COPY> __host__ __device__ constexpr int gn_warp_grad_smem(int items) {
-  return GN_WARP_THREADS * GN_GRAD_V * items * (int)(sizeof(T) + (COPY ? 1 : sizeof(T))) * GN_WARP_STAGES;
+  return GN_WARP_THREADS * GN_STREAM_V * items * (int)(sizeof(T) + (COPY ? 1 : sizeof(T))) * GN_WARP_STAGES;
 }
 
 template <typename T, int ITEMS, bool COPY, bool TEAM>
 __global__ void __launch_bounds__(GN_WARP_THREADS, 2)
 group_norm_warp_grad_kernel(NormArgs g) {
-  constexpr int V = GN_GRAD_V, P = V / 2;
+  constexpr int V = GN_STREAM_V, P = V / 2;
   using X = std::conditional_t<COPY, signed char, T>;
   constexpr int DY_BYTES = 32 * V * ITEMS * sizeof(T), STAGE = DY_BYTES + 32 * V * ITEMS * sizeof(X);
   extern __shared__ __align__(16) uint8_t gw_raw[];

@@ -152,7 +152,7 @@ void norm_plan(NormArgs& g, int V, int elem, int sms, bool grad) {
   g.threads = (int)min((long long)most, max(wanted, max(64ll, (g.cols + 31ll) / 32 * 32)));
   g.lanes = g.threads / g.cols;
   g.ranks = 1;
-  while (g.ranks < 8 && (long long)g.N * g.sets * g.ranks < 2 * sms && g.L >= 8ll * g.lanes * g.ranks) g.ranks *= 2;
+  while (g.ranks < GN_MAX_RANKS && (long long)g.N * g.sets * g.ranks < 2 * sms && g.L >= 8ll * g.lanes * g.ranks) g.ranks *= 2;
   const long long fill = (long long)sms * (GN_STREAM_THREADS / g.threads) * 2 / ((long long)g.sets * g.ranks);
   g.splits = (int)min((long long)g.N, max(1ll, grad ? fill : (1ll << 24) / ((long long)g.sets * g.ranks)));
 }
@@ -270,17 +270,19 @@ bool vectors_wide(const NormArgs& g) { return ((uintptr_t)g.gamma & 7) == 0 && (
 // The three forms of the forward pass; the first two write the copies on their way.
 enum { NORM_STREAM = 0, NORM_WARPS = 1, NORM_SLABS = 2 };
 template <typename T, int V>
-cudaError_t norm_forward(NormArgs& g, int form, int items, int bytes, int sms, int device, cudaStream_t s) {
-  if constexpr (V > 1) {
-    if (form == NORM_WARPS) return norm_warp<T>(g, items, device, s);
-    if (form == NORM_SLABS)
-      return items <= 1 ? norm_slab<T, 1>(g, bytes, device, s) : (items <= 2 ? norm_slab<T, 2>(g, bytes, device, s) : norm_slab<T, 4>(g, bytes, device, s));
-  }
+cudaError_t norm_stream(NormArgs& g, int sms, int device, cudaStream_t s) {
   norm_plan(g, V, sizeof(T), sms, false);
   static std::atomic<unsigned long long> done{0};
   const int smem = (2 * g.threads * V + 4 * g.per_set) * 4;
   const cudaError_t e = allow_smem(group_norm_kernel<T, V>, (2 * GN_THREADS * V + 4 * GN_MAX_WIDTH) * 4, device, done);
   return e != cudaSuccess ? e : launch(group_norm_kernel<T, V>, (unsigned)((long long)g.splits * g.sets * g.ranks), g.threads, g.ranks, smem, s, g);
+}
+template <typename T>
+cudaError_t norm_forward(NormArgs& g, int form, bool wide, int items, int bytes, int sms, int device, cudaStream_t s) {
+  if (form == NORM_WARPS) return norm_warp<T>(g, items, device, s);
+  if (form == NORM_SLABS)
+    return items <= 1 ? norm_slab<T, 1>(g, bytes, device, s) : (items <= 2 ? norm_slab<T, 2>(g, bytes, device, s) : norm_slab<T, 4>(g, bytes, device, s));
+  return wide ? norm_stream<T, GN_STREAM_V>(g, sms, device, s) : norm_stream<T, 1>(g, sms, device, s);
 }
 
 enum { GRAD_STREAM = 0, GRAD_WARPS = 1, GRAD_SLABS = 2 };
@@ -411,8 +413,7 @@ int tsdp_group_norm(int device, const tsdp_norm_t* shape, const void* d_x, int64
   if (form != NORM_STREAM) { g.cx = cx; g.cy = cy; }
   else if (cx.q) e = dtype == TSDP_TYPE_BF16 ? pack<__nv_bfloat16>(g.x, cx, N, L, C, sms, s) : pack<float>(g.x, cx, N, L, C, sms, s);
   if (e == cudaSuccess) {
-    if (dtype == TSDP_TYPE_BF16) e = wide ? norm_forward<__nv_bfloat16, 8>(g, form, items, bytes, sms, device, s) : norm_forward<__nv_bfloat16, 1>(g, form, items, bytes, sms, device, s);
-    else e = wide ? norm_forward<float, 4>(g, form, items, bytes, sms, device, s) : norm_forward<float, 1>(g, form, items, bytes, sms, device, s);
+    e = dtype == TSDP_TYPE_BF16 ? norm_forward<__nv_bfloat16>(g, form, wide, items, bytes, sms, device, s) : norm_forward<float>(g, form, wide, items, bytes, sms, device, s);
   }
   if (e == cudaSuccess && form == NORM_STREAM && cy.q)
     e = dtype == TSDP_TYPE_BF16 ? pack<__nv_bfloat16>(g.y, cy, N, L, C, sms, s) : pack<float>(g.y, cy, N, L, C, sms, s);
@@ -432,8 +433,8 @@ size_t tsdp_group_norm_grad_workspace(int device, const tsdp_norm_t* shape) {
     int items, bytes;
     g.N = shape->N < 1 ? 1 : shape->N; g.L = shape->L; g.C = shape->C; g.groups = shape->groups;
     g.dfilm = form & 1 ? &some : nullptr;
-    if (form < 2) norm_plan(g, form == 0 ? 1 : GN_GRAD_V, elem, sms, true);
-    else if (form == 6 ? !warp_plan(g, GN_GRAD_V, elem == 2 ? 8 : 4, 2, sms, items) : !slab_plan(g, GN_GRAD_V, V, elem, sms, true, form >= 4, items, bytes)) continue;
+    if (form < 2) norm_plan(g, form == 0 ? 1 : GN_STREAM_V, elem, sms, true);
+    else if (form == 6 ? !warp_plan(g, GN_STREAM_V, elem == 2 ? 8 : 4, 2, sms, items) : !slab_plan(g, GN_STREAM_V, V, elem, sms, true, form >= 4, items, bytes)) continue;
     if (norm_grad_bytes(g) > most) most = norm_grad_bytes(g);
   }
   return most;
@@ -474,10 +475,10 @@ int tsdp_group_norm_grad(int device, const tsdp_norm_t* shape, const void* d_dy,
   int items = 0, bytes = 0;
   int form = GRAD_STREAM;
   if (wide && vectors_wide(g) && ((uintptr_t)d_dfilm & 7) == 0 && ((uintptr_t)d_workspace & 7) == 0) {
-    if ((!copy || aligned16(g.cx.q)) && warp_plan(g, GN_GRAD_V, dtype == TSDP_TYPE_BF16 ? 8 : 4, 2, sms, items)) form = GRAD_WARPS;
-    else if ((!copy || aligned16(g.cx.q)) && slab_plan(g, GN_GRAD_V, V, (int)esize(dtype), sms, true, copy, items, bytes)) form = GRAD_SLABS;
+    if ((!copy || aligned16(g.cx.q)) && warp_plan(g, GN_STREAM_V, dtype == TSDP_TYPE_BF16 ? 8 : 4, 2, sms, items)) form = GRAD_WARPS;
+    else if ((!copy || aligned16(g.cx.q)) && slab_plan(g, GN_STREAM_V, V, (int)esize(dtype), sms, true, copy, items, bytes)) form = GRAD_SLABS;
   }
-  if (form == GRAD_STREAM) norm_plan(g, wide ? GN_GRAD_V : 1, (int)esize(dtype), sms, true);
+  if (form == GRAD_STREAM) norm_plan(g, wide ? GN_STREAM_V : 1, (int)esize(dtype), sms, true);
   if (workspace_bytes < norm_grad_bytes(g)) return TSDP_ERR_ARG;
   if (dtype == TSDP_TYPE_BF16) {
     if (wide) e = copy ? norm_backward<__nv_bfloat16, 4, true>(g, form, items, bytes, device, s) : norm_backward<__nv_bfloat16, 4, false>(g, form, items, bytes, device, s);

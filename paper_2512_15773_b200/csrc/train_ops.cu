@@ -143,6 +143,10 @@ void norm_plan(NormArgs& g, int V, int elem, int sms, bool grad) {
   const int step = g.per_set;
   // rows of 128 bytes at least, where a row does not outgrow the threads
   while (g.per_set + step <= g.groups && (g.per_set + step) * cg <= most * V && g.per_set * cg * elem < 128) g.per_set += step;
+  // short sequences: more groups a CTA, up to half its threads with four positions each, while every SM has eight of them to do
+  // (3102 sequences of 4 x 288 channels in 32 groups, fp32, backward: 124 us with the smallest sets, 75 with these)
+  while (2 * g.per_set <= g.groups && (long long)(2 * g.per_set * cg / V) * ((g.L + 3) / 4) <= most / 2 && (long long)g.N * ((g.groups + 2 * g.per_set - 1) / (2 * g.per_set)) >= 8ll * sms)
+    g.per_set *= 2;
   g.width = g.per_set * cg;
   g.sets = (g.groups + g.per_set - 1) / g.per_set;
   g.cols = min((g.width + V - 1) / V, most);

@@ -329,6 +329,8 @@ WgradPlan wgrad_plan(WgradArgs& g, bool fp32, bool pair, int sms) {
   p.bn = g.O <= 64 ? 64 : (g.O <= 128 || fp32 ? 128 : 256);
   const int k128 = (g.K + WG_BM - 1) / WG_BM;
   g.stages = (int)((g.M + WG_BK - 1) / WG_BK);
+  // narrower tiles where there are too few steps for the SMs (us, 256 -> 64 wide: 384 x 128 -> 512 10.5 -> 8.7, 16 x 256 -> 1024 18.1 -> 9.5)
+  while (p.bn > 64 && (long long)g.stages * g.taps * k128 * ((g.O + p.bn - 1) / p.bn) < sms) p.bn /= 2;
   g.tiles_o = (g.O + p.bn - 1) / p.bn;
   // pairs where 256-wide tiles leave little of K unused and the line keeps them busy
   p.cg = pair && !fp32 && p.bn == 256 && (k128 % 2 == 0 || k128 >= 7) && (long long)g.stages * g.taps * (k128 / 2) * g.tiles_o >= 16ll * sms ? 2 : 1;
@@ -350,7 +352,13 @@ cudaError_t wgrad_launch(const CUtensorMap& map, const CUtensorMap& qmap, const 
   e = launch(weight_grad_kernel<BN, DYK, CG>, (unsigned)(units * CG), WG_THREADS, CG, smem, s, map, qmap, g);
   if (e != cudaSuccess) return e;
   const int tiles = g.taps * g.tiles_k * g.tiles_o;
-  return launch(weight_grad_join_kernel<BN, CG>, (unsigned)(tiles * (BN / 16 * CG) + (g.db ? g.tiles_o : 0)), 256, 1, 0, s, g, units, tiles);
+  const int db = g.db ? g.tiles_o * (BN / 8) : 0;
+  // owners of a tile that a join's thread reads in turn; with many of them groups of threads read side by side (us, groups of 1 / 4 / 8:
+  // 16384 x 512 -> 512 with 5 taps, 3.7 owners, 57 / 63 / 75; 1024 x 256 -> 256 with 5 taps, 8 owners, 14.8 / 13.3 / 17.5;
+  // 45056 x 512 -> 256, 37 owners, 45 / 28.6 / 31.5; 45056 x 256 -> 256, 74 owners, 54 / 21.9 / 19.3)
+  const int split = units <= 6 * tiles ? 1 : units <= 40 * tiles ? 4 : 8;
+  return launch(split == 1 ? weight_grad_join_kernel<BN, CG, 1> : split == 4 ? weight_grad_join_kernel<BN, CG, 4> : weight_grad_join_kernel<BN, CG, 8>,
+                (unsigned)(tiles * (BN / 16 * CG) * (split == 1 ? 1 : 2 * split) + db), 256, 1, 0, s, g, units, tiles);
 }
 
 bool wgrad_ok(int dtype, long long N, int L, int K, int O, int taps) {

@@ -495,37 +495,32 @@ __device__ __forceinline__ void wg_owners(const WgradArgs& g, int ctas, int t, i
   first = owner(a); last = owner(b);
 }
 
-// Tiles that several CTAs worked on: their shares, in the order of the line; a block has 16 columns of a tile, a warp 8 rows x 16 columns at
-// a time (128 bytes of a share, 64 bytes of a row of dW).  The last tiles_o blocks (with db): the bias gradient of a column of tiles.
-template <int BN, int CG>
+// Tiles that several CTAs worked on: the sum of their shares.  A block has 512 (SPLIT 1) or 256 / SPLIT quads of four columns of a tile, a warp
+// 8 rows x 16 columns at a time (128 bytes of a share, 64 bytes of a row of dW); with SPLIT > 1 group i of its threads takes every SPLIT-th
+// share from the i-th on, and the groups' sums are added in order.  The last blocks (with db): the bias gradient of eight columns each.
+template <int BN, int CG, int SPLIT>
 __global__ void __launch_bounds__(256)
 weight_grad_join_kernel(WgradArgs g, int units, int tiles) {
-  constexpr int PARTS = BN / 16 * CG, BH = BN / CG;
+  constexpr int SUBS = SPLIT == 1 ? 1 : 2 * SPLIT, SPAN = 256 / SPLIT, PARTS = BN / 16 * CG * SUBS, BH = BN / CG;
+  const int group = threadIdx.x / SPAN, at = threadIdx.x % SPAN;
   pdl_wait();
   int first, last;
-  if ((int)blockIdx.x >= tiles * PARTS) {
-    __shared__ float s_db[CG][WG_BIAS];
-    const int ot = blockIdx.x - tiles * PARTS;
-    float v[CG][4] = {};
+  if ((int)blockIdx.x >= tiles * PARTS) {                                // eight columns of db
+    constexpr int ROWS = WG_BIAS / BH, GROUPS = 256 / (8 * ROWS);
+    __shared__ float s_db[256];
+    const int block = blockIdx.x - tiles * PARTS, ot = block / (BN / 8), col = block % (BN / 8) * 8 + (threadIdx.x & 7);
+    const int row = (threadIdx.x >> 3) % ROWS, db_group = threadIdx.x / (8 * ROWS);
+    float sum = 0.f;
     for (int kt = 0; kt < g.tiles_k; ++kt) {
       const int t = ((g.taps / 2) * g.tiles_k + kt) * g.tiles_o + ot;
       wg_owners(g, units, t, first, last);
-#pragma unroll 4
-      for (int i = first; i <= last; ++i)
-#pragma unroll
-        for (int r = 0; r < CG; ++r)
-#pragma unroll
-          for (int j = 0; j < 4; ++j) v[r][j] += g.bias[((size_t)(i + t) * CG + r) * WG_BIAS + j * 256 + threadIdx.x];
+#pragma unroll 8
+      for (int i = first + db_group; i <= last; i += GROUPS) sum += g.bias[((size_t)(i + t) * CG + col / BH) * WG_BIAS + row * BH + col % BH];
     }
-#pragma unroll
-    for (int r = 0; r < CG; ++r)
-#pragma unroll
-      for (int j = 0; j < 4; ++j) s_db[r][j * 256 + threadIdx.x] = v[r][j];
+    s_db[threadIdx.x] = sum;
     __syncthreads();
-    const int col = threadIdx.x;
-    if (col >= BN || ot * BN + col >= g.O) return;
-    float sum = 0.f;
-    for (int i = 0; i < WG_BIAS / BH; ++i) sum += s_db[col / BH][i * BH + col % BH];
+    if (threadIdx.x >= 8 || ot * BN + col >= g.O) return;
+    for (int i = 1; i < ROWS * GROUPS; ++i) sum += s_db[i * 8 + threadIdx.x];
     g.db[ot * BN + col] = sum;
     return;
   }
@@ -534,16 +529,29 @@ weight_grad_join_kernel(WgradArgs g, int units, int tiles) {
   if (first == last) return;                                             // one CTA (or pair) had all of it
   const int o0 = t % g.tiles_o * BN, tk = t / g.tiles_o, tap = tk / g.tiles_k, k0 = ((tk - tap * g.tiles_k) * CG + rank) * WG_BM;
   const int which0 = wg_begin(g.line, first, units) / g.stages == t ? 0 : 1;         // of the first; the others begin in this tile
+  const int part = blockIdx.x % (PARTS / CG) / SUBS, sub = blockIdx.x % SUBS;
 #pragma unroll
-  for (int j = 0; j < 2; ++j) {
-    const int e = j * 256 + threadIdx.x, row = (e >> 5) * 8 + (e & 7), c = (blockIdx.x % (PARTS / CG)) * 16 + ((e >> 3) & 3) * 4, k = k0 + row;
-    if (k >= g.K || o0 + c >= g.O) continue;
+  for (int j = 0; j < (SPLIT == 1 ? 2 : 1); ++j) {
+    const int e = SPLIT == 1 ? j * 256 + threadIdx.x : sub * SPAN + at, row = (e >> 5) * 8 + (e & 7), c = part * 16 + ((e >> 3) & 3) * 4, k = k0 + row;
+    if (SPLIT == 1 && (k >= g.K || o0 + c >= g.O)) continue;
     const float* sh = g.share + (c >> 2) * (WG_BM * 4) + row * 4;
-    float4 v = *reinterpret_cast<const float4*>(sh + (2ll * (first * CG + rank) + which0) * (WG_BM * BN));
-#pragma unroll 4
-    for (int i = first + 1; i <= last; ++i) {
+    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (group == 0) v = *reinterpret_cast<const float4*>(sh + (2ll * (first * CG + rank) + which0) * (WG_BM * BN));
+#pragma unroll 8
+    for (int i = first + (group ? group : SPLIT); i <= last; i += SPLIT) {
       const float4 u = *reinterpret_cast<const float4*>(sh + 2ll * (i * CG + rank) * (WG_BM * BN));
       v.x += u.x; v.y += u.y; v.z += u.z; v.w += u.w;
+    }
+    if constexpr (SPLIT > 1) {
+      __shared__ float4 s_v[SPLIT][SPAN];
+      s_v[group][at] = v;
+      __syncthreads();
+      if (group || k >= g.K || o0 + c >= g.O) return;
+#pragma unroll
+      for (int i = 1; i < SPLIT; ++i) {
+        const float4 u = s_v[i][at];
+        v.x += u.x; v.y += u.y; v.z += u.z; v.w += u.w;
+      }
     }
     float* out = g.dW + ((long long)tap * g.K + k) * g.O + o0 + c;
     if ((g.O & 3) == 0 && ((uintptr_t)g.dW & 15) == 0) *reinterpret_cast<float4*>(out) = v;

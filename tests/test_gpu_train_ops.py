@@ -475,6 +475,15 @@ def test_weight_gradient_by_pairs(N, L, K, O, taps):
     check_weight(saved, dy, taps, L)
 
 
+# Many rows over few tiles: 8 to 148 CTAs (or pairs) share a tile, whose sums groups of the joining threads take side by side.
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("N,L,K,O,taps", [(400, 16, 200, 130, 1), (1187, 16, 77, 51, 1), (601, 32, 40, 257, 1), (130, 77, 100, 72, 3),
+                                          (64, 16, 256, 256, 5), (40, 512, 256, 256, 1)])
+def test_weight_gradient_of_few_tiles(N, L, K, O, taps, dtype):
+    saved, dy = weight_case(N, L, K, O, taps, dtype, N * L + K)
+    check_weight(saved, dy, taps, L)
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
 @pytest.mark.parametrize("O,ldy", [(128, 136), (128, 131), (100, 104), (256, 1024)])
 def test_weight_gradient_of_strided_rows(O, ldy, dtype):

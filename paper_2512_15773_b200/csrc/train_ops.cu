@@ -201,6 +201,12 @@ bool slab_plan(NormArgs& g, int V, int unit, int elem, int sms, bool grad, bool 
   return true;
 }
 
+// Slabs are taken where a row of a set is a copy worth its name, or all of its rows are one: with copies of 64 to 384 bytes the engine that
+// makes them is what they wait for.  (us, slabs / stream; bf16 unless said: 4096 x 8 x 512 in one group 51 / 107, backward 69 / 139; 4096 x 16 x 256
+// in 32 groups 56 / 95, 96 / 129; 512 bytes: 4096 x 16 x 512 in 32 groups 113 / 157, 182 / 232, fp32 177 / 171, 179 / 237; 384 bytes: 4096 x 16 x 384
+// in 8 groups 130 / 118; 192 bytes: 512 x 16 x 384 in 8 groups 47 / 14, 31 / 27; 128 bytes: 1024 x 64 x 256 in 32 groups 73 / 75, 146 / 96)
+bool slab_rows(const NormArgs& g, const Rows& r, int elem) { return g.width * elem >= 512 || (g.width == g.C && r.sl == g.C); }
+
 // Teams of warps: false where a group's channels are not 32, 64, 128 or 256 or a lane of eight warps would hold more than `most` pieces of V channels.
 bool warp_plan(NormArgs& g, int V, int most, int ctas, int sms, int& items) {
   const int cg = g.C / g.groups;
@@ -418,7 +424,9 @@ int tsdp_group_norm(int device, const tsdp_norm_t* shape, const void* d_x, int64
   if (wide && vectors_wide(g) && ((uintptr_t)cx.q & 7) == 0 && ((uintptr_t)cy.q & 7) == 0) {
     const int V = 16 / (int)esize(dtype), unit = set_fits(C, g.groups, 32) ? 32 : V;      // (with or without copies: the same plan, the same bits)
     if (warp_plan(g, V, 32 / V, 3, sms, items)) form = NORM_WARPS;
-    else if ((unit == 32 || (!cx.q && !cy.q)) && slab_plan(g, V, unit, (int)esize(dtype), sms, false, false, items, bytes)) form = NORM_SLABS;
+    else if ((unit == 32 || (!cx.q && !cy.q)) && slab_plan(g, V, unit, (int)esize(dtype), sms, false, false, items, bytes) &&
+             slab_rows(g, g.x, (int)esize(dtype)))
+      form = NORM_SLABS;
   }
   // copies are written on the way by the forms that hold a group, by a pass of their own otherwise
   cudaError_t e = cudaSuccess;
@@ -488,7 +496,9 @@ int tsdp_group_norm_grad(int device, const tsdp_norm_t* shape, const void* d_dy,
   int form = GRAD_STREAM;
   if (wide && vectors_wide(g) && ((uintptr_t)d_dfilm & 7) == 0 && ((uintptr_t)d_workspace & 7) == 0) {
     if ((!copy || aligned16(g.cx.q)) && warp_plan(g, GN_STREAM_V, dtype == TSDP_TYPE_BF16 ? 8 : 4, 2, sms, items)) form = GRAD_WARPS;
-    else if ((!copy || aligned16(g.cx.q)) && slab_plan(g, GN_STREAM_V, V, (int)esize(dtype), sms, true, copy, items, bytes)) form = GRAD_SLABS;
+    else if ((!copy || aligned16(g.cx.q)) && slab_plan(g, GN_STREAM_V, V, (int)esize(dtype), sms, true, copy, items, bytes) &&
+             slab_rows(g, g.dy, (int)esize(dtype)))
+      form = GRAD_SLABS;
   }
   if (form == GRAD_STREAM) norm_plan(g, wide ? GN_STREAM_V : 1, (int)esize(dtype), sms, true);
   if (workspace_bytes < norm_grad_bytes(g)) return TSDP_ERR_ARG;

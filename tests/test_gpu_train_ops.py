@@ -264,6 +264,41 @@ def test_walks_over_many_sequences(N, L, C, G, dtype):
     check_gradient(dy, None, sx, ga, be, G, mean, rstd, "mish", fi, dtype)
 
 
+# Sets of groups in a CTA: whole dense rows of many short sequences, sets of 512 bytes and more of a row, groups wider than a warp takes.
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("N,L,C,G", [(1901, 2, 128, 16), (1803, 16, 512, 32), (7, 8, 512, 1), (33, 12, 640, 2), (1301, 5, 640, 8), (37, 3, 1024, 1),
+                                     (2003, 1, 96, 6)])
+def test_sets_of_groups(N, L, C, G, dtype):
+    test_walks_over_many_sequences(N, L, C, G, dtype)
+
+
+@pytest.mark.parametrize("saved", [False, True])
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_sets_of_groups_on_strided_rows(saved, dtype):
+    N, L, C, G = 31, 6, 640, 2
+    rng, x, ga, be, fi = norm_inputs(N, L, C, G, dtype, True, 77)
+    dy = rng_tensor(rng, (N, L, C), dtype, 0.1)
+    out = []
+    for pad, shift in ((0, 0), (64, 32)):
+        apart = [torch.full((N, L + 2 * (pad > 0), C + pad), 7.0, dtype=x.dtype, device="cuda") for _ in range(4)]
+        rows = [t[:, :L, shift:shift + C] for t in apart]
+        rows[0].copy_(x)
+        rows[2].copy_(dy)
+        mean, rstd = torch.empty(N, G, device="cuda"), torch.empty(N, G, device="cuda")
+        keep = binding.saved_like(x) if saved else None
+        binding.group_norm(rows[0], ga, be, G, rows[1], film=fi, mean=mean, rstd=rstd, saved_x=keep)
+        dga, dbe, dfi = torch.empty(C, device="cuda"), torch.empty(C, device="cuda"), torch.empty(N, 2 * C, device="cuda")
+        ws = torch.empty(binding.group_norm_grad_workspace(rows[2], G), dtype=torch.uint8, device="cuda")
+        binding.group_norm_grad(rows[2], None if saved else rows[0], ga, be, G, mean, rstd, rows[3], dga, dbe, ws, film=fi, dfilm=dfi, saved_x=keep)
+        out.append([rows[1].clone(), rows[3].clone(), mean, rstd, dga, dbe, dfi])
+        if pad:
+            for t in (apart[1], apart[3]):
+                t[:, :L, shift:shift + C] = 7.0
+                assert (t == 7.0).all()                       # what lies between rows stays
+    for a, b in zip(*out):
+        assert torch.equal(a, b)
+
+
 def test_offsets_past_32_bits():
     """Sequences and rows more than 2^32 bytes apart, in one buffer of 11 GB."""
     far, N, L, C, G = (1 << 31) + 24, 3, 16, 64, 2

@@ -26,6 +26,9 @@
 // Pair form (CG = 2, cta_group::2): a tile of 256 x 256 on two SMs.  Each CTA makes x^ of its own 128 input channels and loads half of the
 // dy columns, so that a stage brings 16 KB less into each SM's shared memory and the tensor core reads 16 KB less of it.  Everything but the
 // MMAs stays within a CTA: the second CTA's idle MMA warp passes on to the first that its stage is complete.
+// What bounds it: the tensor core waits for x^.  45056 rows, 512 -> 2048, bf16, pairs: 102 us and 12 for the join (0.83 PFLOP/s over both; tensor pipe
+// 49 % busy, arithmetic pipe 61 %), 128 us in a long loop at the power limit; of them the conversion of x^ costs 17, draining 6, the bias gradient 3.
+// 16384 rows, 512 -> 512, 5 taps: 58 us (0.74 PFLOP/s).  Operands with the reduction index slowest cost nothing against the other order.
 // Every wait is bounded; a CTA whose wait runs out leaves NaN in what it had to write.
 #pragma once
 #include "checkpoint_kernels.cuh"

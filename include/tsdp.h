@@ -472,6 +472,7 @@ int tsdp_group_norm_grad(int device, const tsdp_norm_t* shape, const void* d_dy,
  * 8-bit copy [N L, K]:
  *     dW[tap][i][o] = sum_{n, l} x[n, l + tap - taps / 2, i] dy[n, l, o],     db[o] = sum_{n, l} dy[n, l, o]
  * dW [taps, K, O] and db [O] (null to skip) fp32, the order of tsdp_load_weights' matrices ([in, out], convolutions [tap, in, out]).
+ * (Padding takes part as zeros: an infinity in dy at the end of a sequence makes NaN of its column in the taps that reach past it.)
  * d_dy [N L, O] of type dtype, rows dy_l elements apart.  Products are exact (an fp32 dy is taken in three bf16 parts), sums fp32.  A wait inside the
  * kernel that expires (each is bounded) leaves NaN in dW.  Workspace: tsdp_weight_grad_workspace bytes, on a 16-byte boundary. */
 size_t tsdp_weight_grad_workspace(int device, int dtype, int N, int L, int K, int O, int taps);

@@ -208,6 +208,9 @@ def _dtype_code(t, name):
     raise ValueError(f"{name}: bfloat16 or float32 expected, got {t.dtype}")
 
 
+_MOST = 2**31 - 1          # what an int of the C side holds; its own limits are below
+
+
 def _rows(t, name, like=None):
     """(address, stride of a sequence, stride of a position, N, L, C) of a tensor [N, L, C] or [rows, C]."""
     if not t.is_cuda:
@@ -223,6 +226,8 @@ def _rows(t, name, like=None):
         raise ValueError(f"{name}: [N, L, C] or [rows, C] expected, got {tuple(shape)}")
     if sc != 1 and ch != 1:
         raise ValueError(f"{name}: channels have to be innermost, without a gap")
+    if max(N, L, ch) > _MOST:
+        raise ValueError(f"{name}: sizes up to {_MOST} expected, got {tuple(shape)}")
     if like is not None and (shape != like.shape or t.dtype is not like.dtype or t.get_device() != like.get_device()):
         raise ValueError(f"{name}: {tuple(like.shape)} of {like.dtype} on {like.device} expected, got {tuple(shape)} of {t.dtype} on {t.device}")
     return t.data_ptr(), sn, sl, N, L, ch

@@ -92,3 +92,53 @@ def test_binding_refuses_what_the_library_cannot_see():
         binding._dense(x.transpose(0, 1), "x", x.numel(), torch.float32, cpu)
     with pytest.raises(ValueError, match="x: 512 values"):
         binding._dense(x, "x", 512, torch.bfloat16, cpu)
+
+
+class Rows:
+    """Stands for a tensor on a GPU: the sizes of one, no memory."""
+    is_cuda, device = True, "cuda:0"
+
+    def __init__(self, *shape):
+        import torch
+        self.shape, self.dtype = shape, torch.bfloat16
+
+    def stride(self):
+        return tuple(0 if i + 1 < len(self.shape) else 1 for i in range(len(self.shape)))
+
+    def dim(self):
+        return len(self.shape)
+
+    def get_device(self):
+        return 0
+
+    def data_ptr(self):
+        return P
+
+    def numel(self):
+        n = 1
+        for v in self.shape:
+            n *= v
+        return n
+
+    def is_contiguous(self):
+        return True
+
+
+@pytest.mark.parametrize("shape", [(2**32 + 5, 1), (2**32 + 1, 4, 64), (2, 2**32 + 4, 64)])
+def test_sizes_past_an_int_are_not_cut(lib, shape):
+    """2^32 + 5 rows are not five."""
+    import torch
+    x, f32 = Rows(*shape), torch.zeros(shape[-1])
+    q, b = Rows(*shape), Rows(*shape[:-1], -(-shape[-1] // 32))
+    q.dtype, b.dtype = torch.int8, torch.uint8
+    with pytest.raises(ValueError):
+        binding.checkpoint_pack(x, (q, b))
+    with pytest.raises(ValueError):
+        binding.checkpoint_unpack((q, b), x)
+    with pytest.raises(ValueError):
+        binding.group_norm(x, f32, f32, 1, x)
+    with pytest.raises(ValueError):
+        binding.group_norm_grad_workspace(x, 1)
+    if len(shape) == 2:
+        with pytest.raises(ValueError):
+            binding.weight_grad_workspace(x, 32, length=5)

@@ -406,8 +406,8 @@ int tsdp_group_norm(int device, const tsdp_norm_t* shape, const void* d_x, int64
                     const float* d_film, void* d_y, int64_t y_n, int64_t y_l, float* d_mean, float* d_rstd, const tsdp_saved_t* saved_x,
                     const tsdp_saved_t* saved_y, void* stream) {
   if (device < 0 || device >= MAX_DEVICES || !norm_ok(shape) || !strides_ok(x_n, x_l) || !strides_ok(y_n, y_l)) return TSDP_ERR_ARG;
+  if (shape->N == 0) return TSDP_OK;                      // (empty copies have no addresses)
   if ((saved_x && !copy_ok(saved_x)) || (saved_y && !copy_ok(saved_y))) return TSDP_ERR_ARG;
-  if (shape->N == 0) return TSDP_OK;
   if (!d_x || !d_gamma || !d_beta || !d_y || !rows_apart(shape->N, shape->L, shape->C, y_n, y_l)) return TSDP_ERR_ARG;
   DeviceScope scope(device);
   if (scope.err != cudaSuccess) return fail_cuda("tsdp_group_norm", scope.err);

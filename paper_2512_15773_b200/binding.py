@@ -259,6 +259,13 @@ def _norm_t(*sizes):
     return NormT(*sizes)
 
 
+def _count(v, name):
+    """A size that is no tensor's: ctypes would cut it to the low 32 bits."""
+    if not -1 <= v <= _MOST:
+        raise ValueError(f"{name}: up to {_MOST} expected, got {v}")
+    return v
+
+
 def _act(act):
     if act not in ACT:
         raise ValueError(f"act: one of {sorted(ACT)} expected, got {act!r}")
@@ -305,7 +312,7 @@ def group_norm(x, gamma, beta, groups, y, act="mish", film=None, eps=1e-5, mean=
     yp, yn, yl = _rows(y, "y", x)[:3]
     dev, f32 = x.get_device(), _torch().float32
     _status(load_library().tsdp_group_norm(
-        dev, _norm_t(_dtype_code(x, "x"), N, L, ch, groups, _act(act), eps), p, sn, sl, _dense(gamma, "gamma", ch, f32, dev),
+        dev, _norm_t(_dtype_code(x, "x"), N, L, ch, _count(groups, "groups"), _act(act), eps), p, sn, sl, _dense(gamma, "gamma", ch, f32, dev),
         _dense(beta, "beta", ch, f32, dev), _dense(film, "film", 2 * N * ch, f32, dev), yp, yn, yl,
         _dense(mean, "mean", N * groups, f32, dev), _dense(rstd, "rstd", N * groups, f32, dev), _saved(saved_x, "saved_x", N * L, ch, dev),
         _saved(saved_y, "saved_y", N * L, ch, dev), stream), "tsdp_group_norm")
@@ -314,7 +321,7 @@ def group_norm(x, gamma, beta, groups, y, act="mish", film=None, eps=1e-5, mean=
 def group_norm_grad_workspace(dy, groups):
     """Bytes of workspace that group_norm_grad takes for gradients like dy."""
     _, _, _, N, L, ch = _rows(dy, "dy")
-    n = load_library().tsdp_group_norm_grad_workspace(dy.get_device(), NormT(_dtype_code(dy, "dy"), N, L, ch, groups, 0, 1e-5))
+    n = load_library().tsdp_group_norm_grad_workspace(dy.get_device(), NormT(_dtype_code(dy, "dy"), N, L, ch, _count(groups, "groups"), 0, 1e-5))
     if n == 0:
         raise TsdpError(1, "tsdp_group_norm_grad_workspace", "sizes")
     return n
@@ -330,7 +337,7 @@ def group_norm_grad(dy, x, gamma, beta, groups, mean, rstd, dx, dgamma, dbeta, w
     dp, dn, dl = _rows(dx, "dx", dy)[:3]
     dev, f32 = dy.get_device(), _torch().float32
     _status(load_library().tsdp_group_norm_grad(
-        dev, _norm_t(_dtype_code(dy, "dy"), N, L, ch, groups, _act(act), 1.0), p, sn, sl, xp, xn, xl, _saved(saved_x, "saved_x", N * L, ch, dev),
+        dev, _norm_t(_dtype_code(dy, "dy"), N, L, ch, _count(groups, "groups"), _act(act), 1.0), p, sn, sl, xp, xn, xl, _saved(saved_x, "saved_x", N * L, ch, dev),
         _dense(gamma, "gamma", ch, f32, dev), _dense(beta, "beta", ch, f32, dev), _dense(film, "film", 2 * N * ch, f32, dev),
         _dense(mean, "mean", N * groups, f32, dev), _dense(rstd, "rstd", N * groups, f32, dev), dp, dn, dl,
         _dense(dgamma, "dgamma", ch, f32, dev), _dense(dbeta, "dbeta", ch, f32, dev), _dense(dfilm, "dfilm", 2 * N * ch, f32, dev),
@@ -341,7 +348,7 @@ def _weight_sizes(dy, length):
     p, _, sl, _, rows, out = _rows(dy, "dy")
     if dy.dim() != 2:
         raise ValueError(f"dy: [rows, out] expected, got {tuple(dy.shape)}")
-    L = max(rows, 1) if length is None else length
+    L = max(rows, 1) if length is None else _count(length, "length")
     if L < 1 or rows % L:
         raise ValueError(f"length: a divisor of the {rows} rows expected, got {L}")
     return p, sl, rows // L, L, out
@@ -350,7 +357,7 @@ def _weight_sizes(dy, length):
 def weight_grad_workspace(dy, channels, taps=1, length=None):
     """Bytes of workspace that weight_grad takes for gradients like dy and `channels` input channels."""
     _, _, N, L, out = _weight_sizes(dy, length)
-    n = load_library().tsdp_weight_grad_workspace(dy.get_device(), _dtype_code(dy, "dy"), N, L, channels, out, taps)
+    n = load_library().tsdp_weight_grad_workspace(dy.get_device(), _dtype_code(dy, "dy"), N, L, _count(channels, "channels"), out, _count(taps, "taps"))
     if n == 0:
         raise TsdpError(1, "tsdp_weight_grad_workspace", "sizes")
     return n
@@ -366,7 +373,7 @@ def weight_grad(saved_x, dy, dW, workspace, db=None, length=None, stream=0):
         raise ValueError(f"dW: [taps, in, {out}] or [in, {out}] expected, got {tuple(shape)}")
     dev, f32 = dy.get_device(), _torch().float32
     _status(load_library().tsdp_weight_grad(
-        dev, _dtype_code(dy, "dy"), _saved(saved_x, "saved_x", N * L, channels, dev), p, sl, N, L, channels, out, taps,
+        dev, _dtype_code(dy, "dy"), _saved(saved_x, "saved_x", N * L, _count(channels, "dW"), dev), p, sl, N, L, channels, out, _count(taps, "dW"),
         _dense(dW, "dW", taps * channels * out, f32, dev), _dense(db, "db", out, f32, dev), *_workspace(workspace, dev), stream), "tsdp_weight_grad")
 
 

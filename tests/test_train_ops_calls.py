@@ -21,3 +21,79 @@ def test_an_empty_batch_with_copies_is_a_call_with_nothing_to_do(lib):
         assert lib.tsdp_group_norm(0, n, None, 0, 64, P, P, None, None, 0, 64, None, None, sx, sy, None) == 0
     one = binding.NormT(1, 1, 16, 64, 8, 1, 1e-5)
     assert lib.tsdp_group_norm(0, one, P, 0, 64, P, P, None, P, 0, 64, None, None, none, None, None) == 1
+
+
+class Rows:
+    """Stands for a dense tensor on a GPU: sizes and an address, no memory."""
+    is_cuda, device = True, "cuda:0"
+
+    def __init__(self, *shape, dtype="bfloat16"):
+        import torch
+        self.shape, self.dtype = shape, getattr(torch, dtype)
+
+    def stride(self):
+        s = [1]
+        for v in self.shape[:0:-1]:
+            s.append(s[-1] * v)
+        return tuple(reversed(s))
+
+    def dim(self):
+        return len(self.shape)
+
+    def get_device(self):
+        return 0
+
+    def data_ptr(self):
+        return P
+
+    def numel(self):
+        n = 1
+        for v in self.shape:
+            n *= v
+        return n
+
+    def element_size(self):
+        return self.dtype.itemsize
+
+    def is_contiguous(self):
+        return True
+
+
+class Taken:
+    """Stands for the library: takes every call, keeps its arguments."""
+
+    def __init__(self):
+        self.calls = []
+
+    def __getattr__(self, name):
+        def call(*a):
+            self.calls.append((name, a))
+            return 16 if name.endswith("_workspace") else 0
+        return call
+
+
+def taken(monkeypatch):
+    t = Taken()
+    monkeypatch.setattr(binding, "load_library", lambda: t)
+    return t
+
+
+FAR = 2**32 + 8
+
+
+@pytest.mark.parametrize("far", [FAR, -FAR, 2**31])
+def test_counts_past_an_int_are_not_cut(monkeypatch, far):
+    """2^32 + 8 groups are not eight; nor are so many input channels or taps."""
+    lib = taken(monkeypatch)
+    x, f32 = Rows(2, 16, 64), Rows(64, dtype="float32")
+    stat, ws, dy = Rows(2 * FAR, dtype="float32"), Rows(1 << 20, dtype="uint8"), Rows(32, 64)
+    stat.numel = lambda: 2 * far
+    for call in (lambda: binding.group_norm(x, f32, f32, far, x, stream=0), lambda: binding.group_norm_grad_workspace(x, far),
+                 lambda: binding.group_norm_grad(x, x, f32, f32, far, stat, stat, x, f32, f32, ws, stream=0),
+                 lambda: binding.weight_grad_workspace(dy, far), lambda: binding.weight_grad_workspace(dy, 64, taps=far),
+                 lambda: binding.weight_grad_workspace(dy, 64, length=far)):
+        with pytest.raises(ValueError):
+            call()
+    assert not lib.calls
+    binding.group_norm(x, f32, f32, 8, x, stream=0)
+    assert lib.calls[0][0] == "tsdp_group_norm"

@@ -261,8 +261,8 @@ def _norm_t(*sizes):
 
 def _count(v, name):
     """A size that is no tensor's: ctypes would cut it to the low 32 bits."""
-    if not -1 <= v <= _MOST:
-        raise ValueError(f"{name}: up to {_MOST} expected, got {v}")
+    if not -_MOST <= v <= _MOST:
+        raise ValueError(f"{name}: sizes up to {_MOST} expected, got {v}")
     return v
 
 

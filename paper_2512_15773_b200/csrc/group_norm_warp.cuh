@@ -124,9 +124,9 @@ group_norm_warp_kernel(NormArgs g) {
     T* y = reinterpret_cast<T*>(g.y.p) + n * g.y.sn + (l_first + lr) * g.y.sl + c;
     const long long r0 = (long long)n * g.L + l_first + lr;
     long long qo = r0 * g.C + c, bo = r0 * copy_blocks(g.C) + (c >> 5);
-    float2 ka[P], kb[P];                       // z = x ka + kb
+    float2 ka[P];                              // z = (x - mean) ka + beta
 #pragma unroll
-    for (int i = 0; i < P; ++i) { ka[i] = __fmul2_rn(ga[i], two(rstd)); kb[i] = __ffma2_rn(ka[i], two(-mean), be[i]); }
+    for (int i = 0; i < P; ++i) ka[i] = __fmul2_rn(ga[i], two(rstd));
     with_act(g.act, [&](auto act) {
 #pragma unroll 1                               // (one piece at a time: several do not fit the registers of three CTAs)
       for (int j = 0; j < ITEMS; ++j) {
@@ -137,7 +137,7 @@ group_norm_warp_kernel(NormArgs g) {
 #pragma unroll
         for (int i = 0; i < P; ++i) {
           float2 d;
-          act_pair<false>(decltype(act)::value, __ffma2_rn(v[i], ka[i], kb[i]), v[i], d);
+          act_pair<false>(decltype(act)::value, __ffma2_rn(__fadd2_rn(v[i], two(-mean)), ka[i], be[i]), v[i], d);
         }
         if (g.film)
 #pragma unroll
@@ -229,17 +229,16 @@ group_norm_warp_grad_kernel(NormArgs g) {
     float2 dz[ITEMS][P], s_z[P], s_h[P], s_a[P], s_y[P];
 #pragma unroll
     for (int i = 0; i < P; ++i) s_z[i] = s_h[i] = s_a[i] = s_y[i] = two(0.f);
-    // h = x rstd - mean rstd (an 8-bit copy's steps times rstd)
-    const float shift = -mean * rstd;
+    // h = (x - mean) rstd, the difference first: x rstd - mean rstd rounds at the size of mean rstd, which has no limit but |mean| / sqrt(eps)
+    // (a group of values of 1000: h = 0.002 instead of 0)
     float scale[COPY ? ITEMS : 1];
-    scale[0] = rstd;
     if constexpr (COPY)
 #pragma unroll
-      for (int j = 0; j < ITEMS; ++j) scale[j] = __shfl_sync(0xffffffffu, steps, min((lr + j * R) * gb + (cc >> 5), 31)) * rstd;
+      for (int j = 0; j < ITEMS; ++j) scale[j] = __shfl_sync(0xffffffffu, steps, min((lr + j * R) * gb + (cc >> 5), 31));
     auto h_values = [&](int j, float2* h) {
       piece_values<X, V>(load_piece<X, V>(xs + j * R * cg * sizeof(X)), h);
 #pragma unroll
-      for (int i = 0; i < P; ++i) h[i] = __ffma2_rn(h[i], two(scale[COPY ? j : 0]), two(shift));
+      for (int i = 0; i < P; ++i) h[i] = __fmul2_rn(COPY ? __ffma2_rn(h[i], two(scale[COPY ? j : 0]), two(-mean)) : __fadd2_rn(h[i], two(-mean)), two(rstd));
     };
     with_act(g.act, [&](auto act) {
 #pragma unroll

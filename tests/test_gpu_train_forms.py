@@ -1,0 +1,98 @@
+"""GroupNorm and its gradients in each of their forms, where a form can go wrong alone: values far from zero, groups of one value, strided rows,
+values that are not finite.
+
+The forms (paper_2512_15773_b200/csrc/train_ops.cu): one warp a group, a team of warps, slabs, the stream form.  u = 2^-24."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import train
+from paper_2512_15773_b200 import binding
+from tests.test_gpu_train_ops import DEPTH, TYPES, U, half, host, rng_tensor
+
+pytestmark = pytest.mark.gpu
+
+# (N, L, C, groups) of dense rows
+FORMS = {"warp": (3, 16, 128, 2), "warps of 32": (3, 16, 256, 8), "team": (3, 64, 256, 2), "slab": (3, 8, 512, 1), "slab of 320": (3, 16, 640, 2),
+         "stream": (2, 256, 64, 8), "cluster": (1, 2048, 64, 4)}
+
+
+def empty(*shape):
+    return torch.full(shape, float("nan"), device="cuda")
+
+
+def forward(x, ga, be, G, act="none", film=None, **kw):
+    y, mean, rstd = torch.full_like(x, float("nan")), empty(x.shape[0], G), empty(x.shape[0], G)
+    binding.group_norm(x, ga, be, G, y, act=act, film=film, mean=mean, rstd=rstd, **kw)
+    return y, mean, rstd
+
+
+def backward(dy, x, saved, ga, be, G, mean, rstd, act="none", film=None, dx=None):
+    N, _, C = dy.shape
+    dx, dga, dbe = torch.full_like(dy, float("nan")) if dx is None else dx, empty(C), empty(C)
+    dfi = None if film is None else empty(N, 2 * C)
+    ws = torch.empty(binding.group_norm_grad_workspace(dy, G), dtype=torch.uint8, device="cuda")
+    binding.group_norm_grad(dy, x, ga, be, G, mean, rstd, dx, dga, dbe, ws, act=act, film=film, dfilm=dfi, saved_x=saved)
+    return dx, dga, dbe, dfi
+
+
+def packed(x):
+    saved = binding.saved_like(x)
+    binding.checkpoint_pack(x, saved)
+    return saved
+
+
+def affine(rng, C):
+    return rng_tensor(rng, (C,), "fp32", 1, 0.2), rng_tensor(rng, (C,), "fp32", 0, 0.2)
+
+
+# ------------------------------------------------------------------------------------------------ far from zero
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("form", FORMS)
+def test_groups_of_one_value_are_normalised_to_nothing(form, dtype):
+    """A group that is 1000 everywhere (its sums are exact: 1000 2^k): y is beta, but for one rounding, and h is zero."""
+    N, L, C, G = FORMS[form]
+    if (L * C // G) & (L * C // G - 1):
+        pytest.skip("the mean of that many values is not exact")
+    rng = np.random.default_rng(1)
+    ga, be = affine(rng, C)
+    x = torch.full((N, L, C), 1000.0, dtype=TYPES[dtype], device="cuda")
+    y, mean, rstd = forward(x, ga, be, G)
+    assert (mean == 1000).all() and (host(y) == be.to(TYPES[dtype]).double().cpu().numpy()).all()
+    dy = rng_tensor(rng, (N, L, C), dtype, 0.1)
+    for s in (None, packed(x)):
+        _, dga, _, _ = backward(dy, None if s else x, s, ga, be, G, mean, rstd)
+        assert (dga == 0).all()
+
+
+def check_far(dy, x, saved, ga, be, G, mean, rstd, dtype):
+    """dx and dgamma of the identity.  x - mean is one rounding, its product with rstd another: h is off by 2 u |h| (and a second order), whatever the size
+    of x.  Sums have a depth of DEPTH at most."""
+    N, L, C = dy.shape
+    dx, dga, dbe, _ = backward(dy, x, saved, ga, be, G, mean, rstd)
+    xs = host(x) if x is not None else train.unpack(saved[0].cpu().numpy().reshape(N * L, C), saved[1].cpu().numpy().reshape(N * L, -1)).reshape(N, L, C)
+    wide = lambda t: np.repeat(t, C // G, axis=1)[:, None, :]  # noqa: E731
+    m, r, d, gam = wide(host(mean)), wide(host(rstd)), np.abs(host(dy)), np.abs(host(ga))
+    h = np.abs((xs - m) * r)
+    rdx, rga, rbe, _ = train.group_norm_grad(host(dy), xs, host(ga), host(be), G, host(mean), host(rstd), "none")
+    depth = (DEPTH + 16) * U
+    assert (np.abs(host(dbe) - rbe) <= depth * d.sum((0, 1))).all()
+    assert (np.abs(host(dga) - rga) <= (depth + 3 * U) * (d * h).sum((0, 1))).all()
+    of_group = lambda t: wide(t.reshape(N, L, G, C // G).mean(axis=(1, 3)))  # noqa: E731
+    m1, m2 = of_group(d * gam), of_group(d * gam * h)
+    e = r * ((depth + 3 * U) * (m1 + h * m2) + 3 * U * h * m2 + 6 * U * (d * gam + m1 + h * m2))
+    assert (np.abs(host(dx) - rdx) <= e + (half(dtype) * np.abs(rdx) * 1.01 if dtype != "fp32" else 0) + 1e-30).all()
+
+
+@pytest.mark.parametrize("offset", [0.0, 100.0, 4000.0])
+@pytest.mark.parametrize("form", FORMS)
+def test_gradients_far_from_zero_keep_their_digits(form, offset):
+    N, L, C, G = FORMS[form]
+    rng = np.random.default_rng(int(offset) + L)
+    ga, be = affine(rng, C)
+    x, dy = rng_tensor(rng, (N, L, C), "fp32", offset), rng_tensor(rng, (N, L, C), "fp32", 0.1)
+    for s in (None, packed(x)):
+        v = host(x) if s is None else train.unpack(s[0].cpu().numpy().reshape(N * L, C), s[1].cpu().numpy().reshape(N * L, -1)).reshape(N, L, C)
+        _, m, r = train.group_norm(v, host(ga), host(be), G, "none")
+        mean, rstd = (torch.tensor(t, dtype=torch.float32, device="cuda") for t in (m, r))
+        check_far(dy, None if s else x, s, ga, be, G, mean, rstd, "fp32")

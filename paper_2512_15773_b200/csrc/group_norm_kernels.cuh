@@ -133,6 +133,10 @@ __device__ __forceinline__ float ld_rank_f32(const float* p, uint32_t rank) {   
   return v;
 }
 
+// The variance from the mean square and the mean of values about some point near their mean.  (Rounding may leave the difference of two
+// equal numbers below zero; a NaN stays one.)
+__device__ __forceinline__ float variance_about(float square, float off) { const float v = fmaf(-off, off, square); return v < 0.f ? 0.f : v; }
+
 // Positions of lane r of a share that is walked in steps of `lanes`: `all` each, one more in the first `extra`.
 struct LaneRows {
   int all, extra;
@@ -207,13 +211,15 @@ group_norm_kernel(NormArgs g) {
       for (int gr = t0 / cg + warp; gr * cg < t1; gr += threads / 32) {
         const int a = max(gr * cg, t0) - t0, b = min(gr * cg + cg, t1) - t0, w = b - a, items = w * g.lanes;
         const float inv_w = 1.f / w;                         // (i / w of a few thousand by a product: off by less than the half it stands away from a whole number)
+        // (about one of them: the sum of large means would be rounded at their size)
+        const float about = s_mean[a];
         float sum = 0.f;
         for (int i = wl; i < items; i += 32) {
           const int r = (int)((i + 0.5f) * inv_w);
-          sum += lane_rows(r) * s_mean[r * tile + a + i - r * w];
+          sum += lane_rows(r) * (s_mean[r * tile + a + i - r * w] - about);
         }
         const float cnt = (float)(hi - lo) * w;
-        const float m = cnt > 0.f ? warp_sum(sum) / cnt : 0.f;
+        const float m = cnt > 0.f ? about + warp_sum(sum) / cnt : 0.f;
         float m2 = 0.f;
         for (int i = wl; i < items; i += 32) {
           const int r = (int)((i + 0.5f) * inv_w), rows = lane_rows(r);
@@ -244,8 +250,8 @@ group_norm_kernel(NormArgs g) {
         auto rows_of = [&](int r) { return (float)max(0, min(g.L, (r + 1) * share) - min(g.L, r * share)); };
 #pragma unroll
         for (int r = 0; r < GN_MAX_RANKS; ++r)
-          if (r < g.ranks) m += mr[r] * rows_of(r);
-        m /= (float)g.L;
+          if (r < g.ranks) m += (mr[r] - mr[0]) * rows_of(r);
+        m = mr[0] + m / (float)g.L;
 #pragma unroll
         for (int r = 0; r < GN_MAX_RANKS; ++r)
           if (r < g.ranks && rows_of(r) > 0.f) { const float d = mr[r] - m; m2 += qr[r] + d * d * rows_of(r) * cg; }

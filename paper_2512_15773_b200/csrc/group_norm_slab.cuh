@@ -93,7 +93,7 @@ __global__ void __launch_bounds__(GN_THREADS, GN_SLAB_CTAS)
 group_norm_slab_kernel(NormArgs g) {
   constexpr int V = 16 / sizeof(T), P = V / 2;
   extern __shared__ __align__(16) uint8_t gs_raw[];
-  __shared__ float s_red[2][GN_THREADS];
+  __shared__ float s_red[GN_THREADS], s_red2[2 * GN_THREADS];
   __shared__ __align__(8) unsigned long long s_bar[GN_RING];
   const int cg = g.C / g.groups, gcols = cg / V;
   const int set = blockIdx.x % g.sets, split = blockIdx.x / g.sets;
@@ -159,11 +159,12 @@ group_norm_slab_kernel(NormArgs g) {
       for (int i = 0; i < P; ++i) t2 = __fadd2_rn(t2, v[i]);       // (zeros where there is no row)
     }
     float sum[1] = {t2.x + t2.y};
-    group_sum<1>(g, gcols, col, lane, s_red[0], sum);
+    group_sum<1>(g, gcols, col, lane, s_red, sum);
     // every thread has taken its share of the stage
     if (threadIdx.x < 32 && n + GN_RING * g.splits < g.N) issue(n + GN_RING * g.splits, s);
     if (++s == GN_RING) { s = 0; ph ^= 1; }
-    const float mean = sum[0] * inv;
+    const float about = sum[0] * inv;          // the mean, but for the roundings of a sum of values; the sum of what lies about it gives their size
+    float2 t1 = two(0.f);
     t2 = two(0.f);
 #pragma unroll
     for (int j = 0; j < ITEMS; ++j) {
@@ -171,12 +172,13 @@ group_norm_slab_kernel(NormArgs g) {
         float2 v[P];
         unpack16<T, V>(raw[j], v);
 #pragma unroll
-        for (int i = 0; i < P; ++i) { v[i] = __fadd2_rn(v[i], two(-mean)); t2 = __ffma2_rn(v[i], v[i], t2); }
+        for (int i = 0; i < P; ++i) { v[i] = __fadd2_rn(v[i], two(-about)); t1 = __fadd2_rn(t1, v[i]); t2 = __ffma2_rn(v[i], v[i], t2); }
       }
     }
-    float sq[1] = {in ? t2.x + t2.y : 0.f};
-    group_sum<1>(g, gcols, col, lane, s_red[1], sq);
-    const float rstd = rsqrtf(sq[0] * inv + g.eps);
+    float moments[2] = {in ? t1.x + t1.y : 0.f, in ? t2.x + t2.y : 0.f};
+    group_sum<2>(g, gcols, col, lane, s_red2, moments);
+    const float off = moments[0] * inv, mean = about + off;
+    const float rstd = rsqrtf(variance_about(moments[1] * inv, off) + g.eps);
     if (in && lane == 0 && col % gcols == 0) {
       const long long at = (long long)n * g.groups + c / cg;
       if (g.mean) g.mean[at] = mean;

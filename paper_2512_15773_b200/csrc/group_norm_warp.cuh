@@ -47,7 +47,7 @@ __global__ void __launch_bounds__(GN_WARP_THREADS, 3)
 group_norm_warp_kernel(NormArgs g) {
   constexpr int V = 16 / sizeof(T), P = V / 2;
   extern __shared__ __align__(16) uint8_t gw_raw[];
-  __shared__ float s_words[TEAM ? 2 : 1][GN_WARP_THREADS / 32];      // (unused by single warps)
+  __shared__ float s_words[GN_WARP_THREADS / 32], s_words2[2 * GN_WARP_THREADS / 32];      // (of teams)
   const int gw = blockIdx.x * (GN_WARP_THREADS / 32) + (threadIdx.x >> 5), wl = threadIdx.x & 31;
   const int team = TEAM ? g.team : 1, part = TEAM ? gw & (team - 1) : 0, grp = gw / team % g.groups, split = gw / team / g.groups;      // this warp's part of its team's positions
   pdl_wait();
@@ -97,14 +97,15 @@ group_norm_warp_kernel(NormArgs g) {
       for (int i = 0; i < P; ++i) t2 = __fadd2_rn(t2, v[i]);
     }
     float sum[1] = {warp_sum(t2.x + t2.y)};
-    if (TEAM) team_sum(team, s_words[0], sum);
-    const float mean = sum[0] * inv;
+    if (TEAM) team_sum(team, s_words, sum);
+    const float about = sum[0] * inv;          // the mean, but for the roundings of a sum of values; the sum of what lies about it gives their size
+    float2 t1 = two(0.f);
     t2 = two(0.f);
     auto squares = [&](int j) {
       float2 v[P];
       unpack16<T, V>(piece(j), v);
 #pragma unroll
-      for (int i = 0; i < P; ++i) { v[i] = __fadd2_rn(v[i], two(-mean)); t2 = __ffma2_rn(v[i], v[i], t2); }
+      for (int i = 0; i < P; ++i) { v[i] = __fadd2_rn(v[i], two(-about)); t1 = __fadd2_rn(t1, v[i]); t2 = __ffma2_rn(v[i], v[i], t2); }
     };
     if (full) {
 #pragma unroll
@@ -114,9 +115,10 @@ group_norm_warp_kernel(NormArgs g) {
       for (int j = 0; j < ITEMS; ++j)
         if (lr + j * R < rows) squares(j);
     }
-    sum[0] = warp_sum(t2.x + t2.y);
-    if (TEAM) team_sum(team, s_words[1], sum);
-    const float rstd = rsqrtf(sum[0] * inv + g.eps);
+    float moments[2] = {warp_sum(t1.x + t1.y), warp_sum(t2.x + t2.y)};
+    if (TEAM) team_sum(team, s_words2, moments);
+    const float off = moments[0] * inv, mean = about + off;
+    const float rstd = rsqrtf(variance_about(moments[1] * inv, off) + g.eps);
     if (wl == 0 && part == 0) {
       if (g.mean) g.mean[(long long)n * g.groups + grp] = mean;
       if (g.rstd) g.rstd[(long long)n * g.groups + grp] = rstd;

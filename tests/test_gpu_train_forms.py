@@ -48,12 +48,10 @@ def affine(rng, C):
 
 # ------------------------------------------------------------------------------------------------ far from zero
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
-@pytest.mark.parametrize("form", FORMS)
+@pytest.mark.parametrize("form", [f for f, (_, L, C, G) in FORMS.items() if not (L * C // G) & (L * C // G - 1)])      # (other counts' means: below)
 def test_groups_of_one_value_are_normalised_to_nothing(form, dtype):
     """A group that is 1000 everywhere (its sums are exact: 1000 2^k): y is beta, but for one rounding, and h is zero."""
     N, L, C, G = FORMS[form]
-    if (L * C // G) & (L * C // G - 1):
-        pytest.skip("the mean of that many values is not exact")
     rng = np.random.default_rng(1)
     ga, be = affine(rng, C)
     x = torch.full((N, L, C), 1000.0, dtype=TYPES[dtype], device="cuda")
@@ -96,3 +94,39 @@ def test_gradients_far_from_zero_keep_their_digits(form, offset):
         _, m, r = train.group_norm(v, host(ga), host(be), G, "none")
         mean, rstd = (torch.tensor(t, dtype=torch.float32, device="cuda") for t in (m, r))
         check_far(dy, None if s else x, s, ga, be, G, mean, rstd, "fp32")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("value", [0.1, -1000.1, 77777.0])
+@pytest.mark.parametrize("N,L,C,G", [*FORMS.values(), (3, 3, 128, 2), (2, 11, 256, 4), (2, 50, 128, 2), (3, 7, 160, 2), (5, 3, 640, 1), (2, 77, 15, 3),
+                                     (1, 1500, 96, 3), (1, 40, 3000, 2)])
+def test_a_group_of_one_value_has_that_mean(N, L, C, G, value, dtype):
+    """Whatever the number of values and however their sum is rounded: the mean is the value, y beta, rstd that of no variance."""
+    rng = np.random.default_rng(L)
+    ga, be = affine(rng, C)
+    x = torch.full((N, L, C), value, dtype=TYPES[dtype], device="cuda")
+    y, mean, rstd = forward(x, ga, be, G)
+    assert (mean == float(x[0, 0, 0])).all()
+    assert (host(y) == be.to(TYPES[dtype]).double().cpu().numpy()).all()
+    assert (np.abs(host(rstd) * np.float32(1e-5) ** 0.5 - 1) <= 8 * U).all()
+
+
+@pytest.mark.parametrize("offset", [0.0, 100.0, 4000.0])
+@pytest.mark.parametrize("form", FORMS)
+def test_far_from_zero_the_mean_is_off_by_its_own_rounding(form, offset):
+    """fp32: the mean is rounded to u |mean| and off by DEPTH u of the widest deviation; so are x - mean; rstd is off by a relative DEPTH u."""
+    N, L, C, G = FORMS[form]
+    rng = np.random.default_rng(int(offset) + L + 1)
+    ga, be = affine(rng, C)
+    x = rng_tensor(rng, (N, L, C), "fp32", offset)
+    y, mean, rstd = forward(x, ga, be, G)
+    ry, rm, rr = train.group_norm(host(x), host(ga), host(be), G, "none")
+    wide = lambda t: np.repeat(t, C // G, axis=1)[:, None, :]  # noqa: E731
+    d = np.abs(host(x) - wide(rm)).reshape(N, L, G, C // G).max(axis=(1, 3))
+    e_m = 1.01 * U * np.abs(rm) + DEPTH * U * d
+    assert (np.abs(host(mean) - rm) <= e_m).all()
+    # (the variance about a mean that is off by e_m is larger by e_m^2; only its own rounding counts beside DEPTH u)
+    assert (np.abs(host(rstd) / rr - 1) <= (DEPTH + 4) * U + 0.5 * (e_m * rr) ** 2).all()
+    h = np.abs((host(x) - wide(rm)) * wide(rr))
+    e = np.abs(host(ga)) * (wide(rr) * wide(e_m) + h * (DEPTH + 8) * U + h * wide(0.5 * (e_m * rr) ** 2)) + 3 * U * (np.abs(ry) + np.abs(host(be)))
+    assert (np.abs(host(y) - ry) <= e).all()

@@ -145,8 +145,10 @@ struct LaneRows {
 };
 
 // ------------------------------------------------------------------------------------------------------------------ forward
-// First walk: each thread keeps, per channel, the sums about its own first value (so that a large mean costs no digits); mean and centred
-// sum of squares of its share are then merged, thread by thread and CTA by CTA, with their counts: M2 = sum M2_i + n_i (mean_i - mean)^2.
+// First walk: each thread keeps, per channel, the sums S and Q of deviations and their squares about a point p, at first its first value.  After
+// every eight positions p moves to the mean of the n values so far, by d: Q -= d (2 S - n d), S -= n d.  So neither a large mean costs digits nor
+// a first value apart from the rest (about one fixed point, 1000 before 2000 values of 0.1: variance 8 % off).  p and Q, the mean and the centred
+// sum of squares of its share, are then merged, thread by thread and CTA by CTA, with their counts: M2 = sum M2_i + n_i (mean_i - mean)^2.
 template <typename T, int V>
 __global__ void __launch_bounds__(GN_THREADS, 2)
 group_norm_kernel(NormArgs g) {
@@ -172,37 +174,51 @@ group_norm_kernel(NormArgs g) {
       const int c = t0 + col * V;
       const bool in = lane < g.lanes && c < width;
       if (in) {
-        float2 k[P], s[P], q[P];
+        float2 k[P], sum[P], sq[P];               // minus a point at the mean so far, sums about it
 #pragma unroll
-        for (int i = 0; i < P; ++i) k[i] = s[i] = q[i] = two(0.f);
+        for (int i = 0; i < P; ++i) k[i] = sum[i] = sq[i] = two(0.f);
         int l = lo + lane;
-        Piece<T, V> pivot{};
-        if (l < hi) { pivot = load_piece<T, V>(reinterpret_cast<const uint8_t*>(x + l * g.x.sl + c)); piece_pairs<T, V>(pivot, k); }
+        if (l < hi) piece_pairs<T, V>(load_piece<T, V>(reinterpret_cast<const uint8_t*>(x + l * g.x.sl + c)), k);
 #pragma unroll
         for (int i = 0; i < P; ++i) k[i] = __fmul2_rn(k[i], two(-1.f));
         constexpr int U = 8;                      // positions asked for together
-        for (; l < hi; l += U * g.lanes) {
+        const T* at_l = x + l * g.x.sl + c;
+        const long long step = g.lanes * g.x.sl;
+        int seen = 0;
+        for (; l < hi; l += U * g.lanes, at_l += U * step) {
           Piece<T, V> raw[U];
 #pragma unroll
           for (int j = 0; j < U; ++j) {
-            raw[j] = pivot;                                    // (counts nothing)
-            if (l + j * g.lanes < hi) raw[j] = load_piece<T, V>(reinterpret_cast<const uint8_t*>(x + (l + j * g.lanes) * g.x.sl + c));
+            raw[j] = Piece<T, V>{};
+            if (l + j * g.lanes < hi) raw[j] = load_piece<T, V>(reinterpret_cast<const uint8_t*>(at_l + j * step));
           }
 #pragma unroll
           for (int j = 0; j < U; ++j) {
+            const bool there = l + j * g.lanes < hi;
             float2 v[P];
             piece_pairs<T, V>(raw[j], v);
 #pragma unroll
-            for (int i = 0; i < P; ++i) { const float2 d = __fadd2_rn(v[i], k[i]); s[i] = __fadd2_rn(s[i], d); q[i] = __ffma2_rn(d, d, q[i]); }
+            for (int i = 0; i < P; ++i) {
+              float2 d = __fadd2_rn(v[i], k[i]);
+              if (!there) d = two(0.f);
+              sum[i] = __fadd2_rn(sum[i], d); sq[i] = __ffma2_rn(d, d, sq[i]);
+            }
+            seen += there;
+          }
+          const float n = (float)seen, of_seen = -act_rcp(n);
+#pragma unroll
+          for (int i = 0; i < P; ++i) {
+            const float2 at = __ffma2_rn(sum[i], two(of_seen), k[i]), by = __ffma2_rn(at, two(-1.f), k[i]);         // the point moves by `by`
+            const float2 rest = __ffma2_rn(by, two(-n), sum[i]);
+            sq[i] = __ffma2_rn(__fmul2_rn(by, two(-1.f)), __fadd2_rn(sum[i], rest), sq[i]);
+            sum[i] = rest;
+            k[i] = at;
           }
         }
-        const int cnt = lane_rows(lane);
-        const float inv = cnt ? 1.f / cnt : 0.f;
 #pragma unroll
         for (int i = 0; i < V; ++i) {
-          const float si = i & 1 ? s[i / 2].y : s[i / 2].x, qi = i & 1 ? q[i / 2].y : q[i / 2].x, ki = i & 1 ? k[i / 2].y : k[i / 2].x;
-          s_mean[lane * tile + col * V + i] = fmaf(si, inv, -ki);
-          s_m2[lane * tile + col * V + i] = fmaf(-si * inv, si, qi);
+          s_mean[lane * tile + col * V + i] = -(i & 1 ? k[i / 2].y : k[i / 2].x);      // (the sums about it are what its rounding leaves)
+          s_m2[lane * tile + col * V + i] = i & 1 ? sq[i / 2].y : sq[i / 2].x;
         }
       }
       __syncthreads();

@@ -130,3 +130,27 @@ def test_far_from_zero_the_mean_is_off_by_its_own_rounding(form, offset):
     h = np.abs((host(x) - wide(rm)) * wide(rr))
     e = np.abs(host(ga)) * (wide(rr) * wide(e_m) + h * (DEPTH + 8) * U + h * wide(0.5 * (e_m * rr) ** 2)) + 3 * U * (np.abs(ry) + np.abs(host(be)))
     assert (np.abs(host(y) - ry) <= e).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("first,rest,spread", [(1000.0, 0.1, 0.0), (1000.0, 0.0, 1.0), (0.0, 500.0, 1.0), (-3e4, 3e4, 0.25)])
+@pytest.mark.parametrize("L,C,G", [(16384, 1024, 1), (9001, 64, 4), (5003, 30, 3)])
+def test_a_first_position_unlike_the_rest_costs_no_digits(L, C, G, first, rest, spread, dtype):
+    """A thread merges eight positions at a time, L / 64 times at most (8 CTAs share a sequence): the sum of squares, whose terms are all positive, is off by
+    as many u and those of the merging of threads (DEPTH)."""
+    rng = np.random.default_rng(L)
+    ga, be = affine(rng, C)
+    x = rng_tensor(rng, (1, L, C), dtype, rest, spread)
+    x[:, 0] = first
+    y, mean, rstd = forward(x, ga, be, G)
+    ry, rm, rr = train.group_norm(host(x), host(ga), host(be), G, "none")
+    w = C // G
+    wide = lambda t: np.repeat(t, w, axis=1)[:, None, :]  # noqa: E731
+    apart = np.abs(host(x) - wide(rm)).reshape(1, L, G, w).mean(axis=(1, 3))
+    e_m = 1.01 * U * np.abs(rm) + 8 * DEPTH * U * apart              # (sums about a mean that is still on its way: at most 8 times those about the last one)
+    assert (np.abs(host(mean) - rm) <= e_m).all()
+    e_r = (L / 64 + DEPTH) * U + 0.5 * (e_m * rr) ** 2
+    assert (np.abs(host(rstd) / rr - 1) <= e_r).all()
+    h = np.abs((host(x) - wide(rm)) * wide(rr))
+    e = np.abs(host(ga)) * (wide(rr * e_m) + h * (wide(e_r) + 6 * U)) + 3 * U * (np.abs(ry) + np.abs(host(be)))
+    assert (np.abs(host(y) - ry) <= e + (half(dtype) * np.abs(ry) * 1.01 if dtype != "fp32" else 0)).all()

@@ -474,10 +474,16 @@ int tsdp_group_norm_grad(int device, const tsdp_norm_t* shape, const void* d_dy,
  * dW [taps, K, O] and db [O] (null to skip) fp32, the order of tsdp_load_weights' matrices ([in, out], convolutions [tap, in, out]).
  * (Padding takes part as zeros: an infinity in dy at the end of a sequence makes NaN of its column in the taps that reach past it.)
  * d_dy [N L, O] of type dtype, rows dy_l elements apart.  Products are exact (an fp32 dy is taken in three bf16 parts), sums fp32.  A wait inside the
- * kernel that expires (each is bounded) leaves NaN in dW.  Workspace: tsdp_weight_grad_workspace bytes, on a 16-byte boundary. */
+ * kernel that expires (each is bounded, to about a second) leaves NaN in what its CTA had to give to dW and db.  Workspace: tsdp_weight_grad_workspace bytes, on a 16-byte boundary. */
 size_t tsdp_weight_grad_workspace(int device, int dtype, int N, int L, int K, int O, int taps);
 int tsdp_weight_grad(int device, int dtype, const tsdp_saved_t* saved_x, const void* d_dy, int64_t dy_l, int N, int L, int K,
                      int O, int taps, float* d_dW, float* d_db, void* d_workspace, size_t workspace_bytes, void* cuda_stream);
+
+/* Exercise the waits of these operators without hanging anything (test interface), as tsdp_debug_arm_gemm_timeout does for the GEMM: the
+ * NEXT tsdp_weight_grad call of this host thread runs with its waits bounded to `wait_cycles` SM clock cycles (1e3 .. 2e9) and with dy
+ * withheld from CTA 0.  That CTA's waits run out, it leaves NaN in its part of the result and returns; the others finish normally.  One-shot.
+ * Errors: ARG. */
+int tsdp_debug_arm_train_timeout(long long wait_cycles);
 
 #ifdef __cplusplus
 }

@@ -19,7 +19,7 @@ EXPORTS = ["tsdp_init", "tsdp_destroy", "tsdp_strerror", "tsdp_last_error", "tsd
            "tsdp_kernel_launches", "tsdp_profile", "tsdp_profile_read", "tsdp_verify_commit_static", "tsdp_set_scheduler", "tsdp_set_progress",
            "tsdp_sched_eval", "tsdp_serve", "tsdp_request_counts", "tsdp_process_reward", "tsdp_distill_loss", "tsdp_distill_step", "tsdp_debug_arm_gemm_timeout", "tsdp_debug_arm_round_failure", "tsdp_debug_check_guards",
            "tsdp_checkpoint_pack", "tsdp_checkpoint_unpack", "tsdp_group_norm", "tsdp_group_norm_grad_workspace", "tsdp_group_norm_grad",
-           "tsdp_weight_grad_workspace", "tsdp_weight_grad"]
+           "tsdp_weight_grad_workspace", "tsdp_weight_grad", "tsdp_debug_arm_train_timeout"]
 ACT = {"none": 0, "mish": 1, "silu": 2, "gelu": 3}
 PROF_FAMILIES = ["gemm", "layernorm", "attention", "embed_head", "round", "small_net", "gemm_draft", "drafter_cluster", "accept", "verifier_cluster",
                  "layernorm_draft", "attention_draft", "embed_head_draft"]
@@ -118,6 +118,7 @@ def load_library():
     lib.tsdp_group_norm_grad.argtypes = [i, C.POINTER(NormT), vp, i64, i64, vp, i64, i64, saved, vp, vp, vp, vp, vp, vp, i64, i64,
                                          vp, vp, vp, vp, C.c_size_t, vp]
     lib.tsdp_weight_grad_workspace.argtypes = [i, i, i, i, i, i, i]; lib.tsdp_weight_grad_workspace.restype = C.c_size_t
+    lib.tsdp_debug_arm_train_timeout.argtypes = [C.c_longlong]
     lib.tsdp_weight_grad.argtypes = [i, i, saved, vp, i64, i, i, i, i, i, vp, vp, vp, C.c_size_t, vp]
     _lib = lib
     return lib
@@ -375,6 +376,11 @@ def weight_grad(saved_x, dy, dW, workspace, db=None, length=None, stream=0):
     _status(load_library().tsdp_weight_grad(
         dev, _dtype_code(dy, "dy"), _saved(saved_x, "saved_x", N * L, _count(channels, "dW"), dev), p, sl, N, L, channels, out, _count(taps, "dW"),
         _dense(dW, "dW", taps * channels * out, f32, dev), _dense(db, "db", out, f32, dev), *_workspace(workspace, dev), stream), "tsdp_weight_grad")
+
+
+def arm_train_timeout(wait_cycles):
+    """Test interface: the next weight_grad call of this thread has a wait that runs out (see tsdp.h)."""
+    _status(load_library().tsdp_debug_arm_train_timeout(int(wait_cycles)), "tsdp_debug_arm_train_timeout")
 
 
 class Sampler:

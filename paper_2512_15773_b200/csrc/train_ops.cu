@@ -32,6 +32,14 @@ struct DeviceScope {
   ~DeviceScope() { if (before >= 0) cudaSetDevice(before); }
 };
 
+// tsdp_debug_arm_train_timeout: the limit of the next call's waits, 0 where there is none but the usual one.
+thread_local long long armed_wait = 0;
+struct Waits {
+  long long cycles = GEMM_WAIT_CYCLES;
+  int withhold = 0;
+  Waits() { if (armed_wait) { cycles = armed_wait; withhold = 1; armed_wait = 0; } }
+};
+
 int fail_cuda(const char* what, cudaError_t e) {
   fprintf(stderr, "%s: %s\n", what, cudaGetErrorString(e));
   return TSDP_ERR_CUDA;
@@ -376,6 +384,12 @@ bool wgrad_ok(int dtype, long long N, int L, int K, int O, int taps) {
 
 extern "C" {
 
+int tsdp_debug_arm_train_timeout(long long wait_cycles) {
+  if (wait_cycles < 1000 || wait_cycles > GEMM_WAIT_CYCLES) return TSDP_ERR_ARG;
+  armed_wait = wait_cycles;
+  return TSDP_OK;
+}
+
 int tsdp_checkpoint_pack(int device, int dtype, const void* d_x, int64_t x_n, int64_t x_l, int N, int L, int C, const tsdp_saved_t* out, void* stream) {
   if (device < 0 || device >= MAX_DEVICES || !dtype_ok(dtype) || N < 0 || N > MOST_ROWS || L < 0 || L > MOST_ROWS || C < 1 || C > MOST_CHANNELS || !strides_ok(x_n, x_l)) return TSDP_ERR_ARG;
   if (N == 0 || L == 0) return TSDP_OK;
@@ -542,6 +556,8 @@ int tsdp_weight_grad(int device, int dtype, const tsdp_saved_t* saved_x, const v
   }
   if (!copy_ok(saved_x) || !d_dy || !d_workspace || !aligned16(d_workspace)) return TSDP_ERR_ARG;
   WgradArgs g{};
+  const Waits waits;
+  g.wait_cycles = waits.cycles; g.withhold = waits.withhold;
   g.x = copy_of(saved_x);
   g.dy = d_dy; g.ldy = dy_l;
   g.M = (long long)N * L; g.L = L; g.K = K; g.O = O; g.taps = taps;

@@ -29,7 +29,7 @@
 // What bounds it: the tensor core waits for x^.  45056 rows, 512 -> 2048, bf16, pairs: 102 us and 12 for the join (0.83 PFLOP/s over both; tensor pipe
 // 49 % busy, arithmetic pipe 61 %), 128 us in a long loop at the power limit; of them the conversion of x^ costs 17, draining 6, the bias gradient 3.
 // 16384 rows, 512 -> 512, 5 taps: 58 us (0.74 PFLOP/s).  Operands with the reduction index slowest cost nothing against the other order.
-// Every wait is bounded; a CTA whose wait runs out leaves NaN in what it had to write.
+// Every wait is bounded; a CTA whose wait runs out leaves NaN in what it had to write, of dW and of db.
 #pragma once
 #include "checkpoint_kernels.cuh"
 #include "gemm_tcgen05.cuh"
@@ -62,6 +62,8 @@ struct WgradArgs {
   int stages, line;                         // of a tile; of all tiles (line + grid < 2^31)
   float* dW;                                // [taps, K, O]
   float* share;                             // [grid][2][BN / 4][128][4]: what a CTA has of its first / of its last tile
+  long long wait_cycles;                    // limit of every wait
+  int withhold;                             // CTA 0 gets no dy (tsdp_debug_arm_train_timeout)
   float *db, *bias;                         // [O] or null; [units + tiles][CG][WG_BIAS]: shares of it, of unit (CTA or pair) i in tile t at i + t
 };
 // The line's piece of CTA i of n.
@@ -145,11 +147,11 @@ weight_grad_kernel(const __grid_constant__ CUtensorMap tmDy, const __grid_consta
   bool ok = true;
 
   if (warp == 0) {
-    if (DYK == WG_DY_TMA && ptx::elect_one()) {
+    if (DYK == WG_DY_TMA && !(g.withhold && blockIdx.x == 0) && ptx::elect_one()) {
       int t = t_first, st = begin - t * g.stages, s = 0;
       uint32_t ph = 1;
       for (int i = begin; i < end; ++i) {
-        if (!ptx::mbar_wait_thread(empty_b(s), ph)) { ok = false; break; }
+        if (!ptx::mbar_wait_thread(empty_b(s), ph, g.wait_cycles)) { ok = false; break; }
         const int o0 = t % g.tiles_o * BN + rank * BH;
         ptx::mbar_expect_tx(full_b(s), BH * WG_BK * 2);
 #pragma unroll
@@ -163,7 +165,7 @@ weight_grad_kernel(const __grid_constant__ CUtensorMap tmDy, const __grid_consta
       int t = t_first, st = begin - t * g.stages, s = 0;
       uint32_t ph = 1;
       for (int i = begin; i < end; ++i) {
-        if (!ptx::mbar_wait_thread(empty_q(s), ph)) { ok = false; break; }
+        if (!ptx::mbar_wait_thread(empty_q(s), ph, g.wait_cycles)) { ok = false; break; }
         const int tk = t / g.tiles_o, tap = tk / g.tiles_k;
         ptx::mbar_expect_tx(full_q(s), WG_TILE_Q);
         ptx::tma_load_2d(base + OFF_Q + s * WG_TILE_Q, &tmQ, ((tk - tap * g.tiles_k) * CG + rank) * WG_BM, st * WG_BK + tap - g.taps / 2, full_q(s));
@@ -176,7 +178,7 @@ weight_grad_kernel(const __grid_constant__ CUtensorMap tmDy, const __grid_consta
       int sa = 0, sb = 0;
       uint32_t pa = 0, pb = 0;
       for (int i = begin; i < end; ++i) {
-        if (!ptx::mbar_wait_thread(full_b(sb), pb) || !ptx::mbar_wait_thread(full_a(sa), pa)) { ok = false; break; }
+        if (!ptx::mbar_wait_thread(full_b(sb), pb, g.wait_cycles) || !ptx::mbar_wait_thread(full_a(sa), pa, g.wait_cycles)) { ok = false; break; }
         wg_pass_on(ptx::mapa_rank(peer(sa), 0));
         if (++sa == SA) { sa = 0; pa ^= 1; }
         if (++sb == SB) { sb = 0; pb ^= 1; }
@@ -189,8 +191,8 @@ weight_grad_kernel(const __grid_constant__ CUtensorMap tmDy, const __grid_consta
       bool fresh = true;
       auto commit = [&](uint32_t bar) { if (CG == 2) ptx::tc_commit_pair(bar); else ptx::tc_commit(bar); };
       for (int i = begin; i < end; ++i) {
-        if (fresh && !ptx::mbar_wait_thread(tempty(buf), tph)) { ok = false; break; }
-        if (!ptx::mbar_wait_thread(full_b(sb), pb) || !ptx::mbar_wait_thread(full_a(sa), pa) || (CG == 2 && !ptx::mbar_wait_thread(peer(sa), pa))) { ok = false; break; }
+        if (fresh && !ptx::mbar_wait_thread(tempty(buf), tph, g.wait_cycles)) { ok = false; break; }
+        if (!ptx::mbar_wait_thread(full_b(sb), pb, g.wait_cycles) || !ptx::mbar_wait_thread(full_a(sa), pa, g.wait_cycles) || (CG == 2 && !ptx::mbar_wait_thread(peer(sa), pa, g.wait_cycles))) { ok = false; break; }
         ptx::tc_fence_after();
         const uint32_t a0 = base + sa * WG_TILE_A, b0 = base + OFF_B + sb * TILE_B, d = tmem + buf * BN;
 #pragma unroll
@@ -267,7 +269,7 @@ weight_grad_kernel(const __grid_constant__ CUtensorMap tmDy, const __grid_consta
 #pragma unroll
     for (int d = 0; d < WG_AHEAD; ++d)
       if (begin + group + d * WG_GROUPS < end) steps_of(ahead[d]);
-    for (int i0 = begin + group; i0 < end && ok; i0 += WG_AHEAD * WG_GROUPS)
+    for (int i0 = DYK != WG_DY_TMA && g.withhold && blockIdx.x == 0 ? end : begin + group; i0 < end && ok; i0 += WG_AHEAD * WG_GROUPS)
 #pragma unroll
     for (int d = 0; d < WG_AHEAD; ++d) {
       const int i = i0 + d * WG_GROUPS;
@@ -276,7 +278,7 @@ weight_grad_kernel(const __grid_constant__ CUtensorMap tmDy, const __grid_consta
       if (i + WG_AHEAD * WG_GROUPS < end) steps_of(ahead[d]);
       uint4 w[2];
       if (g.q_tma) {
-        ok = ptx::mbar_wait_warp(full_q(sq), pq);
+        ok = ptx::mbar_wait_warp(full_q(sq), pq, g.wait_cycles);
         if (!ok) continue;
         const uint8_t* q = raw + OFF_Q + sq * WG_TILE_Q + r * WG_BM + p * 16;
         w[0] = *reinterpret_cast<const uint4*>(q);
@@ -310,7 +312,7 @@ weight_grad_kernel(const __grid_constant__ CUtensorMap tmDy, const __grid_consta
           w[h] = make_uint4(v[0], v[1], v[2], v[3]);
         }
       }
-      ok = ptx::mbar_wait_warp(empty_a(sa), pa);
+      ok = ptx::mbar_wait_warp(empty_a(sa), pa, g.wait_cycles);
       if (!ok) continue;
       const uint32_t a0 = base + sa * WG_TILE_A + row_off;
 #pragma unroll
@@ -322,7 +324,7 @@ weight_grad_kernel(const __grid_constant__ CUtensorMap tmDy, const __grid_consta
       }
       if constexpr (DYK != WG_DY_TMA) {
         // eight output channels at a time
-        ok = ptx::mbar_wait_warp(empty_b(sb), pb);
+        ok = ptx::mbar_wait_warp(empty_b(sb), pb, g.wait_cycles);
         if (!ok) continue;
         const int rd = tid >> 2, bq = tid & 3;
         const long long m_cur = (long long)st_cur * WG_BK + rd;
@@ -399,7 +401,7 @@ weight_grad_kernel(const __grid_constant__ CUtensorMap tmDy, const __grid_consta
       for (bool first = true; i < t_end; first = false) {
         i = min(i + CHUNK, t_end);
         const bool last = i == t_end;
-        ok = ok && ptx::mbar_wait_warp(tfull(buf), ph);
+        ok = ok && ptx::mbar_wait_warp(tfull(buf), ph, g.wait_cycles);
         ptx::tc_fence_after();
         for (int c0 = 0; c0 < BN; c0 += 16) {
           uint32_t v[16];
@@ -461,7 +463,7 @@ weight_grad_kernel(const __grid_constant__ CUtensorMap tmDy, const __grid_consta
     int tk = t / g.tiles_o, kt = tk % g.tiles_k, turn = st % g.tiles_k;
     bool centre = tk / g.tiles_k == g.taps / 2;
     for (int i = begin; i < end; ++i) {
-      ok = ptx::mbar_wait_warp(full_b(s), ph);
+      ok = ptx::mbar_wait_warp(full_b(s), ph, g.wait_cycles);
       if (!ok) break;
       if (centre && turn == kt) {
         float2 part[4];                                                    // (of a stage apart: fewer additions to the long sum)
@@ -499,6 +501,11 @@ weight_grad_kernel(const __grid_constant__ CUtensorMap tmDy, const __grid_consta
         }
       }
     }
+    if (!ok)                                                               // what this CTA has not written: of this tile and of those after it
+      for (; t <= (end - 1) / g.stages; ++t)
+        if (t / g.tiles_o / g.tiles_k == g.taps / 2)
+#pragma unroll 1
+          for (int j = 0; j < 8; ++j) g.bias[((size_t)(unit + t) * CG + rank) * WG_BIAS + grp * BH + piece * 8 + j] = __uint_as_float(0x7fc00000u);
   }
   if (!ok) {
     const long long t0 = clock64();

@@ -453,7 +453,7 @@ typedef struct {
 /* y = scale act(gamma (x - mean) rstd + beta) + bias, mean and rstd = 1 / sqrt(variance + eps) over the L positions and C / groups channels
  * of each group.  gamma, beta [C] fp32; d_film [N, 2C] fp32 (scale, then bias) or null; x, y of the type in `shape`; d_mean, d_rstd
  * [N, groups] fp32 or null; saved_x, saved_y (null: none) receive the 8-bit copies of x and of y as it was rounded.
- * d_y may be d_x with the same strides. */
+ * d_y may be d_x with the same strides.  A wait inside a kernel that expires leaves NaN, here and in the gradients, in what its CTA had to write. */
 int tsdp_group_norm(int device, const tsdp_norm_t* shape, const void* d_x, int64_t x_n, int64_t x_l, const float* d_gamma,
                     const float* d_beta, const float* d_film, void* d_y, int64_t y_n, int64_t y_l, float* d_mean, float* d_rstd,
                     const tsdp_saved_t* saved_x, const tsdp_saved_t* saved_y, void* cuda_stream);
@@ -480,8 +480,9 @@ int tsdp_weight_grad(int device, int dtype, const tsdp_saved_t* saved_x, const v
                      int O, int taps, float* d_dW, float* d_db, void* d_workspace, size_t workspace_bytes, void* cuda_stream);
 
 /* Exercise the waits of these operators without hanging anything (test interface), as tsdp_debug_arm_gemm_timeout does for the GEMM: the
- * NEXT tsdp_weight_grad call of this host thread runs with its waits bounded to `wait_cycles` SM clock cycles (1e3 .. 2e9) and with dy
- * withheld from CTA 0.  That CTA's waits run out, it leaves NaN in its part of the result and returns; the others finish normally.  One-shot.
+ * NEXT tsdp_weight_grad, tsdp_group_norm or tsdp_group_norm_grad call of this host thread runs with its waits bounded to `wait_cycles` SM clock
+ * cycles (1e3 .. 2e9) and with its rows (of dy, of x) withheld from CTA 0.  That CTA's waits run out, it leaves NaN in its part of the
+ * result and returns; the others finish normally.  (GroupNorm waits only where a CTA holds whole groups of a sequence.)  One-shot.
  * Errors: ARG. */
 int tsdp_debug_arm_train_timeout(long long wait_cycles);
 

@@ -379,7 +379,7 @@ def weight_grad(saved_x, dy, dW, workspace, db=None, length=None, stream=0):
 
 
 def arm_train_timeout(wait_cycles):
-    """Test interface: the next weight_grad call of this thread has a wait that runs out (see tsdp.h)."""
+    """Test interface: the next group_norm, group_norm_grad or weight_grad call of this thread has a wait that runs out (see tsdp.h)."""
     _status(load_library().tsdp_debug_arm_train_timeout(int(wait_cycles)), "tsdp_debug_arm_train_timeout")
 
 

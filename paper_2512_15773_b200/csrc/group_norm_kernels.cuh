@@ -119,6 +119,8 @@ struct NormArgs {
   // slab kernels: threads of a group that a shuffle adds up; rows of partial sums left (of warps or lanes); bytes of a stage
   int fold, red_rows, stage_bytes;
   int team;                                    // warp kernels: warps of a group (0 elsewhere)
+  long long wait_cycles;                       // slab kernels: limit of every wait
+  int withhold;                                // CTA 0 gets no rows (tsdp_debug_arm_train_timeout)
 };
 
 constexpr int GN_STREAM_V = 4;                 // channels of a thread over long sequences and in every backward pass: with eight (16 bytes of

@@ -88,6 +88,22 @@ __device__ __forceinline__ void group_sum(const NormArgs& g, int gcols, int col,
       for (int k = 0; k < K; ++k) v[k] += s_red[(i * per + gi * parts + j) * K + k];
 }
 
+// Waits are bounded.  A thread whose wait ran out waits no more and takes NaN for what it did not get, which its group's sums carry to all of the
+// group; the CTA asks for no further rows (lost, set before the barrier of a sum) and stays until copies that may still be in flight have landed.
+__device__ __forceinline__ bool slab_wait(uint32_t bar, uint32_t ph, long long limit, int& lost) {
+  const bool ok = ptx::mbar_wait_thread(bar, ph, limit);
+  if (!ok) lost = 1;
+  return ok;
+}
+__device__ __forceinline__ bool slab_more(const int& lost) { return __all_sync(0xffffffffu, *(const volatile int*)&lost == 0) != 0; }
+__device__ __forceinline__ void slab_drain(const int& lost) {      // by all threads
+  __syncthreads();
+  if (lost) {
+    const long long t0 = clock64();
+    while (clock64() - t0 < 400000ll) { }
+  }
+}
+
 template <typename T, int ITEMS>
 __global__ void __launch_bounds__(GN_THREADS, GN_SLAB_CTAS)
 group_norm_slab_kernel(NormArgs g) {
@@ -95,6 +111,7 @@ group_norm_slab_kernel(NormArgs g) {
   extern __shared__ __align__(16) uint8_t gs_raw[];
   __shared__ float s_red[GN_THREADS], s_red2[2 * GN_THREADS];
   __shared__ __align__(8) unsigned long long s_bar[GN_RING];
+  __shared__ int s_lost;
   const int cg = g.C / g.groups, gcols = cg / V;
   const int set = blockIdx.x % g.sets, split = blockIdx.x / g.sets;
   const int c_set = set * g.width, width = min(g.width, g.C - c_set);
@@ -112,13 +129,14 @@ group_norm_slab_kernel(NormArgs g) {
     if (g.film && wl < 2) bulk_load(dst + film_off + wl * 4u * g.width, g.film + ((long long)n * 2 + wl) * g.C + c_set, 4u * width, bar);
   };
   if (threadIdx.x == 0) {
+    s_lost = 0;
     for (int s = 0; s < GN_RING; ++s) ptx::mbar_init(ptx::smem_u32(&s_bar[s]), 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
   }
   __syncthreads();
   pdl_wait();
-  if (threadIdx.x < 32)
+  if (threadIdx.x < 32 && !(g.withhold && blockIdx.x == 0))
     for (int s = 0; s < GN_RING; ++s)
       if (split + s * g.splits < g.N) issue(split + s * g.splits, s);
   float2 ga[P], be[P];
@@ -130,8 +148,9 @@ group_norm_slab_kernel(NormArgs g) {
   const float inv = 1.f / ((float)g.L * cg);
   int s = 0;
   uint32_t ph = 0;
+  bool ok = true;
   for (int n = split; n < g.N; n += g.splits) {
-    const bool ok = ptx::mbar_wait_thread(ptx::smem_u32(&s_bar[s]), ph);
+    ok = ok && slab_wait(ptx::smem_u32(&s_bar[s]), ph, g.wait_cycles, s_lost);
     const uint8_t* stage = gs_raw + s * g.stage_bytes;
     uint4 raw[ITEMS];
     float2 fs[P], fb[P];
@@ -161,7 +180,7 @@ group_norm_slab_kernel(NormArgs g) {
     float sum[1] = {t2.x + t2.y};
     group_sum<1>(g, gcols, col, lane, s_red, sum);
     // every thread has taken its share of the stage
-    if (threadIdx.x < 32 && n + GN_RING * g.splits < g.N) issue(n + GN_RING * g.splits, s);
+    if (threadIdx.x < 32 && n + GN_RING * g.splits < g.N && slab_more(s_lost)) issue(n + GN_RING * g.splits, s);
     if (++s == GN_RING) { s = 0; ph ^= 1; }
     const float about = sum[0] * inv;          // the mean, but for the roundings of a sum of values; the sum of what lies about it gives their size
     float2 t1 = two(0.f);
@@ -207,6 +226,7 @@ group_norm_slab_kernel(NormArgs g) {
       }
     });
   }
+  slab_drain(s_lost);
 }
 
 // Backward.  dz stays in registers between the sums and dx; h is taken from x again.  A thread owns four channels: with eight, the sums of
@@ -219,6 +239,7 @@ group_norm_slab_grad_kernel(NormArgs g) {
   extern __shared__ __align__(16) uint8_t gs_raw[];
   __shared__ float s_red[2][2 * GN_THREADS];
   __shared__ __align__(8) unsigned long long s_bar[GN_RING];
+  __shared__ int s_lost;
   const int cg = g.C / g.groups, gcols = cg / V;
   const int set = blockIdx.x % g.sets, split = blockIdx.x / g.sets;
   const int c_set = set * g.width, width = min(g.width, g.C - c_set);
@@ -241,13 +262,14 @@ group_norm_slab_grad_kernel(NormArgs g) {
     if (g.film && wl == 0) bulk_load(dst + film_off, g.film + (long long)n * 2 * g.C + c_set, 4u * width, bar);
   };
   if (threadIdx.x == 0) {
+    s_lost = 0;
     for (int s = 0; s < GN_RING; ++s) ptx::mbar_init(ptx::smem_u32(&s_bar[s]), 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
   }
   __syncthreads();
   pdl_wait();
-  if (threadIdx.x < 32)
+  if (threadIdx.x < 32 && !(g.withhold && blockIdx.x == 0))
     for (int s = 0; s < GN_RING; ++s)
       if (split + s * g.splits < g.N) issue(split + s * g.splits, s);
   float2 ga[P], be[P], acc_z[P], acc_h[P];
@@ -277,13 +299,14 @@ group_norm_slab_grad_kernel(NormArgs g) {
   ahead(split);
   int s = 0, odd = 0;
   uint32_t ph = 0;
+  bool ok = true;
   for (int n = split; n < g.N; n += g.splits) {
     const float mean = mu_next, rstd = rs_next;
     uint32_t step[ITEMS];
 #pragma unroll
     for (int j = 0; j < ITEMS; ++j) step[j] = COPY ? sb[j] : 0u;
     ahead(n + g.splits);
-    const bool ok = ptx::mbar_wait_thread(ptx::smem_u32(&s_bar[s]), ph);
+    ok = ok && slab_wait(ptx::smem_u32(&s_bar[s]), ph, g.wait_cycles, s_lost);
     const uint8_t* stage = gs_raw + s * g.stage_bytes;
     float2 fs[P];
 #pragma unroll
@@ -311,7 +334,9 @@ group_norm_slab_grad_kernel(NormArgs g) {
         dyr = load_piece<T, V>(stage + l * row_bytes + col * V * (int)sizeof(T));
         xr[j] = load_piece<X, V>(stage + x_off + l * x_bytes + col * V * (int)sizeof(X));
       }
-      if (!ok) dyr.w[0] = dyr.w[sizeof(dyr) / 4 - 1] = 0x7fc07fc0u;             // a wait that ran out: NaN
+      if (!ok)                                     // a wait that ran out: NaN
+#pragma unroll
+        for (int i = 0; i < (int)(sizeof(dyr) / 4); ++i) dyr.w[i] = 0x7fc07fc0u;
       float2 h[P], dy[P];
       x_values(j, h);
       piece_values<T, V>(dyr, dy);
@@ -345,7 +370,7 @@ group_norm_slab_grad_kernel(NormArgs g) {
         *reinterpret_cast<float2*>(film + (g.lanes + lane) * g.width + col * V + 2 * i) = s_y[i];
       }
     group_sum<2>(g, gcols, col, lane, s_red[odd], m);
-    if (threadIdx.x < 32 && n + GN_RING * g.splits < g.N) issue(n + GN_RING * g.splits, s);
+    if (threadIdx.x < 32 && n + GN_RING * g.splits < g.N && slab_more(s_lost)) issue(n + GN_RING * g.splits, s);
     if (++s == GN_RING) { s = 0; ph ^= 1; }
     odd ^= 1;
     const float m1 = m[0] * inv, m2 = m[1] * inv;
@@ -371,7 +396,7 @@ group_norm_slab_grad_kernel(NormArgs g) {
       }
   }
   // shares of dbeta and dgamma: over the lanes, through the memory of the ring
-  __syncthreads();
+  slab_drain(s_lost);
   float* s_acc = reinterpret_cast<float*>(gs_raw);          // [2][lanes][width]
   if (in)
 #pragma unroll

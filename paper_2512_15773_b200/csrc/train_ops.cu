@@ -429,6 +429,8 @@ int tsdp_group_norm(int device, const tsdp_norm_t* shape, const void* d_x, int64
   cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
   NormArgs g{};
   g.N = N; g.L = L; g.C = C; g.groups = shape->groups; g.act = shape->act; g.eps = shape->eps;
+  const Waits waits;
+  g.wait_cycles = waits.cycles; g.withhold = waits.withhold;
   g.x = rows_of(d_x, x_n, x_l, N, L, C);
   g.y = rows_of(d_y, y_n, y_l, N, L, C);
   g.gamma = d_gamma; g.beta = d_beta; g.film = d_film; g.mean = d_mean; g.rstd = d_rstd;
@@ -496,6 +498,8 @@ int tsdp_group_norm_grad(int device, const tsdp_norm_t* shape, const void* d_dy,
     return TSDP_ERR_ARG;
   NormArgs g{};
   g.N = shape->N; g.L = shape->L; g.C = C; g.groups = shape->groups; g.act = shape->act; g.eps = shape->eps;
+  const Waits waits;
+  g.wait_cycles = waits.cycles; g.withhold = waits.withhold;
   g.x = rows_of(d_x, x_n, x_l, g.N, g.L, C);
   g.dy = rows_of(d_dy, dy_n, dy_l, g.N, g.L, C);
   g.dx = rows_of(d_dx, dx_n, dx_l, g.N, g.L, C);

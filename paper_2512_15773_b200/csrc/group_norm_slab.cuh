@@ -62,9 +62,16 @@ template <typename T, int V> __device__ __forceinline__ uint4 pack16(const float
   if constexpr (sizeof(T) == 2) return make_uint4(pack_bf16(y[0].x, y[0].y), pack_bf16(y[1].x, y[1].y), pack_bf16(y[2].x, y[2].y), pack_bf16(y[3].x, y[3].y));
   else return make_uint4(__float_as_uint(y[0].x), __float_as_uint(y[0].y), __float_as_uint(y[1].x), __float_as_uint(y[1].y));
 }
-// Sum over the threads of a group: within a warp by shuffles, the rest through s_red.  One barrier.
+// The parts of a row of s_red that make up the sum of a column's group: none for a thread without a column (cols is rounded up to whole blocks of
+// 32 channels, and threads may be left over behind the last row), which lies in no group.
+struct GroupParts { int first, count; };
+__host__ __device__ __forceinline__ GroupParts group_parts(const NormArgs& g, int gcols, int col, bool in) {
+  const int parts = gcols / g.fold;
+  return GroupParts{col / gcols * parts, in ? parts : 0};
+}
+// Sum over the threads of a group: within a warp by shuffles, the rest through s_red.  One barrier.  Zero for a thread without a column.
 template <int K>
-__device__ __forceinline__ void group_sum(const NormArgs& g, int gcols, int col, int row, float* s_red, float (&v)[K]) {
+__device__ __forceinline__ void group_sum(const NormArgs& g, int gcols, int col, int row, bool in, float* s_red, float (&v)[K]) {
   const int wl = threadIdx.x & 31, per = g.cols / g.fold;
   for (int o = 1; o < g.fold; o *= 2)
 #pragma unroll
@@ -79,13 +86,13 @@ __device__ __forceinline__ void group_sum(const NormArgs& g, int gcols, int col,
 #pragma unroll
     for (int k = 0; k < K; ++k) s_red[(r * per + col / g.fold) * K + k] = v[k];
   __syncthreads();
-  const int gi = col / gcols, parts = gcols / g.fold;
+  const GroupParts mine = group_parts(g, gcols, col, in);
 #pragma unroll
   for (int k = 0; k < K; ++k) v[k] = 0.f;
   for (int i = 0; i < g.red_rows; ++i)
-    for (int j = 0; j < parts; ++j)
+    for (int j = 0; j < mine.count; ++j)
 #pragma unroll
-      for (int k = 0; k < K; ++k) v[k] += s_red[(i * per + gi * parts + j) * K + k];
+      for (int k = 0; k < K; ++k) v[k] += s_red[(i * per + mine.first + j) * K + k];
 }
 
 // Waits are bounded.  A thread whose wait ran out waits no more and takes NaN for what it did not get, which its group's sums carry to all of the
@@ -178,7 +185,7 @@ group_norm_slab_kernel(NormArgs g) {
       for (int i = 0; i < P; ++i) t2 = __fadd2_rn(t2, v[i]);       // (zeros where there is no row)
     }
     float sum[1] = {t2.x + t2.y};
-    group_sum<1>(g, gcols, col, lane, s_red, sum);
+    group_sum<1>(g, gcols, col, lane, in, s_red, sum);
     // every thread has taken its share of the stage
     if (threadIdx.x < 32 && n + GN_RING * g.splits < g.N && slab_more(s_lost)) issue(n + GN_RING * g.splits, s);
     if (++s == GN_RING) { s = 0; ph ^= 1; }
@@ -195,7 +202,7 @@ group_norm_slab_kernel(NormArgs g) {
       }
     }
     float moments[2] = {in ? t1.x + t1.y : 0.f, in ? t2.x + t2.y : 0.f};
-    group_sum<2>(g, gcols, col, lane, s_red2, moments);
+    group_sum<2>(g, gcols, col, lane, in, s_red2, moments);
     const float off = moments[0] * inv, mean = about + off;
     const float rstd = rsqrtf(variance_about(moments[1] * inv, off) + g.eps);
     if (in && lane == 0 && col % gcols == 0) {
@@ -369,7 +376,7 @@ group_norm_slab_grad_kernel(NormArgs g) {
         *reinterpret_cast<float2*>(film + lane * g.width + col * V + 2 * i) = s_a[i];
         *reinterpret_cast<float2*>(film + (g.lanes + lane) * g.width + col * V + 2 * i) = s_y[i];
       }
-    group_sum<2>(g, gcols, col, lane, s_red[odd], m);
+    group_sum<2>(g, gcols, col, lane, in, s_red[odd], m);
     if (threadIdx.x < 32 && n + GN_RING * g.splits < g.N && slab_more(s_lost)) issue(n + GN_RING * g.splits, s);
     if (++s == GN_RING) { s = 0; ph ^= 1; }
     odd ^= 1;

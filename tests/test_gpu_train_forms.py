@@ -1,7 +1,7 @@
 """GroupNorm and its gradients in each of their forms, where a form can go wrong alone: values far from zero, groups of one value, strided rows,
 values that are not finite.
 
-The forms (paper_2512_15773_b200/csrc/train_ops.cu): one warp a group, a team of warps, slabs, the stream form.  u = 2^-24."""
+The forms (paper_2512_15773_b200/csrc/group_norm_plan.cuh): one warp a group, a team of warps, slabs, the stream form.  u = 2^-24."""
 import numpy as np
 import pytest
 import torch

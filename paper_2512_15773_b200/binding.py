@@ -192,7 +192,8 @@ def verify_commit_static(d_xt, d_muhat, d_eps, h_t, B, K, D, accept, seed, d_act
 
 # ---------------------------------------------------------------------------------------------- operators of a training step
 # Module-level functions on torch tensors (see tsdp.h): they check types, shapes and devices, which the C side cannot see, and
-# only enqueue work on `stream` (a cudaStream_t; 0 is the default stream).  The tensors have to live until that work is done.
+# only enqueue work on `stream` (a cudaStream_t; 0 is the default stream; None, torch's current stream of the tensors' device).  The
+# tensors have to live until that work is done.
 
 @functools.lru_cache(maxsize=None)
 def _torch():
@@ -279,6 +280,14 @@ def _workspace(t, device):
     return t.data_ptr(), t.numel() * t.element_size()
 
 
+def _current_stream(device):
+    return _torch()._C._cuda_getCurrentRawStream(device)
+
+
+def _on(stream, device):
+    return _current_stream(device) if stream is None else stream
+
+
 def _status(st, what):
     if st != 0:
         raise TsdpError(st, what, load_library().tsdp_strerror(st).decode())
@@ -291,23 +300,23 @@ def saved_like(x):
             torch.empty((*x.shape[:-1], -(-x.shape[-1] // 32)), dtype=torch.uint8, device=x.device))
 
 
-def checkpoint_pack(x, saved, stream=0):
+def checkpoint_pack(x, saved, stream=None):
     """Write the 8-bit copy of x into saved = (q, scale)."""
     p, sn, sl, N, L, ch = _rows(x, "x")
     dev = x.get_device()
-    _status(load_library().tsdp_checkpoint_pack(dev, _dtype_code(x, "x"), p, sn, sl, N, L, ch, _saved(saved, "saved", N * L, ch, dev), stream),
+    _status(load_library().tsdp_checkpoint_pack(dev, _dtype_code(x, "x"), p, sn, sl, N, L, ch, _saved(saved, "saved", N * L, ch, dev), _on(stream, dev)),
             "tsdp_checkpoint_pack")
 
 
-def checkpoint_unpack(saved, x, stream=0):
+def checkpoint_unpack(saved, x, stream=None):
     """Write the values that saved = (q, scale) stands for into x."""
     p, sn, sl, N, L, ch = _rows(x, "x")
     dev = x.get_device()
-    _status(load_library().tsdp_checkpoint_unpack(dev, _dtype_code(x, "x"), _saved(saved, "saved", N * L, ch, dev), p, sn, sl, N, L, ch, stream),
+    _status(load_library().tsdp_checkpoint_unpack(dev, _dtype_code(x, "x"), _saved(saved, "saved", N * L, ch, dev), p, sn, sl, N, L, ch, _on(stream, dev)),
             "tsdp_checkpoint_unpack")
 
 
-def group_norm(x, gamma, beta, groups, y, act="mish", film=None, eps=1e-5, mean=None, rstd=None, saved_x=None, saved_y=None, stream=0):
+def group_norm(x, gamma, beta, groups, y, act="mish", film=None, eps=1e-5, mean=None, rstd=None, saved_x=None, saved_y=None, stream=None):
     """y = film scale * act(GroupNorm(x)) + film bias; mean, rstd [N, groups] and the 8-bit copies of x and y where given."""
     p, sn, sl, N, L, ch = _rows(x, "x")
     yp, yn, yl = _rows(y, "y", x)[:3]
@@ -316,7 +325,7 @@ def group_norm(x, gamma, beta, groups, y, act="mish", film=None, eps=1e-5, mean=
         dev, _norm_t(_dtype_code(x, "x"), N, L, ch, _count(groups, "groups"), _act(act), eps), p, sn, sl, _dense(gamma, "gamma", ch, f32, dev),
         _dense(beta, "beta", ch, f32, dev), _dense(film, "film", 2 * N * ch, f32, dev), yp, yn, yl,
         _dense(mean, "mean", N * groups, f32, dev), _dense(rstd, "rstd", N * groups, f32, dev), _saved(saved_x, "saved_x", N * L, ch, dev),
-        _saved(saved_y, "saved_y", N * L, ch, dev), stream), "tsdp_group_norm")
+        _saved(saved_y, "saved_y", N * L, ch, dev), _on(stream, dev)), "tsdp_group_norm")
 
 
 def group_norm_grad_workspace(dy, groups):
@@ -329,7 +338,7 @@ def group_norm_grad_workspace(dy, groups):
 
 
 def group_norm_grad(dy, x, gamma, beta, groups, mean, rstd, dx, dgamma, dbeta, workspace, act="mish", film=None, dfilm=None,
-                    saved_x=None, stream=0):
+                    saved_x=None, stream=None):
     """Gradients of group_norm: dx, dgamma, dbeta and, where given, dfilm; the input as x or (x None) as its 8-bit copy saved_x."""
     p, sn, sl, N, L, ch = _rows(dy, "dy")
     if (x is None) == (saved_x is None):
@@ -342,7 +351,7 @@ def group_norm_grad(dy, x, gamma, beta, groups, mean, rstd, dx, dgamma, dbeta, w
         _dense(gamma, "gamma", ch, f32, dev), _dense(beta, "beta", ch, f32, dev), _dense(film, "film", 2 * N * ch, f32, dev),
         _dense(mean, "mean", N * groups, f32, dev), _dense(rstd, "rstd", N * groups, f32, dev), dp, dn, dl,
         _dense(dgamma, "dgamma", ch, f32, dev), _dense(dbeta, "dbeta", ch, f32, dev), _dense(dfilm, "dfilm", 2 * N * ch, f32, dev),
-        *_workspace(workspace, dev), stream), "tsdp_group_norm_grad")
+        *_workspace(workspace, dev), _on(stream, dev)), "tsdp_group_norm_grad")
 
 
 def _weight_sizes(dy, length):
@@ -364,7 +373,7 @@ def weight_grad_workspace(dy, channels, taps=1, length=None):
     return n
 
 
-def weight_grad(saved_x, dy, dW, workspace, db=None, length=None, stream=0):
+def weight_grad(saved_x, dy, dW, workspace, db=None, length=None, stream=None):
     """dW [taps, in, out] (or [in, out]) and db [out] from dy [rows, out] and the 8-bit copy of the layer's input [rows, in];
     length: rows of a sequence, beyond whose ends a convolution sees zeros (default: all rows are one sequence)."""
     shape = dW.shape
@@ -375,7 +384,7 @@ def weight_grad(saved_x, dy, dW, workspace, db=None, length=None, stream=0):
     dev, f32 = dy.get_device(), _torch().float32
     _status(load_library().tsdp_weight_grad(
         dev, _dtype_code(dy, "dy"), _saved(saved_x, "saved_x", N * L, _count(channels, "dW"), dev), p, sl, N, L, channels, out, _count(taps, "dW"),
-        _dense(dW, "dW", taps * channels * out, f32, dev), _dense(db, "db", out, f32, dev), *_workspace(workspace, dev), stream), "tsdp_weight_grad")
+        _dense(dW, "dW", taps * channels * out, f32, dev), _dense(db, "db", out, f32, dev), *_workspace(workspace, dev), _on(stream, dev)), "tsdp_weight_grad")
 
 
 def arm_train_timeout(wait_cycles):

@@ -154,3 +154,60 @@ def test_a_first_position_unlike_the_rest_costs_no_digits(L, C, G, first, rest, 
     h = np.abs((host(x) - wide(rm)) * wide(rr))
     e = np.abs(host(ga)) * (wide(rr * e_m) + h * (wide(e_r) + 6 * U)) + 3 * U * (np.abs(ry) + np.abs(host(be)))
     assert (np.abs(host(y) - ry) <= e + (half(dtype) * np.abs(ry) * 1.01 if dtype != "fp32" else 0)).all()
+
+
+# ------------------------------------------------------------------------------------------------ streams
+def test_calls_without_a_stream_join_a_capture():
+    """Under torch.cuda.graph the current stream is the captured one; the replay works on what the inputs hold by then."""
+    N, L, C, G = 3, 16, 128, 2
+    rng = np.random.default_rng(4)
+    ga, be = affine(rng, C)
+    x, dy = rng_tensor(rng, (N, L, C), "bf16"), rng_tensor(rng, (N, L, C), "bf16", 0)
+    y, dx, saved = torch.empty_like(x), torch.empty_like(x), binding.saved_like(x)
+    mean, rstd, dga, dbe = torch.empty(N, G, device="cuda"), torch.empty(N, G, device="cuda"), torch.empty(C, device="cuda"), torch.empty(C, device="cuda")
+    dW, db = torch.empty(C, C, device="cuda"), torch.empty(C, device="cuda")
+    flat = saved[0].view(N * L, C), saved[1].view(N * L, -1)
+    ws = torch.empty(max(binding.group_norm_grad_workspace(dy, G), binding.weight_grad_workspace(dy.view(N * L, C), C)), dtype=torch.uint8, device="cuda")
+
+    def step():
+        binding.group_norm(x, ga, be, G, y, mean=mean, rstd=rstd)
+        binding.checkpoint_pack(x, saved)
+        binding.group_norm_grad(dy, None, ga, be, G, mean, rstd, dx, dga, dbe, ws, saved_x=saved)
+        binding.weight_grad(flat, dx.view(N * L, C), dW, ws, db=db)
+        binding.checkpoint_unpack(saved, x)
+    outs = (y, mean, rstd, dx, dga, dbe, dW, db, x)
+    step()                                               # (kernels are set up outside the capture or within: either will do)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    fresh = rng_tensor(rng, (N, L, C), "bf16")
+    x.copy_(fresh)
+    step()
+    torch.cuda.synchronize()
+    want = [t.clone() for t in outs]
+    for t in outs:
+        t.zero_()
+    x.copy_(fresh)
+    graph.replay()
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(outs, want))
+
+
+def test_calls_under_a_stream_of_torch_follow_its_work():
+    N, L, C, G = 64, 16, 512, 8
+    rng = np.random.default_rng(5)
+    ga, be = affine(rng, C)
+    x = rng_tensor(rng, (N, L, C), "fp32")
+    want = forward(x, ga, be, G)[0]
+    torch.cuda.synchronize()
+    s = torch.cuda.Stream()
+    with torch.cuda.stream(s):
+        late, y = torch.zeros_like(x), torch.empty_like(x)
+        a = torch.randn(4096, 4096, device="cuda")
+        for _ in range(20):
+            a = a @ a.clamp(-1e-3, 1e-3)                 # some milliseconds before x is there
+        late.add_(x).add_(0.0 * a[0, 0].clamp(-1, 1))
+        binding.group_norm(late, ga, be, G, y, act="none")
+        got = y.clone()
+    s.synchronize()
+    assert torch.equal(got, want)

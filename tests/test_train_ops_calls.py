@@ -97,3 +97,20 @@ def test_counts_past_an_int_are_not_cut(monkeypatch, far):
     assert not lib.calls
     binding.group_norm(x, f32, f32, 8, x, stream=0)
     assert lib.calls[0][0] == "tsdp_group_norm"
+
+
+@pytest.mark.parametrize("given,taken_as", [({}, 77), (dict(stream=None), 77), (dict(stream=0), 0), (dict(stream=5), 5)])
+def test_a_call_goes_to_the_current_stream_unless_one_is_given(monkeypatch, given, taken_as):
+    """Between torch operations under torch.cuda.stream(s), or in a capture, the default stream would be another one than that of the tensors' own work."""
+    lib = taken(monkeypatch)
+    monkeypatch.setattr(binding, "_current_stream", lambda device: 77 + device)
+    x, f32, dW = Rows(2, 16, 64), Rows(64, dtype="float32"), Rows(64, 64, dtype="float32")
+    saved = Rows(2, 16, 64, dtype="int8"), Rows(2, 16, 2, dtype="uint8")
+    flat = Rows(32, 64, dtype="int8"), Rows(32, 2, dtype="uint8")
+    stat, ws = Rows(2, 8, dtype="float32"), Rows(1 << 20, dtype="uint8")
+    binding.checkpoint_pack(x, saved, **given)
+    binding.checkpoint_unpack(saved, x, **given)
+    binding.group_norm(x, f32, f32, 8, x, **given)
+    binding.group_norm_grad(x, x, f32, f32, 8, stat, stat, x, f32, f32, ws, **given)
+    binding.weight_grad(flat, Rows(32, 64), dW, ws, **given)
+    assert [a[-1] for _, a in lib.calls] == [taken_as] * 5

@@ -211,3 +211,141 @@ def test_calls_under_a_stream_of_torch_follow_its_work():
         got = y.clone()
     s.synchronize()
     assert torch.equal(got, want)
+
+
+# ------------------------------------------------------------------------------------------------ layouts
+def laid_out(shape, dtype, layout):
+    """An empty tensor [N, L, C] of this layout and the buffer around it, full of sevens.  All but the last keep rows in 16-byte pieces, and so the form that
+    dense rows take."""
+    N, L, C = shape
+    full = lambda *s: torch.full(s, 7.0, dtype=TYPES[dtype], device="cuda")  # noqa: E731
+    if layout == "padded":                                  # two rows before and after the sequence, the UNet's own layout
+        buf = full(N, L + 4, C)
+        return buf[:, 2:2 + L], buf
+    if layout == "slice":                                   # channels of a wider row
+        buf = full(N, L, C + 64)
+        return buf[:, :, 32:32 + C], buf
+    if layout == "positions first":
+        buf = full(L, N, C)
+        return buf.transpose(0, 1), buf
+    if layout == "every other":                             # sequences and rows of a larger tensor
+        buf = full(2 * N, 2 * L, C)
+        return buf[::2, ::2], buf
+    buf = full(N, L, C + 3)                                 # odd addresses: the stream form, whatever dense rows take
+    return buf[:, :, 1:1 + C], buf
+
+
+LAYOUTS = ["padded", "slice", "positions first", "every other"]
+
+
+@pytest.mark.parametrize("saved", [False, True])
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("layout", LAYOUTS)
+@pytest.mark.parametrize("form", FORMS)
+def test_strided_rows_give_the_bits_of_dense_ones(form, layout, dtype, saved):
+    N, L, C, G = FORMS[form]
+    rng = np.random.default_rng(L + C)
+    ga, be = affine(rng, C)
+    film = rng_tensor(rng, (N, 2 * C), "fp32", 0.5, 0.3)
+    dense = [rng_tensor(rng, (N, L, C), dtype, 0.4), rng_tensor(rng, (N, L, C), dtype, 0.1)]
+    def both(x, dy, y, dx):
+        sx, sy = (binding.saved_like(dense[0]), binding.saved_like(dense[0])) if saved else (None, None)
+        mean, rstd = empty(N, G), empty(N, G)
+        binding.group_norm(x, ga, be, G, y, film=film, mean=mean, rstd=rstd, saved_x=sx, saved_y=sy)
+        grads = backward(dy, None if saved else x, sx, ga, be, G, mean, rstd, "mish", film, dx)
+        return [y, mean, rstd, *grads, *(sx + sy if saved else ())]
+    want = both(*dense, *[torch.full_like(dense[0], float("nan")) for _ in range(2)])
+    apart = [laid_out((N, L, C), dtype, layout) for _ in range(4)]
+    for (t, _), v in zip(apart, dense):
+        t.copy_(v)
+    got = both(*[t for t, _ in apart])
+    for a, b in zip(got, want):
+        assert torch.equal(a, b)
+    for t, buf in apart[2:]:
+        t.fill_(7.0)
+        assert (buf == 7.0).all()                            # nothing between the rows was written
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("form", FORMS)
+def test_inputs_of_one_row_for_all(form, dtype):
+    """Strides of zero: an x of one sequence for all, of one position for all; a dy of one row for all."""
+    N, L, C, G = FORMS[form]
+    rng = np.random.default_rng(C)
+    ga, be = affine(rng, C)
+    x, row = rng_tensor(rng, (1, L, C), dtype).expand(N, L, C), rng_tensor(rng, (1, 1, C), dtype).expand(N, L, C)
+    out = lambda: torch.full((N, L, C), float("nan"), dtype=TYPES[dtype], device="cuda")  # noqa: E731
+    for t in (x, row):
+        y, want, stats, dense = out(), out(), (empty(N, G), empty(N, G)), (empty(N, G), empty(N, G))
+        binding.group_norm(t, ga, be, G, y, mean=stats[0], rstd=stats[1])
+        binding.group_norm(t.contiguous(), ga, be, G, want, mean=dense[0], rstd=dense[1])
+        assert torch.equal(y, want) and all(torch.equal(a, b) for a, b in zip(stats, dense))
+        got = backward(row, t, None, ga, be, G, *stats, "mish", None, out())
+        ref = backward(row.contiguous(), t.contiguous(), None, ga, be, G, *stats, "mish", None, out())
+        assert all(torch.equal(a, b) for a, b in zip(got[:3], ref[:3]))
+
+
+# ------------------------------------------------------------------------------------------------ what is not finite
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("bad", [float("inf"), float("-inf"), float("nan")])
+@pytest.mark.parametrize("form", FORMS)
+def test_what_is_not_finite_stays_in_its_group(form, bad, dtype):
+    """In x: its group's y, dx and dfilm are NaN and the statistics not finite, its block's copy stands for NaN, its channels' dgamma are NaN; all else keeps its
+    bits.  (A gradient that reads x from its copy meets NaN in all groups of that block.)  In dy: no dx of its group is finite, which subtracts an
+    infinite mean; nor are dgamma and dbeta of its channel."""
+    N, L, C, G = FORMS[form]
+    w = C // G
+    rng = np.random.default_rng(C + 1)
+    ga, be = affine(rng, C)
+    film = rng_tensor(rng, (N, 2 * C), "fp32", 0.5, 0.3)
+    x, dy = rng_tensor(rng, (N, L, C), dtype), rng_tensor(rng, (N, L, C), dtype, 0.1)
+
+    def run(x, dy):
+        sx, sy, y, mean, rstd = binding.saved_like(x), binding.saved_like(x), torch.full_like(x, 7.0), empty(N, G), empty(N, G)
+        binding.group_norm(x, ga, be, G, y, film=film, mean=mean, rstd=rstd, saved_x=sx, saved_y=sy)
+        return [y, mean, rstd, sx, sy] + [backward(dy, None if s else x, s, ga, be, G, mean, rstd, "mish", film) for s in (None, sx)]
+    good = run(x, dy)
+    n, l, c = N - 1, L // 2, C - 1
+    grp = c // w
+    xb, dyb = x.clone(), dy.clone()
+    xb[n, l, c] = bad
+    dyb[n, l, c] = bad
+    here = torch.zeros(N, L, C, dtype=torch.bool, device="cuda")
+    here[n, :, grp * w:grp * w + w] = True
+    per_group = torch.zeros(N, G, dtype=torch.bool, device="cuda")
+    per_group[n, grp] = True
+    channels = here.any(0).any(0)
+    films = torch.cat([here.any(1), torch.zeros(N, C, dtype=torch.bool, device="cuda")], 1)      # (of the scale; that of the bias is a sum of dy)
+
+    def nan_there(a, b, where):
+        assert torch.isnan(a[where]).all() and torch.equal(a[~where], b[~where])
+    got = run(xb, dy)
+    nan_there(got[0], good[0], here)
+    for i in (1, 2):
+        assert not torch.isfinite(got[i][n, grp]) and torch.equal(got[i][~per_group], good[i][~per_group])
+    blocks = torch.zeros(N, L, -(-C // 32), dtype=torch.bool, device="cuda")
+    blocks[n, l, c // 32] = True
+    assert (got[3][1][blocks] == 255).all() and torch.equal(got[3][1][~blocks], good[3][1][~blocks])
+    inside = torch.zeros_like(blocks)
+    inside[n, :, grp * w // 32:(grp * w + w - 1) // 32 + 1] = True
+    assert (got[4][1][inside] == 255).all() and torch.equal(got[4][1][~inside], good[4][1][~inside])
+    for copy, g, want in zip((False, True), got[5:], good[5:]):
+        if copy:
+            c0, c1 = min(c // 32 * 32 // w, grp) * w, C                    # (c is the last channel: its block and its group end together)
+            here[n, :, c0:c1] = True
+            channels[c0:c1] = True
+            films[n, c0:c1] = True
+        nan_there(g[0], want[0], here)
+        nan_there(g[1], want[1], channels)
+        nan_there(g[2], want[2], channels)
+        nan_there(g[3], want[3], films)
+    here[:] = False
+    here[n, :, grp * w:] = True
+    got = run(x, dyb)
+    for a, b in zip(got[:3], good[:3]):
+        assert torch.equal(a, b)
+    for g, want in zip(got[5:], good[5:]):
+        assert not torch.isfinite(g[0][n, l, c]) and not torch.isfinite(g[0][here]).any() and torch.equal(g[0][~here], want[0][~here])
+        for i in (1, 2):
+            keep = torch.arange(C, device="cuda") != c
+            assert not torch.isfinite(g[i][c]) and torch.equal(g[i][keep], want[i][keep])

@@ -364,7 +364,7 @@ __device__ __forceinline__ void norm_walk(const NormArgs& g, int n, int l0, int 
 #pragma unroll
       for (int j = 0; j < GN_WALK; ++j) {
         const int lj = l + j * g.lanes;
-        x[j] = Piece<X, V>{};                                  // (a position that is not there counts nothing: its dy is zero)
+        x[j] = Piece<X, V>{};
         dy[j] = Piece<T, V>{};
         b[j] = 0u;
         if (lj < hi) {
@@ -375,6 +375,7 @@ __device__ __forceinline__ void norm_walk(const NormArgs& g, int n, int l0, int 
       }
 #pragma unroll
       for (int j = 0; j < GN_WALK; ++j) {
+        if (j > 0 && l + j * g.lanes >= hi) break;
         float2 h[P], dz[P], dya[P], dyf[P];
         piece_pairs<X, V>(x[j], h);
         piece_pairs<T, V>(dy[j], dyf);
@@ -496,7 +497,7 @@ group_norm_grad_kernel(NormArgs g) {
         // (the product rounded before m1 is taken off: where a group is one value, the two are the same number)
 #pragma unroll
         for (int i = 0; i < P; ++i) dz[i] = __fmul2_rn(p.rs[i], __ffma2_rn(h[i], m2[i], __fadd2_rn(__fmul2_rn(dz[i], p.ga[i]), m1[i])));
-        if (l < hi) store_pairs<T, V>(dx + l * g.dx.sl + c, dz);
+        store_pairs<T, V>(dx + l * g.dx.sl + c, dz);
       });
     }
     if (g.ranks > 1) ptx::cluster_sync_all();

@@ -215,6 +215,7 @@ group_norm_warp_grad_kernel(NormArgs g) {
   __syncwarp();
   fetch(split, 0);
   const long long dx_step = R * g.dx.sl;
+  const int have = (rows - lr + R - 1) / R;     // of this lane
   int s = 0, odd = 0;
   for (int n = split; n < g.N; n += g.splits) {
     const float mean = nmean, rstd = nrstd, steps = COPY ? copy_step(nstep) : 1.f;
@@ -237,16 +238,16 @@ group_norm_warp_grad_kernel(NormArgs g) {
     if constexpr (COPY)
 #pragma unroll
       for (int j = 0; j < ITEMS; ++j) scale[j] = __shfl_sync(0xffffffffu, steps, min((lr + j * R) * gb + (cc >> 5), 31));
-    auto h_values = [&](int j, float2* h) {
+    auto h_values = [&](int j, float2* h, float rs) {
       piece_values<X, V>(load_piece<X, V>(xs + j * R * cg * sizeof(X)), h);
 #pragma unroll
-      for (int i = 0; i < P; ++i) h[i] = __fmul2_rn(COPY ? __ffma2_rn(h[i], two(scale[COPY ? j : 0]), two(-mean)) : __fadd2_rn(h[i], two(-mean)), two(rstd));
+      for (int i = 0; i < P; ++i) h[i] = __fmul2_rn(COPY ? __ffma2_rn(h[i], two(scale[COPY ? j : 0]), two(-mean)) : __fadd2_rn(h[i], two(-mean)), two(rs));
     };
     with_act(g.act, [&](auto act) {
 #pragma unroll
       for (int j = 0; j < ITEMS; ++j) {
         float2 h[P], dy[P];
-        h_values(j, h);
+        h_values(j, h, j < have ? rstd : 0.f);      // (a row that is not there has a dy of zero, and must not have an h that is infinite)
         piece_values<T, V>(load_piece<T, V>(dys + j * R * cg * sizeof(T)), dy);
 #pragma unroll
         for (int i = 0; i < P; ++i) {
@@ -300,10 +301,10 @@ group_norm_warp_grad_kernel(NormArgs g) {
 #pragma unroll
     for (int j = 0; j < ITEMS; ++j) {
       float2 h[P];
-      h_values(j, h);
+      h_values(j, h, rstd);
 #pragma unroll
       for (int i = 0; i < P; ++i) dz[j][i] = __ffma2_rn(dz[j][i], ka[i], __ffma2_rn(h[i], two(m2), two(m1)));
-      if (lr + j * R < rows) {
+      if (j < have) {
         if constexpr (sizeof(T) == 2) *reinterpret_cast<uint2*>(dx) = make_uint2(pack_bf16(dz[j][0].x, dz[j][0].y), pack_bf16(dz[j][1].x, dz[j][1].y));
         else *reinterpret_cast<float4*>(dx) = make_float4(dz[j][0].x, dz[j][0].y, dz[j][1].x, dz[j][1].y);
       }

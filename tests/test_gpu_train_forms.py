@@ -349,3 +349,21 @@ def test_what_is_not_finite_stays_in_its_group(form, bad, dtype):
         for i in (1, 2):
             keep = torch.arange(C, device="cuda") != c
             assert not torch.isfinite(g[i][c]) and torch.equal(g[i][keep], want[i][keep])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("act", ["mish", "silu", "gelu", "none"])
+@pytest.mark.parametrize("N,L,C,G", [(3, 3, 128, 2), (3, 15, 256, 8), (2, 61, 256, 2), (3, 7, 640, 2), (2, 255, 64, 8), (1, 2045, 60, 4)])
+def test_rows_that_are_not_there_count_nothing(N, L, C, G, act, dtype):
+    """Lengths that leave places of a tile without a row, and a mean times rstd past the largest fp32 (2^120 everywhere, rstd of an eps of 2^-40): h is zero where
+    there are rows, so dgamma is zero, and dbeta the sum of dy act'(beta), a sum of L N terms."""
+    rng = np.random.default_rng(L)
+    ga, be = affine(rng, C)
+    x, dy = torch.full((N, L, C), 2.0 ** 120, dtype=TYPES[dtype], device="cuda"), rng_tensor(rng, (N, L, C), dtype, 0.1)
+    mean, rstd = torch.full((N, G), 2.0 ** 120, device="cuda"), torch.full((N, G), 2.0 ** 20, device="cuda")
+    film = rng_tensor(rng, (N, 2 * C), "fp32", 0.5, 0.3)
+    want = host(dy) * host(film)[:, None, :C] * train.act(act, host(be))[1]
+    for s in (None, packed(x)):
+        dx, dga, dbe, dfi = backward(dy, None if s else x, s, ga, be, G, mean, rstd, act, film)
+        assert (dga == 0).all() and torch.isfinite(dx).all() and torch.isfinite(dfi).all()
+        assert (np.abs(host(dbe) - want.sum((0, 1))) <= (DEPTH + 32) * U * (np.abs(host(dy)) * np.abs(host(film))[:, None, :C] * 1.2).sum((0, 1))).all()

@@ -38,7 +38,9 @@ struct Waits {
   Waits() { if (armed_wait) { cycles = armed_wait; withhold = 1; armed_wait = 0; } }
 };
 
+// (The runtime keeps an error until it is read, and the sampler's calls read it behind their launches: it would be taken for theirs.)
 int fail_cuda(const char* what, cudaError_t e) {
+  cudaGetLastError();
   fprintf(stderr, "%s: %s\n", what, cudaGetErrorString(e));
   return TSDP_ERR_CUDA;
 }
@@ -47,7 +49,7 @@ int device_sms(int device) {
   static std::atomic<int> known[MAX_DEVICES];
   int n = known[device].load(std::memory_order_relaxed);
   if (n == 0) {
-    if (cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, device) != cudaSuccess || n < 1) n = 148;
+    if (cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, device) != cudaSuccess || n < 1) { n = 148; cudaGetLastError(); }
     known[device].store(n, std::memory_order_relaxed);
   }
   return n;

@@ -429,8 +429,10 @@ enum { TSDP_MAX_TAPS = 15 };
 
 /* A tensor kept in eight bits: dense rows r = n L + l, q [N L, C] and scale [N L, ceil(C / 32)].  Channels 32 j .. 32 j + 31 of a row
  * stand for q 2^(scale - 127), |q| <= 127; scale is the smallest of 1 .. 248 for which no rounded value exceeds 127, so that a value
- * is off by half a step at most (2^(scale-128), 2^-7 of the block's largest magnitude); rounding to nearest, halves to even.  A
- * block with an infinity or a NaN has scale 255 and stands for NaN. */
+ * is off by half a step at most (2^(scale-128), 1 / 127.5 of the block's largest magnitude); rounding to nearest, halves to even.  A
+ * block with an infinity or a NaN has scale 255 and stands for NaN.  At the ends of the range: where even scale 248 would round a value past
+ * 127 (from 127.5 2^121 on, 0.4 % below the largest fp32), q is 127, and the value is off by up to a step; at scale 1 (blocks below 2^-120) the
+ * half step, 2^-127, is no longer that share of the largest magnitude, and values of at most 2^-127 become zero. */
 typedef struct {
   int8_t* q;
   uint8_t* scale;

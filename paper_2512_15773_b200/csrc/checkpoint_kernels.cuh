@@ -4,10 +4,11 @@
 // q * 2^(b - 127); b is the smallest in 1 .. 248 with max |rint(x 2^(127 - b))| <= 127, and 255 for a block that holds an infinity
 // or a NaN (read back as NaN).  The scale is a power of two, so that scaling is exact in every type, a copy depends on nothing but
 // the values, and what it stands for is exact in bf16 (7 bits and a sign): the backward products take it without a rounding.
-// The one rounding is that to q, half a step at most: |x - q 2^(b-127)| <= 2^(b-128), 2^-7 of the block's largest value.
+// The one rounding is that to q, half a step at most: |x - q 2^(b-127)| <= 2^(b-128), 1 / 127.5 of the block's largest value.  At the ends of the range:
+// from 127.5 2^121 on q stays at 127, off by up to a step (b = 249 would stand for values past the largest fp32); at b = 1 (blocks below 2^-120)
+// the half step is 2^-127 whatever the block's largest value.
 // What bounds them: bytes, next to the arithmetic that finds the largest magnitude.  45056 x 2048, bf16, there and back: 103 us (5.4 TB/s, 0.83 of a plain
 // copy's rate; arithmetic pipe 60 % used).
-// (b = 249 would stand for values past the largest fp32: there q stays at 127 instead.)
 #pragma once
 #include "common.cuh"
 

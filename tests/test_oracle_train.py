@@ -75,3 +75,14 @@ def test_weight_gradient_against_central_differences():
             arr[i] = keep - 0.5; dn = loss()
             arr[i] = keep
             assert abs(up - dn - got[i]) < 1e-11                      # the loss is linear in W and b
+
+
+def test_copies_at_the_ends_of_the_range():
+    """Off by half a step, 1 / 127.5 of the block's largest magnitude; but by up to a step where q is held at 127, and by 2^-127 for the smallest blocks."""
+    x = np.zeros((6, 32))
+    x[:, 0] = [3.4e38, 127.5 * 2.0 ** 121, 127.49 * 2.0 ** 121, 2.0 ** -127, 1.01 * 2.0 ** -127, 127.5 * 2.0 ** -60]
+    q, s = train.pack(x)
+    off, step = np.abs(train.unpack(q, s) - x)[:, 0], 2.0 ** (s[:, 0].astype(float) - 127)
+    assert list(s[:4, 0]) == [248, 248, 248, 1] and list(q[:4, 0]) == [127, 127, 127, 0]
+    assert 0.5 * step[0] < off[0] < step[0] and off[1] == 0.5 * step[1] and (off[2:] <= 0.5 * step[2:]).all()
+    assert s[5, 0] == 68 and q[5, 0] == 64 and off[5] <= x[5, 0] / 127.5

@@ -7,8 +7,8 @@
 // The one rounding is that to q, half a step at most: |x - q 2^(b-127)| <= 2^(b-128), 1 / 127.5 of the block's largest value.  At the ends of the range:
 // from 127.5 2^121 on q stays at 127, off by up to a step (b = 249 would stand for values past the largest fp32); at b = 1 (blocks below 2^-120)
 // the half step is 2^-127 whatever the block's largest value.
-// What bounds them: bytes, next to the arithmetic that finds the largest magnitude.  45056 x 2048, bf16, there and back: 103 us (5.4 TB/s, 0.83 of a plain
-// copy's rate; arithmetic pipe 60 % used).
+// What bounds them: bytes, next to the arithmetic that finds the largest magnitude.  45056 x 2048, bf16, there and back: 106 us (5.3 TB/s, 0.81 of a plain
+// copy's rate; arithmetic pipe 60 % used).  Widths that are not in 16-byte pieces go one value a lane: 45056 x 1003 288 us (0.95 TB/s), fp32 293 (1.6).
 #pragma once
 #include "common.cuh"
 

@@ -14,9 +14,9 @@
 // A cluster of CTAs owns some groups of one sequence, each CTA a share of the positions: statistics need all of a group before its
 // first output.  A thread owns V neighbouring channels (16 bytes) and walks positions, so that the affine and FiLM
 // vectors stay in registers and sums over positions need no exchange until the end.  The second walk reads x (and dy) again: what the cluster has just read is in the L2.
-// What bounds it where sequences are few: the two dependent walks and the exchange between them.  3 x 4099 x 320 in 32 groups, SiLU, fp32: 14 us
-// back to back (2.2 TB/s; issue slots 18 % used); keeping rows in shared memory for the second walk did not help (17.1 us against 15.8), nor did
-// clusters of 16 (29 us: twice the exchange).  16 x 4096 x 512 in 8 groups, Mish, FiLM, bf16: 66 us, backward 139.
+// What bounds it where sequences are few: the two dependent walks and the exchange between them.  3 x 4099 x 320 in 32 groups, SiLU, fp32: 13 us
+// back to back (2.4 TB/s; issue slots 17 % used); keeping rows in shared memory for the second walk did not help (17.1 us against 15.8), nor did
+// clusters of 16 (29 us: twice the exchange).  16 x 4096 x 512 in 8 groups, Mish, FiLM, bf16: 65 us, backward 141.
 // V: four channels a thread, for 16-bit types too (without FiLM 70 us with eight, 58 with four, in the last case), else one at a time.
 #pragma once
 #include "checkpoint_kernels.cuh"

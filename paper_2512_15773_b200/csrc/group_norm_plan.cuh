@@ -36,6 +36,8 @@ inline void norm_plan(NormArgs& g, int V, int elem, int sms, bool grad) {
 
 // The slab kernels' plan: false where a group of one sequence is more than the threads of a CTA hold in registers (SLAB_ITEMS pieces each).
 // A set grows while it fits two pieces a thread and leaves four CTAs' worth of work for each place on the chip.
+// (GN_SLAB_CTAS on an SM is what the registers allow; past 70 KB of shared memory two fit, and the last of their turns is not full: fp32 backward of
+// 2048 x 12 x 640 in two groups, 78 KB.)
 constexpr int SLAB_ITEMS = 4, SLAB_SMEM = 112 * 1024;
 inline int slab_items(const NormArgs& g, int V, int unit, int per_set, int& cols) {
   cols = (per_set * (g.C / g.groups) + V - 1) / V;
@@ -75,9 +77,11 @@ inline bool slab_plan(NormArgs& g, int V, int unit, int elem, int sms, bool grad
 }
 
 // Slabs are taken where a row of a set is a copy worth its name, or all of its rows are one: with copies of 64 to 384 bytes the engine that
-// makes them is what they wait for.  (us, slabs / stream; bf16 unless said: 4096 x 8 x 512 in one group 51 / 107, backward 69 / 139; 4096 x 16 x 256
-// in 32 groups 56 / 95, 96 / 129; 512 bytes: 4096 x 16 x 512 in 32 groups 113 / 157, 182 / 232, fp32 177 / 171, 179 / 237; 384 bytes: 4096 x 16 x 384
-// in 8 groups 130 / 118; 192 bytes: 512 x 16 x 384 in 8 groups 47 / 14, 31 / 27; 128 bytes: 1024 x 64 x 256 in 32 groups 73 / 75, 146 / 96)
+// makes them is what they wait for.  (us, slabs / stream, with FiLM; bf16 unless said.  Forward, backward: 4096 x 8 x 512 in one group 48 / 90,
+// 70 / 138; 2048 x 12 x 640 in two 60 / 87, 69 / 124, fp32 52 / 104, 113 / 128.  4096 x 16 x 512 in 32 groups: 512 bytes forward 104 / 153, fp32 174 / 169,
+// 181 / 237.  4096 x 16 x 384 in 8: 126 / 114, 197 / 202.  Few sequences: 512 x 16 x 384 in 8 47 / 13, 31 / 27.  128 bytes: 1024 x 64 x 256 in 32 68 / 63, 146 / 96.
+// The rule is wrong for backward sets of 256 bytes of many sequences, which it gives to the stream: 4096 x 16 x 512 in 32 180 / 234, 4096 x 16 x 256
+// in 32 94 / 129.)
 inline bool slab_rows(const NormArgs& g, const Rows& r, int elem) { return g.width * elem >= 512 || (g.width == g.C && r.sl == g.C); }
 
 // Teams of warps: false where a group's channels are not 32, 64, 128 or 256 or a lane of eight warps would hold more than `most` pieces of V channels.

@@ -2,9 +2,10 @@
 // (backward in fp32: 16).  Every level of the UNet takes one warp (512 values: 16 x 32, 8 x 64, 4 x 128), a 50 x 128 group eight.
 // Sums pass by shuffles, between the warps of a team through a few words and a barrier of their own; a warp that waits holds up no other
 // team.  A team keeps its group and walks the sequences; the rows of its next one are on their way while it works on this one.
-// What bounds them: instructions (activation, rounding, largest magnitudes of the copies).  4096 x 16 x 512 in 8 groups, Mish,
-// FiLM, bf16: forward with both copies 66 us (3.3 TB/s; 58 % of the issue slots, arithmetic pipe 47 %, 24 warps an SM in 80 registers), backward from
-// a copy 62 us (3.3 TB/s); by slabs 157 and 201.
+// What bounds them: the latency of dependent chains (two reductions a sequence, activation, rounding, the copies' largest magnitudes) at the few warps
+// that the registers leave; no pipe is full.  4096 x 16 x 512 in 8 groups, Mish, FiLM, bf16: forward with both copies 63 us (3.5 TB/s; 58 % of the issue
+// slots, arithmetic pipe 46 %, 24 warps an SM in 80 registers), backward from a copy 63 us (3.2 TB/s; 52 %, special functions 53 %, 16 warps);
+// by slabs 157 and 201.
 // Lanes lie over the group's channels first (16 bytes each, backward four channels), then over positions.  Channels of a group: 32, 64, 128 or 256.
 #pragma once
 #include "group_norm_slab.cuh"

@@ -22,7 +22,7 @@
 // takes WG_CHUNK stages and is then added, rounded, to this CTA's share in the L2, while the other accumulator fills (2048 rows: 5 10^-7 off;
 // 4400 in one go were 1.2 10^-6, 9700 3.7 10^-6).
 // Work is the line of all (tile, stage) pairs, cut into equal pieces, one per CTA, so that no CTA is idle whatever the sizes; a tile that
-// more than one CTA worked on is added up from their shares in the order of the line: the same bits on every run.
+// more than one CTA worked on is added up from their shares in an order that the sizes alone fix: the same bits on every run.
 // Pair form (CG = 2, cta_group::2): a tile of 256 x 256 on two SMs.  Each CTA makes x^ of its own 128 input channels and loads half of the
 // dy columns, so that a stage brings 16 KB less into each SM's shared memory and the tensor core reads 16 KB less of it.  Everything but the
 // MMAs stays within a CTA: the second CTA's idle MMA warp passes on to the first that its stage is complete.

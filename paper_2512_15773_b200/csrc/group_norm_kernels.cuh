@@ -135,9 +135,12 @@ __device__ __forceinline__ float ld_rank_f32(const float* p, uint32_t rank) {   
   return v;
 }
 
-// The variance from the mean square and the mean of values about some point near their mean.  (Rounding may leave the difference of two
-// equal numbers below zero; a NaN stays one.)
+// Mean and variance from the mean and the mean square of values about a point near their mean (the sum of the values, rounded at its size, over their
+// number).  The point is corrected where it is farther from zero than the values are spread: there the sum's roundings count; elsewhere
+// those of the deviations do (16-bit values less a number of 24 bits are all rounded to one side) and the sum itself is the better one.
+// (Rounding may leave the difference of two equal numbers below zero; a NaN stays one.)
 __device__ __forceinline__ float variance_about(float square, float off) { const float v = fmaf(-off, off, square); return v < 0.f ? 0.f : v; }
+__device__ __forceinline__ float mean_about(float about, float square, float off) { return about * about > square ? about + off : about; }
 
 // Positions of lane r of a share that is walked in steps of `lanes`: `all` each, one more in the first `extra`.
 struct LaneRows {
@@ -229,8 +232,10 @@ group_norm_kernel(NormArgs g) {
       for (int gr = t0 / cg + warp; gr * cg < t1; gr += threads / 32) {
         const int a = max(gr * cg, t0) - t0, b = min(gr * cg + cg, t1) - t0, w = b - a, items = w * g.lanes;
         const float inv_w = 1.f / w;                         // (i / w of a few thousand by a product: off by less than the half it stands away from a whole number)
-        // (about one of them: the sum of large means would be rounded at their size)
-        const float about = s_mean[a];
+        // Where the first and the last channel of lane 0 say that means are far from zero against what they and the values differ by, they are summed about
+        // one of them: a sum of large means is rounded at its size.
+        const float first = s_mean[a];
+        const float about = fabsf(first - s_mean[b - 1]) < 0.125f * fabsf(first) && 64.f * s_m2[a] < lane_rows(0) * first * first ? first : 0.f;
         float sum = 0.f;
         for (int i = wl; i < items; i += 32) {
           const int r = (int)((i + 0.5f) * inv_w);

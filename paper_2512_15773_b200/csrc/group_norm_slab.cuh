@@ -203,8 +203,8 @@ group_norm_slab_kernel(NormArgs g) {
     }
     float moments[2] = {in ? t1.x + t1.y : 0.f, in ? t2.x + t2.y : 0.f};
     group_sum<2>(g, gcols, col, lane, in, s_red2, moments);
-    const float off = moments[0] * inv, mean = about + off;
-    const float rstd = rsqrtf(variance_about(moments[1] * inv, off) + g.eps);
+    const float off = moments[0] * inv, square = moments[1] * inv, mean = mean_about(about, square, off);
+    const float rstd = rsqrtf(variance_about(square, off) + g.eps);
     if (in && lane == 0 && col % gcols == 0) {
       const long long at = (long long)n * g.groups + c / cg;
       if (g.mean) g.mean[at] = mean;

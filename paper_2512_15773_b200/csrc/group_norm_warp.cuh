@@ -118,8 +118,8 @@ group_norm_warp_kernel(NormArgs g) {
     }
     float moments[2] = {warp_sum(t1.x + t1.y), warp_sum(t2.x + t2.y)};
     if (TEAM) team_sum(team, s_words2, moments);
-    const float off = moments[0] * inv, mean = about + off;
-    const float rstd = rsqrtf(variance_about(moments[1] * inv, off) + g.eps);
+    const float off = moments[0] * inv, square = moments[1] * inv, mean = mean_about(about, square, off);
+    const float rstd = rsqrtf(variance_about(square, off) + g.eps);
     if (wl == 0 && part == 0) {
       if (g.mean) g.mean[(long long)n * g.groups + grp] = mean;
       if (g.rstd) g.rstd[(long long)n * g.groups + grp] = rstd;

@@ -111,6 +111,20 @@ def test_a_group_of_one_value_has_that_mean(N, L, C, G, value, dtype):
     assert (np.abs(host(rstd) * np.float32(1e-5) ** 0.5 - 1) <= 8 * U).all()
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("form", ["warp", "warps of 32", "team", "slab"])
+def test_near_zero_the_mean_is_that_of_the_sum(form, dtype):
+    """Values of few bits down to 2^-12: sums of 4096 of them are exact (below 2^12), and over 2^k values so is the mean; what corrects a large mean must not
+    spoil it."""
+    N, L, C, G = FORMS[form]
+    g = torch.Generator(device="cuda").manual_seed(C)
+    x = (torch.round(torch.randn(N, L, C, generator=g, device="cuda").bfloat16().float() * 4096) / 4096).to(TYPES[dtype])
+    ga, be = affine(np.random.default_rng(2), C)
+    _, mean, _ = forward(x, ga, be, G)
+    want = x.double().view(N, L, G, C // G).mean((1, 3))
+    assert (want.abs() < 0.5).all() and torch.equal(mean.double(), want)
+
+
 @pytest.mark.parametrize("offset", [0.0, 100.0, 4000.0])
 @pytest.mark.parametrize("form", FORMS)
 def test_far_from_zero_the_mean_is_off_by_its_own_rounding(form, offset):
